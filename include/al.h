@@ -55,7 +55,9 @@
  * the calling thread. Non-finite or negative values in a non-negative state
  * are not detected; their codes are unspecified.
  *
- * Alignment. Every device pointer must be 16-byte aligned (AL_EALIGN).
+ * Alignment. Every device pointer must be 16-byte aligned (AL_EALIGN), except
+ * the activation matrices of the al_act_*, al_norm_*, al_swiglu_* and
+ * al_linear_wgrad calls (see there).
  */
 #ifndef AL_H
 #define AL_H
@@ -315,6 +317,112 @@ al_status al_apollo_workspace_bytes(const al_apollo_tensor* tensors, int32_t nt,
  * workspace of at least the queried size, 256-byte aligned. */
 al_status al_apollo_step(const al_apollo_tensor* tensors, int32_t nt, const al_apollo_cfg* cfg, int64_t step,
                          void* ws, size_t ws_bytes, void* stream);
+
+/* ------------------------------------------------------------------------
+ * Activations in 8 bits, and the operators that save and use them: the code
+ * itself, layer / RMS norm and their backward pass, the gated activation
+ * silu(gate) * up and its backward pass, and a linear layer's weight gradient
+ * from its saved input. The weight gradients come out in the types the
+ * optimizer steps read (al_tensor.grad).
+ *
+ * Matrices. rows x cols, one row per token, element (i, j) at i * ld + j with
+ * ld >= cols (ignored for rows <= 1). fp32 or bf16; any alignment of the
+ * element type and any ld will do (16-byte aligned rows are fastest). Outputs
+ * must not overlap inputs except where an entry point says so. rows and cols
+ * up to 2^31 - 1, rows * ld below 2^48.
+ *
+ * Activation code E8 (block: 32, 64 or 128 columns; blocks do not cross rows;
+ * the last block of a row may be short). For a block with largest magnitude a:
+ *   E = max(1, floor(log2 a) + 121)        (a = 0: E = 1)
+ *   code = clamp(rint(x 2^(127 - E)), -127, 127), ties to even
+ *   decode: code * 2^(E - 127), exact in bf16 and fp32.
+ * The step 2^(E - 127) is between a / 128 and a / 64, so a decoded value is
+ * within half a step of x (up to one step where |x| > 127 steps). A block
+ * holding a NaN or an infinity has E = 255 and codes 0, and decodes to NaN
+ * throughout. codes: int8, rows of nb * block bytes, nb = ceil(cols / block),
+ * columns past cols coded 0; exps: uint8, rows of nb bytes. Both 16-byte
+ * aligned.
+ *
+ * Sums and statistics are fp32 and independent of scheduling: every result
+ * repeats bit for bit. */
+typedef enum al_norm_kind { AL_NORM_LAYER = 0, AL_NORM_RMS = 1 } al_norm_kind;
+
+/* Bytes of the codes and of the exponents of a rows x cols matrix. -1 for a
+ * bad block or a negative size. */
+int64_t al_act_code_bytes(int64_t rows, int64_t cols, int32_t block);
+int64_t al_act_exp_bytes(int64_t rows, int64_t cols, int32_t block);
+
+/* Encode x (dtype: al_dtype) into codes and exps, and decode them into out. */
+al_status al_act_quantize(int32_t dtype, const void* x, int64_t ld, int64_t rows, int64_t cols, int32_t block,
+                          void* codes, void* exps, void* stream);
+al_status al_act_dequantize(const void* codes, const void* exps, int64_t rows, int64_t cols, int32_t block,
+                            int32_t dtype, void* out, int64_t ld, void* stream);
+
+/* Norm over each row: xhat = (x - mean) rstd, rstd = (var + eps)^-1/2 with the
+ * biased variance about the mean (AL_NORM_RMS: mean = 0, var = the mean
+ * square), y = xhat gamma + beta. gamma, beta: cols floats, NULL = 1 and 0;
+ * beta only for AL_NORM_LAYER. x and y have dtype; y may be x itself (same
+ * ld). mean (AL_NORM_LAYER only, else NULL) and rstd: rows floats, NULL where not
+ * wanted. codes, exps: the E8 code of xhat, both NULL where it is not saved
+ * (block is then ignored). xhat is what a backward pass needs of x, and a
+ * linear layer that reads y needs nothing else either (al_linear_wgrad). */
+al_status al_norm_forward(int32_t kind, int32_t dtype, const void* x, int64_t ldx, int64_t rows, int64_t cols,
+                          double eps, const float* gamma, const float* beta, void* y, int64_t ldy, float* mean,
+                          float* rstd, int32_t block, void* codes, void* exps, void* stream);
+
+/* Workspace bytes of al_norm_backward: partial sums of the weight gradients (0 if neither is asked for). */
+al_status al_norm_backward_workspace_bytes(int32_t kind, int32_t dtype, int64_t rows, int64_t cols, size_t* bytes);
+
+/* Backward pass of al_norm_forward. With a = dy gamma and n = cols,
+ *   dx = rstd (a - sum(a) / n [AL_NORM_LAYER] - xhat sum(a xhat) / n) + add
+ *   dgamma = sum over rows of dy xhat, dbeta = sum over rows of dy.
+ * xhat comes from x, mean and rstd (codes = exps = NULL), or from its E8 code
+ * (x = mean = NULL). dy, x, add and dx have dtype; add (NULL: none) is the
+ * gradient that reaches x past the norm; dx may be add itself (same ld).
+ * dgamma, dbeta: cols values of grad_dtype, NULL where not wanted (dbeta only
+ * for AL_NORM_LAYER). ws: at least the queried bytes, 256-byte aligned, may be NULL
+ * when neither is wanted. rows == 0 writes zero weight gradients. */
+al_status al_norm_backward(int32_t kind, int32_t dtype, const void* dy, int64_t lddy, const void* x, int64_t ldx,
+                           const float* mean, const float* rstd, int32_t block, const void* codes, const void* exps,
+                           int64_t rows, int64_t cols, const float* gamma, const void* add, int64_t ldadd, void* dx,
+                           int64_t lddx, int32_t grad_dtype, void* dgamma, void* dbeta, void* ws, size_t ws_bytes,
+                           void* stream);
+
+/* h = silu(gate) * up, silu(g) = g / (1 + e^-g), in fp32, rounded once to
+ * dtype; optionally the E8 codes of gate and up (all four pointers or none). */
+al_status al_swiglu_forward(int32_t dtype, const void* gate, int64_t ldgate, const void* up, int64_t ldup,
+                            int64_t rows, int64_t cols, void* h, int64_t ldh, int32_t block, void* gate_codes,
+                            void* gate_exps, void* up_codes, void* up_exps, void* stream);
+
+/* Backward pass from the codes: with s = 1 / (1 + e^-gate),
+ *   dup = dh gate s, dgate = dh up s (1 + gate (1 - s)),
+ * and optionally (h_codes, h_exps: both or none) the E8 code of the recomputed
+ * h = gate s up, the input that the next linear layer's weight gradient needs. dgate and dup
+ * may share a buffer (two column ranges of one matrix). */
+al_status al_swiglu_backward(int32_t dtype, const void* dh, int64_t lddh, int64_t rows, int64_t cols, int32_t block,
+                             const void* gate_codes, const void* gate_exps, const void* up_codes,
+                             const void* up_exps, void* dgate, int64_t lddgate, void* dup, int64_t lddup,
+                             void* h_codes, void* h_exps, void* stream);
+
+/* Workspace bytes of al_linear_wgrad (partial sums of products split over the
+ * tokens, and of the bias gradient). */
+al_status al_linear_wgrad_workspace_bytes(int32_t dtype, int64_t tokens, int64_t out_features, int64_t in_features,
+                                          size_t* bytes);
+
+/* Weight gradient of y = z W^T (+ bias), W out_features x in_features row-major, z = xhat gamma +
+ * beta, xhat saved as an E8 code (tokens x in_features):
+ *   dw[n][k] = gamma[k] sum_t dy[t][n] xhat[t][k] + beta[k] sum_t dy[t][n] + base[n][k]
+ *   dbias[n] = sum_t dy[t][n]
+ * dy: tokens x out_features of dtype. gamma, beta: in_features floats, NULL = 1 and 0 (a layer
+ * that does not follow a norm has its own input as xhat). base, dw: packed
+ * out_features x in_features of grad_dtype; base NULL = 0, base may be dw
+ * itself (gradient accumulation). dbias: out_features values of grad_dtype or
+ * NULL. The products are exact (both factors are bf16 numbers, an fp32 dy is three
+ * of them) and summed in fp32 on the matrix cores. tokens == 0: dw = base, dbias = 0. */
+al_status al_linear_wgrad(int32_t dtype, const void* dy, int64_t lddy, const void* codes, const void* exps,
+                          int32_t block, int64_t tokens, int64_t out_features, int64_t in_features,
+                          const float* gamma, const float* beta, int32_t grad_dtype, const void* base, void* dw,
+                          void* dbias, void* ws, size_t ws_bytes, void* stream);
 
 /* Diagnostic: evaluate, elementwise on the device, a math primitive the
  * codes rely on, so tests can bound it against the host: fn 0 = hardware

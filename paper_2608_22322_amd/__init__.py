@@ -83,7 +83,10 @@ EXPORTS = ("al_version", "al_last_error", "al_code_bytes", "al_meta_floats", "al
            "al_dequantize", "al_adamw_workspace_bytes", "al_adamw_step", "al_adamw_step_noalloc",
            "al_adafactor_workspace_bytes", "al_came_workspace_bytes",
            "al_adafactor_step", "al_came_step", "al_apollo_workspace_bytes", "al_apollo_step", "al_diag_math",
-           "al_diag_levels", "al_diag_stream", "al_diff_norms", "al_synth_normal")
+           "al_diag_levels", "al_diag_stream", "al_diff_norms", "al_synth_normal",
+           "al_act_code_bytes", "al_act_exp_bytes", "al_act_quantize", "al_act_dequantize", "al_norm_forward",
+           "al_norm_backward_workspace_bytes", "al_norm_backward", "al_swiglu_forward", "al_swiglu_backward",
+           "al_linear_wgrad_workspace_bytes", "al_linear_wgrad")
 
 
 def lib():
@@ -121,11 +124,27 @@ def lib():
         L.al_diag_levels.argtypes = [i32, vp, i64, vp, vp]
         L.al_diag_stream.argtypes = [i32, vp, vp, vp, vp, i64, vp]
         L.al_diff_norms.argtypes = [vp, vp, i64, vp, vp]
+        for name in ("al_act_code_bytes", "al_act_exp_bytes"):
+            getattr(L, name).argtypes = [i64, i64, i32]
+            getattr(L, name).restype = i64
+        L.al_act_quantize.argtypes = [i32, vp, i64, i64, i64, i32, vp, vp, vp]
+        L.al_act_dequantize.argtypes = [vp, vp, i64, i64, i32, i32, vp, i64, vp]
+        L.al_norm_forward.argtypes = [i32, i32, vp, i64, i64, i64, ctypes.c_double, vp, vp, vp, i64, vp, vp, i32, vp, vp, vp]
+        L.al_norm_backward_workspace_bytes.argtypes = [i32, i32, i64, i64, ctypes.POINTER(sz)]
+        L.al_norm_backward.argtypes = [i32, i32, vp, i64, vp, i64, vp, vp, i32, vp, vp, i64, i64, vp, vp, i64, vp, i64,
+                                       i32, vp, vp, vp, sz, vp]
+        L.al_swiglu_forward.argtypes = [i32, vp, i64, vp, i64, i64, i64, vp, i64, i32, vp, vp, vp, vp, vp]
+        L.al_swiglu_backward.argtypes = [i32, vp, i64, i64, i64, i32, vp, vp, vp, vp, vp, i64, vp, i64, vp, vp, vp]
+        L.al_linear_wgrad_workspace_bytes.argtypes = [i32, i64, i64, i64, ctypes.POINTER(sz)]
+        L.al_linear_wgrad.argtypes = [i32, vp, i64, vp, vp, i32, i64, i64, i64, vp, vp, i32, vp, vp, vp, vp, sz, vp]
         for name in ("al_quantize", "al_dequantize", "al_adamw_workspace_bytes", "al_adamw_step", "al_adamw_step_noalloc",
                      "al_adafactor_workspace_bytes",
                      "al_came_workspace_bytes", "al_adafactor_step", "al_came_step", "al_apollo_workspace_bytes",
                      "al_apollo_step", "al_diag_math", "al_diag_levels", "al_diag_stream",
-                     "al_diff_norms", "al_synth_normal"):
+                     "al_diff_norms", "al_synth_normal",
+                     "al_act_quantize", "al_act_dequantize", "al_norm_forward", "al_norm_backward_workspace_bytes",
+                     "al_norm_backward", "al_swiglu_forward", "al_swiglu_backward", "al_linear_wgrad_workspace_bytes",
+                     "al_linear_wgrad"):
             getattr(L, name).restype = ctypes.c_int
         _lib = L
     return _lib

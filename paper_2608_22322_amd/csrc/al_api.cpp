@@ -13,6 +13,7 @@
 
 #include "../../include/al.h"
 #include "../../include/al_synth.h"
+#include "act_internal.hpp"
 #include "al_internal.hpp"
 
 namespace {
@@ -469,6 +470,10 @@ al_status apollo_plan(const al_apollo_tensor* ts, int nt, const al_apollo_cfg* c
 }  // namespace
 
 namespace al {
+
+al_status api_fail(al_status s, const char* msg) { return fail(s, "%s", msg); }
+
+void api_clear() { g_err[0] = 0; }
 
 int device_cu_count() {
     static std::mutex mu;

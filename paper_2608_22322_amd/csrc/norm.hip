@@ -1,0 +1,501 @@
+// Layer and RMS norm over the rows of a matrix, and their backward pass with
+// the reduction of the weight gradients.
+//
+// A group of G lanes (a wavefront, or a workgroup of up to 1024) holds one row
+// in registers, K chunks of 8 columns per lane, so x is read once and the variance
+// is taken about the mean. Rows wider than 16384 columns go through kernels that read
+// the row again instead.
+#include <algorithm>
+
+#include "act_device.hpp"
+
+namespace al {
+
+namespace {
+
+constexpr int kRowMax = 16384;  // widest row held in registers
+
+// The pitch that chunks are numbered over: the code's, or the width in whole chunks.
+__device__ __forceinline__ void load8f(const float* p, int c, int cols, float fill, float (&v)[8]) {
+    if (c + 8 <= cols) {
+        const u32x4 a = *reinterpret_cast<const u32x4_a4*>(p + c), b = *reinterpret_cast<const u32x4_a4*>(p + c + 4);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) v[j] = bits_f(a[j]), v[4 + j] = bits_f(b[j]);
+    } else {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) v[j] = c + j < cols ? p[c + j] : fill;
+    }
+}
+
+// Sum over the G lanes of a group, the same in every lane. G > 64: the group is the workgroup; `buf` holds a
+// float per wavefront for each of the kernel's sums in turn (double-buffered by the caller).
+template <int G>
+__device__ __forceinline__ float group_sum(float v, float* buf) {
+    v = wave_sum(v);
+    if constexpr (G > 64) {
+        if ((threadIdx.x & 63) == 0) buf[threadIdx.x >> 6] = v;
+        __syncthreads();
+        v = 0.0f;
+#pragma unroll
+        for (int w = 0; w < G / 64; ++w) v += buf[w];
+    }
+    return v;
+}
+
+__device__ __forceinline__ float sum8(const float (&v)[8]) {
+    return ((v[0] + v[1]) + (v[2] + v[3])) + ((v[4] + v[5]) + (v[6] + v[7]));
+}
+
+// Columns of a chunk at c that lie inside the row.
+__device__ __forceinline__ int inside(int c, int cols) { return min(8, max(0, cols - c)); }
+
+template <typename T, int G, int K>
+__global__ __launch_bounds__(G < 256 ? 256 : G) void norm_forward_kernel(NormForward a, bool layer) {
+    constexpr int R = G < 256 ? 256 / G : 1;  // rows per workgroup
+    __shared__ float buf[2][16];
+    const int lane = threadIdx.x % G, cols = a.s.cols;
+    const int64_t row = a.row0 + (int64_t)blockIdx.x * R + threadIdx.x / G;
+    if (row >= a.s.rows) return;  // a whole group
+    const T* const x = static_cast<const T*>(a.x.p) + row * a.x.ld;
+    Chunk<T> raw[K];
+#pragma unroll
+    for (int k = 0; k < K; ++k) load_chunk(raw[k], x, (k * G + lane) * 8, cols);
+    float v[K][8], sum = 0.0f;
+#pragma unroll
+    for (int k = 0; k < K; ++k) {
+        raw[k].get(v[k]);
+        sum += sum8(v[k]);
+    }
+    float mean = 0.0f;
+    if (layer) {
+        mean = group_sum<G>(sum, buf[0]) / (float)cols;
+#pragma unroll
+        for (int k = 0; k < K; ++k) {
+            const int n = inside((k * G + lane) * 8, cols);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) v[k][j] = j < n ? v[k][j] - mean : 0.0f;
+        }
+    }
+    float sq = 0.0f;
+#pragma unroll
+    for (int k = 0; k < K; ++k) {
+        float t[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) t[j] = v[k][j] * v[k][j];
+        sq += sum8(t);
+    }
+    const float rstd = 1.0f / sqrtf(group_sum<G>(sq, buf[1]) / (float)cols + a.eps);
+    if (lane == 0) {
+        if (a.mean) a.mean[row] = mean;
+        if (a.rstd) a.rstd[row] = rstd;
+    }
+    T* const y = static_cast<T*>(a.y.p) + row * a.y.ld;
+#pragma unroll
+    for (int k = 0; k < K; ++k) {
+        const int c = (k * G + lane) * 8;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) v[k][j] *= rstd;
+        if (a.c.p) {
+            const uint32_t e = e8_exp(group_max(max_bits(v[k]), a.s.lb));
+            if (c < a.s.pitch) {
+                *reinterpret_cast<u32x2*>(a.c.p + row * a.s.pitch + c) = e8_encode(v[k], e);
+                const int b = c >> (3 + a.s.lb);
+                if (c == b << (3 + a.s.lb)) a.c.e[row * a.s.nb + b] = (uint8_t)e;
+            }
+        }
+        if (c < cols) {
+            float w[8];
+            if (a.gamma) {
+                load8f(a.gamma, c, cols, 0.0f, w);
+#pragma unroll
+                for (int j = 0; j < 8; ++j) v[k][j] *= w[j];
+            }
+            if (a.beta) {
+                load8f(a.beta, c, cols, 0.0f, w);
+#pragma unroll
+                for (int j = 0; j < 8; ++j) v[k][j] += w[j];
+            }
+            store_chunk(y, c, cols, v[k]);
+        }
+    }
+}
+
+// Rows of any width: one workgroup per row, the row read three times (from the cache after the first).
+template <typename T>
+__global__ __launch_bounds__(1024) void norm_forward_wide_kernel(NormForward a, bool layer) {
+    constexpr int G = 1024;
+    __shared__ float buf[2][16];
+    const int cols = a.s.cols;
+    const int64_t row = a.row0 + blockIdx.x;
+    const T* const x = static_cast<const T*>(a.x.p) + row * a.x.ld;
+    T* const y = static_cast<T*>(a.y.p) + row * a.y.ld;
+    Chunk<T> raw;
+    float v[8], mean = 0.0f, sum = 0.0f;
+    if (layer) {
+        for (int c = threadIdx.x * 8; c < cols; c += G * 8) {
+            load_chunk(raw, x, c, cols);
+            raw.get(v);
+            sum += sum8(v);
+        }
+        mean = group_sum<G>(sum, buf[0]) / (float)cols;
+    }
+    sum = 0.0f;
+    for (int c = threadIdx.x * 8; c < cols; c += G * 8) {
+        load_chunk(raw, x, c, cols);
+        raw.get(v);
+        const int n = inside(c, cols);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) v[j] = j < n ? (v[j] - mean) * (v[j] - mean) : 0.0f;
+        sum += sum8(v);
+    }
+    const float rstd = 1.0f / sqrtf(group_sum<G>(sum, buf[1]) / (float)cols + a.eps);
+    if (threadIdx.x == 0) {
+        if (a.mean) a.mean[row] = mean;
+        if (a.rstd) a.rstd[row] = rstd;
+    }
+    // the trip count is the same in a whole wavefront, which a block's maximum needs
+    for (int c0 = 0; c0 < a.s.pitch; c0 += G * 8) {
+        const int c = c0 + threadIdx.x * 8, n = inside(c, cols);
+        load_chunk(raw, x, c, cols);
+        raw.get(v);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) v[j] = j < n ? (v[j] - mean) * rstd : 0.0f;
+        if (a.c.p) {
+            const uint32_t e = e8_exp(group_max(max_bits(v), a.s.lb));
+            if (c < a.s.pitch) {
+                *reinterpret_cast<u32x2*>(a.c.p + row * a.s.pitch + c) = e8_encode(v, e);
+                const int b = c >> (3 + a.s.lb);
+                if (c == b << (3 + a.s.lb)) a.c.e[row * a.s.nb + b] = (uint8_t)e;
+            }
+        }
+        if (c >= cols) continue;
+        float w[8];
+        if (a.gamma) {
+            load8f(a.gamma, c, cols, 0.0f, w);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) v[j] *= w[j];
+        }
+        if (a.beta) {
+            load8f(a.beta, c, cols, 0.0f, w);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) v[j] += w[j];
+        }
+        store_chunk(y, c, cols, v);
+    }
+}
+
+// ------------------------------------------------------------ backward
+// What a lane reads of one row's chunk.
+template <typename T, bool CODE>
+struct RowChunk {
+    Chunk<T> dy, x, add;
+    u32x2 q;
+    uint32_t e;
+    __device__ __forceinline__ void load(const NormBackward& a, int64_t row, int c) {
+        const int cols = a.s.cols;
+        load_chunk(dy, static_cast<const T*>(a.dy.p) + row * a.dy.ld, c, cols);
+        if constexpr (CODE) {
+            q = 0u;
+            e = 0u;
+            if (c < cols) {
+                q = *reinterpret_cast<const u32x2*>(a.c.p + row * a.s.pitch + c);
+                e = a.c.e[row * a.s.nb + (c >> (3 + a.s.lb))];
+            }
+        } else {
+            load_chunk(x, static_cast<const T*>(a.x.p) + row * a.x.ld, c, cols);
+        }
+        if (a.add.p) load_chunk(add, static_cast<const T*>(a.add.p) + row * a.add.ld, c, cols);
+    }
+    // xhat; columns past the width give 0
+    __device__ __forceinline__ void xhat(float mean, float rstd, int n, float (&v)[8]) const {
+        if constexpr (CODE) {
+            e8_decode(q, e, v);
+        } else {
+            x.get(v);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) v[j] = j < n ? (v[j] - mean) * rstd : 0.0f;
+        }
+    }
+};
+
+// Rows r0, r0 + gridDim * R, ...: dx of each, and the group's sums over its rows of dy xhat and dy.
+template <typename T, int G, int K, bool CODE, bool LAYER>
+__global__ __launch_bounds__(G < 256 ? 256 : G) void norm_backward_kernel(NormBackward a) {
+    constexpr int R = G < 256 ? 256 / G : 1;  // rows at a time
+    __shared__ float buf[2][2][16];
+    __shared__ float fold[R > 1 ? R * G * 8 : 1];
+    const int lane = threadIdx.x % G, group = threadIdx.x / G, cols = a.s.cols;
+    const float inv_n = 1.0f / (float)cols;
+    float gam[K][8], dg[K][8], db[K][8];
+#pragma unroll
+    for (int k = 0; k < K; ++k) {
+        const int c = (k * G + lane) * 8;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) gam[k][j] = 1.0f, dg[k][j] = db[k][j] = 0.0f;
+        if (a.gamma) load8f(a.gamma, c, cols, 0.0f, gam[k]);
+    }
+    int turn = 0;
+    for (int64_t row = (int64_t)blockIdx.x * R + group; row < a.s.rows; row += (int64_t)gridDim.x * R, turn ^= 1) {
+        RowChunk<T, CODE> r[K];
+#pragma unroll
+        for (int k = 0; k < K; ++k) r[k].load(a, row, (k * G + lane) * 8);
+        const float rstd = a.rstd[row], mean = LAYER && !CODE ? a.mean[row] : 0.0f;
+        float s1 = 0.0f, s2 = 0.0f;
+#pragma unroll
+        for (int k = 0; k < K; ++k) {
+            float xh[8], dy[8], t[8], u[8];
+            r[k].xhat(mean, rstd, inside((k * G + lane) * 8, cols), xh);
+            r[k].dy.get(dy);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                dg[k][j] += dy[j] * xh[j];
+                if (LAYER) db[k][j] += dy[j];
+                t[j] = dy[j] * gam[k][j];
+                u[j] = t[j] * xh[j];
+            }
+            s1 += sum8(t);
+            s2 += sum8(u);
+        }
+        if (LAYER) s1 = group_sum<G>(s1, buf[turn][0]) * inv_n;
+        s2 = group_sum<G>(s2, buf[turn][1]) * inv_n;
+        T* const dx = static_cast<T*>(a.dx.p) + row * a.dx.ld;
+#pragma unroll
+        for (int k = 0; k < K; ++k) {
+            const int c = (k * G + lane) * 8;
+            float xh[8], v[8];
+            r[k].xhat(mean, rstd, inside(c, cols), xh);
+            r[k].dy.get(v);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                v[j] = v[j] * gam[k][j] - xh[j] * s2;
+                if (LAYER) v[j] -= s1;
+                v[j] *= rstd;
+            }
+            if (a.add.p) {
+                float w[8];
+                r[k].add.get(w);
+#pragma unroll
+                for (int j = 0; j < 8; ++j) v[j] += w[j];
+            }
+            if (c < cols) store_chunk(dx, c, cols, v);
+        }
+    }
+    if (!a.part) return;
+    // the workgroup's sums: its R groups in order, then one row of partials each for dgamma and dbeta
+    for (int which = 0; which < (LAYER ? 2 : 1); ++which) {
+        float* const out = a.part + ((int64_t)which * a.parts + blockIdx.x) * cols;
+#pragma unroll
+        for (int k = 0; k < K; ++k) {
+            const int c = (k * G + lane) * 8;
+            float v[8];
+#pragma unroll
+            for (int j = 0; j < 8; ++j) v[j] = which ? db[k][j] : dg[k][j];
+            if constexpr (R > 1) {
+                __syncthreads();
+#pragma unroll
+                for (int j = 0; j < 8; ++j) fold[(group * 8 + j) * G + lane] = v[j];
+                __syncthreads();
+                if (group == 0) {
+#pragma unroll
+                    for (int g = 1; g < R; ++g)
+#pragma unroll
+                        for (int j = 0; j < 8; ++j) v[j] += fold[(g * 8 + j) * G + lane];
+                }
+            }
+            if (group == 0 && c < cols) store_chunk(out, c, cols, v);
+        }
+    }
+}
+
+// Rows of any width: dx alone, one workgroup per row, its row read twice.
+template <typename T, bool CODE, bool LAYER>
+__global__ __launch_bounds__(1024) void norm_backward_wide_kernel(NormBackward a) {
+    constexpr int G = 1024;
+    __shared__ float buf[2][16];
+    const int cols = a.s.cols;
+    const int64_t row = a.row0 + blockIdx.x;
+    const float rstd = a.rstd[row], mean = LAYER && !CODE ? a.mean[row] : 0.0f, inv_n = 1.0f / (float)cols;
+    T* const dx = static_cast<T*>(a.dx.p) + row * a.dx.ld;
+    RowChunk<T, CODE> r;
+    float s1 = 0.0f, s2 = 0.0f, xh[8], dy[8], gam[8];
+    for (int c = threadIdx.x * 8; c < cols; c += G * 8) {
+        r.load(a, row, c);
+        r.xhat(mean, rstd, inside(c, cols), xh);
+        r.dy.get(dy);
+        float t[8], u[8];
+        if (a.gamma) load8f(a.gamma, c, cols, 0.0f, gam);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            t[j] = a.gamma ? dy[j] * gam[j] : dy[j];
+            u[j] = t[j] * xh[j];
+        }
+        s1 += sum8(t);
+        s2 += sum8(u);
+    }
+    s1 = LAYER ? group_sum<G>(s1, buf[0]) * inv_n : 0.0f;
+    s2 = group_sum<G>(s2, buf[1]) * inv_n;
+    for (int c = threadIdx.x * 8; c < cols; c += G * 8) {
+        r.load(a, row, c);
+        r.xhat(mean, rstd, inside(c, cols), xh);
+        r.dy.get(dy);
+        if (a.gamma) load8f(a.gamma, c, cols, 0.0f, gam);
+        float w[8], v[8];
+        if (a.add.p) r.add.get(w);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            v[j] = ((a.gamma ? dy[j] * gam[j] : dy[j]) - xh[j] * s2 - s1) * rstd;
+            if (a.add.p) v[j] += w[j];
+        }
+        store_chunk(dx, c, cols, v);
+    }
+}
+
+// The weight gradients of wide rows: a lane holds 8 columns, a workgroup (blockIdx.y) every parts-th row.
+template <typename T, bool CODE, bool LAYER>
+__global__ __launch_bounds__(64) void norm_weights_wide_kernel(NormBackward a) {
+    const int cols = a.s.cols, c = (blockIdx.x * 64 + threadIdx.x) * 8;
+    if (c >= cols) return;
+    a.add.p = nullptr;
+    float dg[8] = {}, db[8] = {};
+    for (int64_t row = blockIdx.y; row < a.s.rows; row += a.parts) {
+        RowChunk<T, CODE> r;
+        r.load(a, row, c);
+        float xh[8], dy[8];
+        r.xhat(LAYER && !CODE ? a.mean[row] : 0.0f, a.rstd[row], inside(c, cols), xh);
+        r.dy.get(dy);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) dg[j] += dy[j] * xh[j], db[j] += dy[j];
+    }
+    store_chunk(a.part + (int64_t)blockIdx.y * cols, c, cols, dg);
+    if (LAYER) store_chunk(a.part + ((int64_t)a.parts + blockIdx.y) * cols, c, cols, db);
+}
+
+// out[c] = sum over p of part[p][c]: 64 columns a workgroup, 4 wavefronts taking every fourth row.
+template <typename O>
+__global__ __launch_bounds__(256) void fold_kernel(const float* part, int32_t parts, int64_t cols, O* out) {
+    __shared__ float buf[4][64];
+    const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
+    const int64_t c = (int64_t)blockIdx.x * 64 + lane;
+    float s = 0.0f;
+    if (c < cols) {
+        float t[4] = {};
+        int p = w;
+        for (; p + 12 < parts; p += 16)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) t[i] += part[(int64_t)(p + 4 * i) * cols + c];
+        for (; p < parts; p += 4) t[0] += part[(int64_t)p * cols + c];
+        s = (t[0] + t[1]) + (t[2] + t[3]);
+    }
+    buf[w][lane] = s;
+    __syncthreads();
+    if (w == 0 && c < cols) put(out + c, (buf[0][lane] + buf[1][lane]) + (buf[2][lane] + buf[3][lane]));
+}
+
+// Lanes and chunks per lane that hold a row of `chunks` chunks.
+struct Shape {
+    int g, k;
+};
+Shape row_shape(int64_t chunks) {
+    for (int k = 1; k <= 4; k *= 2)
+        if (chunks <= 64 * k) return {64, k};
+    for (int k = 2; k <= 4; k *= 2)
+        if (chunks <= 256 * k) return {256, k};
+    return {1024, 2};
+}
+
+constexpr int64_t kSlab = 1 << 21;  // rows of one launch (a grid holds fewer than 2^32 threads)
+
+template <typename T>
+hipError_t forward_slab(bool layer, const NormForward& a, int64_t rows, hipStream_t st) {
+    if (a.s.pitch > kRowMax) {
+        norm_forward_wide_kernel<T><<<dim3((uint32_t)rows), 1024, 0, st>>>(a, layer);
+        return hipGetLastError();
+    }
+    const Shape s = row_shape(a.s.pitch / 8);
+    const dim3 n((uint32_t)(s.g == 64 ? (rows + 3) / 4 : rows));
+    if (s.g == 64 && s.k == 1)
+        norm_forward_kernel<T, 64, 1><<<n, 256, 0, st>>>(a, layer);
+    else if (s.g == 64 && s.k == 2)
+        norm_forward_kernel<T, 64, 2><<<n, 256, 0, st>>>(a, layer);
+    else if (s.g == 64)
+        norm_forward_kernel<T, 64, 4><<<n, 256, 0, st>>>(a, layer);
+    else if (s.g == 256 && s.k == 2)
+        norm_forward_kernel<T, 256, 2><<<n, 256, 0, st>>>(a, layer);
+    else if (s.g == 256)
+        norm_forward_kernel<T, 256, 4><<<n, 256, 0, st>>>(a, layer);
+    else
+        norm_forward_kernel<T, 1024, 2><<<n, 1024, 0, st>>>(a, layer);
+    return hipGetLastError();
+}
+
+template <typename T>
+hipError_t forward(bool layer, NormForward a, hipStream_t st) {
+    hipError_t e = hipSuccess;
+    for (a.row0 = 0; a.row0 < a.s.rows && e == hipSuccess; a.row0 += kSlab)
+        e = forward_slab<T>(layer, a, std::min(kSlab, a.s.rows - a.row0), st);
+    return e;
+}
+
+template <typename T, bool CODE, bool LAYER>
+hipError_t backward(NormBackward a, hipStream_t st) {
+    if (a.s.cols > kRowMax) {
+        for (a.row0 = 0; a.row0 < a.s.rows; a.row0 += kSlab)
+            norm_backward_wide_kernel<T, CODE, LAYER><<<dim3((uint32_t)std::min(kSlab, a.s.rows - a.row0)), 1024, 0, st>>>(a);
+        if (a.part)
+            norm_weights_wide_kernel<T, CODE, LAYER><<<dim3((uint32_t)((a.s.cols + 511) / 512), (uint32_t)a.parts), 64, 0, st>>>(a);
+        return hipGetLastError();
+    }
+    const Shape s = row_shape((a.s.cols + 7) / 8);
+    const dim3 n((uint32_t)a.parts);
+    if (s.g == 64 && s.k == 1)
+        norm_backward_kernel<T, 64, 1, CODE, LAYER><<<n, 256, 0, st>>>(a);
+    else if (s.g == 64 && s.k == 2)
+        norm_backward_kernel<T, 64, 2, CODE, LAYER><<<n, 256, 0, st>>>(a);
+    else if (s.g == 64)
+        norm_backward_kernel<T, 64, 4, CODE, LAYER><<<n, 256, 0, st>>>(a);
+    else if (s.g == 256 && s.k == 2)
+        norm_backward_kernel<T, 256, 2, CODE, LAYER><<<n, 256, 0, st>>>(a);
+    else if (s.g == 256)
+        norm_backward_kernel<T, 256, 4, CODE, LAYER><<<n, 256, 0, st>>>(a);
+    else
+        norm_backward_kernel<T, 1024, 2, CODE, LAYER><<<n, 1024, 0, st>>>(a);
+    return hipGetLastError();
+}
+
+template <typename T>
+hipError_t backward(bool layer, const NormBackward& a, hipStream_t st) {
+    if (a.c.p) return layer ? backward<T, true, true>(a, st) : backward<T, true, false>(a, st);
+    return layer ? backward<T, false, true>(a, st) : backward<T, false, false>(a, st);
+}
+
+}  // namespace
+
+hipError_t launch_fold(int grad_dtype, const float* part, int32_t parts, int64_t cols, void* out, hipStream_t st) {
+    const dim3 n((uint32_t)((cols + 63) / 64));
+    if (grad_dtype == AL_DTYPE_BF16)
+        fold_kernel<bf16><<<n, 256, 0, st>>>(part, parts, cols, static_cast<bf16*>(out));
+    else
+        fold_kernel<float><<<n, 256, 0, st>>>(part, parts, cols, static_cast<float*>(out));
+    return hipGetLastError();
+}
+
+hipError_t launch_norm_forward(int dtype, bool layer, const NormForward& a, hipStream_t st) {
+    return dtype == AL_DTYPE_BF16 ? forward<bf16>(layer, a, st) : forward<float>(layer, a, st);
+}
+
+int32_t norm_backward_parts(int dtype, bool layer, int64_t rows, int64_t cols) {
+    const Shape s = row_shape((cols + 7) / 8);
+    const int64_t at_a_time = s.g == 64 ? 4 : 1, most = cols > kRowMax ? 64 : 1024;
+    return (int32_t)std::min((rows + at_a_time - 1) / at_a_time, most);
+}
+
+hipError_t launch_norm_backward(int dtype, bool layer, int grad_dtype, const NormBackward& a, hipStream_t st) {
+    hipError_t e = hipSuccess;
+    if (a.s.rows > 0) e = dtype == AL_DTYPE_BF16 ? backward<bf16>(layer, a, st) : backward<float>(layer, a, st);
+    if (e == hipSuccess && a.dgamma) e = launch_fold(grad_dtype, a.part, a.parts, a.s.cols, a.dgamma, st);
+    if (e == hipSuccess && a.dbeta)
+        e = launch_fold(grad_dtype, a.part + (int64_t)a.parts * a.s.cols, a.parts, a.s.cols, a.dbeta, st);
+    return e;
+}
+
+}  // namespace al

@@ -1,0 +1,252 @@
+// Weight gradient of a linear layer from its input's E8 code, on the matrix
+// cores: dw[n][k] = sum over tokens t of dy[t][n] xhat[t][k].
+//
+// Both factors are bf16 numbers (a code is 7 bits and a sign times a power of two; an
+// fp32 dy is the sum of three bf16 numbers, taken in three turns), so every
+// product is exact and the sums are the matrix cores' fp32 ones.
+#include <algorithm>
+
+#include "act_device.hpp"
+
+namespace al {
+
+namespace {
+
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef __attribute__((address_space(3))) s16x4* lds_s16x4;
+typedef __attribute__((address_space(3))) uint16_t* lds_u16;
+
+// Both tiles lie in LDS as they do in memory, a row per token. A transposing read gives lane l of
+// a wavefront the 4 tokens 4 (l / 16) + 0..3 of column l % 16: two of them make the 8-token fragment of
+// a 16 x 16 x 32 product (which token comes at which place does not matter, as both factors
+// agree). The 16 rows that one read touches lie in different 32-byte units: unit u of row t is at u ^ (t & 7).
+constexpr int kSmallTile = 128, kSmallTokens = 32;
+
+__device__ __forceinline__ int small_at(int t, int c) { return t * kSmallTile + ((((c >> 4) ^ (t & 7)) << 4) | (c & 15)); }
+
+// The bf16 part `which` (0, 1, 2) of fp32 values: x = x0 + x1 + x2 exactly, by truncation; infinities and NaN
+// are in part 0 alone.
+__device__ __forceinline__ uint32_t split_part(uint32_t x, int which) {
+    const bool fin = (x & 0x7f800000u) != 0x7f800000u;
+    if (!fin) return which == 0 ? (x & 0x007fffffu ? 0x7fc0u : x >> 16) : 0u;
+    const uint32_t h = x & 0xffff0000u;
+    if (which == 0) return h >> 16;
+    const float r = bits_f(x) - bits_f(h);
+    const uint32_t m = f_bits(r) & 0xffff0000u;
+    if (which == 1) return m >> 16;
+    return f_bits(r - bits_f(m)) >> 16;
+}
+
+template <typename T>
+__device__ __forceinline__ u32x4 as_bf16(const Chunk<T>& k, int which);
+template <>
+__device__ __forceinline__ u32x4 as_bf16<bf16>(const Chunk<bf16>& k, int) {
+    return k.q;
+}
+template <>
+__device__ __forceinline__ u32x4 as_bf16<float>(const Chunk<float>& k, int which) {
+    u32x4 q;
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+        q[j] = split_part(k.a[2 * j], which) | split_part(k.a[2 * j + 1], which) << 16;
+        q[2 + j] = split_part(k.b[2 * j], which) | split_part(k.b[2 * j + 1], which) << 16;
+    }
+    return q;
+}
+
+__device__ __forceinline__ bf16x8 fragment(const uint16_t* tile, int c0, int lane) {
+    const int t = 4 * (lane >> 4) + ((lane >> 2) & 3), c = c0 + 4 * (lane & 3);
+    union {
+        s16x4 h[2];
+        bf16x8 f;
+    } u;
+    u.h[0] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4)(lds_u16)(uint16_t*)(tile + small_at(t, c)));
+    u.h[1] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4)(lds_u16)(uint16_t*)(tile + small_at(t + 16, c)));
+    return u.f;
+}
+
+__device__ __forceinline__ float grad_at(const bf16* p, int64_t i) { return to_f(p[i]); }
+__device__ __forceinline__ float grad_at(const float* p, int64_t i) { return p[i]; }
+
+// One finished sum: scale, shift, base, and the only rounding.
+template <typename O>
+__device__ __forceinline__ void finish(const Wgrad& a, int64_t n, int k, float v) {
+    const int64_t i = n * a.s.cols + k;
+    if (a.gamma) v *= a.gamma[k];
+    if (a.beta) v += a.beta[k] * a.bsum[n];
+    if (a.base) v += grad_at(static_cast<const O*>(a.base), i);
+    put(static_cast<O*>(a.dw) + i, v);
+}
+
+// 128 x 128 outputs, 4 wavefronts of 64 x 64, 32 tokens a step, any size and alignment.
+template <typename T, typename O>
+__global__ __launch_bounds__(256) void wgrad_small_kernel(Wgrad a) {
+    __shared__ __attribute__((aligned(16))) uint16_t dy_s[2][kSmallTokens * kSmallTile], x_s[2][kSmallTokens * kSmallTile];
+    constexpr int PARTS = sizeof(T) == 4 ? 3 : 1;
+    const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
+    const int64_t n0 = (int64_t)blockIdx.y * kSmallTile;
+    const int k0 = blockIdx.x * kSmallTile;
+    // this split's tokens
+    const int64_t steps = (a.s.rows + kSmallTokens - 1) / kSmallTokens;
+    const int64_t s0 = steps * blockIdx.z / a.splits, s1 = steps * (blockIdx.z + 1) / a.splits;
+
+    Chunk<T> dy[2];
+    u32x2 xq[2];
+    uint32_t xe[2];
+    const int cc = (tid & 15) * 8;  // this thread's columns; tokens tid / 16 and tid / 16 + 16
+    const int out = (int)std::min<int64_t>(a.out - n0, kSmallTile);
+    const auto load = [&](int64_t step) {
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            const int64_t t = step * kSmallTokens + (tid >> 4) + 16 * i;
+            dy[i].zero();
+            xq[i] = 0u;
+            xe[i] = 0u;
+            if (t >= a.s.rows) continue;
+            load_chunk(dy[i], static_cast<const T*>(a.dy.p) + t * a.dy.ld + n0, cc, out);
+            if (k0 + cc < a.s.pitch) {
+                xq[i] = *reinterpret_cast<const u32x2*>(a.c.p + t * a.s.pitch + k0 + cc);
+                xe[i] = a.c.e[t * a.s.nb + ((k0 + cc) >> (3 + a.s.lb))];
+            }
+        }
+    };
+    const auto stage = [&](int b, int part) {
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            const int t = (tid >> 4) + 16 * i;
+            *reinterpret_cast<u32x4*>(&dy_s[b][small_at(t, cc)]) = as_bf16<T>(dy[i], part);
+            float v[8];
+            e8_decode(xq[i], xe[i], v);
+            u32x4 q;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) q[j] = (f_bits(v[2 * j]) >> 16) | (f_bits(v[2 * j + 1]) & 0xffff0000u);
+            *reinterpret_cast<u32x4*>(&x_s[b][small_at(t, cc)]) = q;
+        }
+    };
+    const int wn = (w >> 1) * 64, wk = (w & 1) * 64;
+    f32x4 acc[4][4] = {};
+    int b = 0;
+    if (s0 < s1) load(s0);
+    for (int64_t s = s0; s < s1; ++s) {
+        for (int part = 0; part < PARTS; ++part, b ^= 1) {
+            stage(b, part);
+            __syncthreads();
+            if (part == PARTS - 1 && s + 1 < s1) load(s + 1);
+            bf16x8 fx[4], fy[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                fx[i] = fragment(x_s[b], wk + 16 * i, lane);
+                fy[i] = fragment(dy_s[b], wn + 16 * i, lane);
+            }
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+#pragma unroll
+                for (int j = 0; j < 4; ++j)
+                    acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fx[j], fy[i], acc[i][j], 0, 0, 0);
+        }
+    }
+    // lane: row n = l % 16, columns k = 4 (l / 16) + 0..3
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const int64_t n = n0 + wn + 16 * i + (lane & 15);
+        if (n >= a.out) continue;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const int k = k0 + wk + 16 * j + 4 * (lane >> 4);
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                if (k + r >= a.s.cols) continue;
+                if (a.splits > 1)
+                    a.part[((int64_t)blockIdx.z * a.out + n) * a.s.cols + k + r] = acc[i][j][r];
+                else
+                    finish<O>(a, n, k + r, acc[i][j][r]);
+            }
+        }
+    }
+}
+
+// The splits' partial products, added in order.
+template <typename O>
+__global__ __launch_bounds__(256) void wgrad_join_kernel(Wgrad a) {
+    const int64_t total = a.out * a.s.cols;
+    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < total; i += (int64_t)gridDim.x * 256) {
+        float v = 0.0f;
+        for (int s = 0; s < a.splits; ++s) v += a.part[(int64_t)s * total + i];
+        const int64_t n = i / a.s.cols;
+        finish<O>(a, n, (int)(i - n * a.s.cols), v);
+    }
+}
+
+// Column sums of dy over every bparts-th slab of 64 rows: 8 columns a lane, 4 wavefronts a workgroup.
+template <typename T>
+__global__ __launch_bounds__(256) void dy_sum_kernel(Wgrad a) {
+    __shared__ float buf[3][64 * 8];
+    const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
+    const int64_t c = ((int64_t)blockIdx.x * 64 + lane) * 8;
+    float s[8] = {};
+    if (c < a.out) {
+        const int64_t r0 = a.s.rows * blockIdx.y / a.bparts, r1 = a.s.rows * (blockIdx.y + 1) / a.bparts;
+        for (int64_t r = r0 + w; r < r1; r += 4) {
+            Chunk<T> k;
+            const T* const row = static_cast<const T*>(a.dy.p) + r * a.dy.ld + c;
+            load_chunk(k, row, 0, (int)std::min<int64_t>(8, a.out - c));
+            float v[8];
+            k.get(v);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) s[j] += v[j];
+        }
+    }
+    if (w > 0)
+        for (int j = 0; j < 8; ++j) buf[w - 1][j * 64 + lane] = s[j];
+    __syncthreads();
+    if (w > 0 || c >= a.out) return;
+    for (int i = 0; i < 3; ++i)
+        for (int j = 0; j < 8; ++j) s[j] += buf[i][j * 64 + lane];
+    float* const p = a.bsum + a.out * (1 + (int64_t)blockIdx.y) + c;  // behind the whole sums
+#pragma unroll
+    for (int j = 0; j < 8; ++j)
+        if (c + j < a.out) p[j] = s[j];
+}
+
+template <typename T, typename O>
+hipError_t run(const Wgrad& a, hipStream_t st) {
+    if (a.bsum) {
+        dy_sum_kernel<T><<<dim3((uint32_t)((a.out + 511) / 512), (uint32_t)a.bparts), 256, 0, st>>>(a);
+        hipError_t e = launch_fold(AL_DTYPE_F32, a.bsum + a.out, a.bparts, a.out, a.bsum, st);
+        if (e == hipSuccess && a.dbias)
+            e = launch_fold(sizeof(O) == 2 ? AL_DTYPE_BF16 : AL_DTYPE_F32, a.bsum, 1, a.out, a.dbias, st);
+        if (e != hipSuccess) return e;
+    }
+    if (a.s.cols == 0) return hipSuccess;
+    const dim3 n((uint32_t)((a.s.cols + kSmallTile - 1) / kSmallTile), (uint32_t)((a.out + kSmallTile - 1) / kSmallTile),
+                 (uint32_t)a.splits);
+    wgrad_small_kernel<T, O><<<n, 256, 0, st>>>(a);
+    if (a.splits > 1) {
+        const int64_t total = a.out * a.s.cols;
+        wgrad_join_kernel<O><<<dim3((uint32_t)std::min<int64_t>((total + 255) / 256, 4096)), 256, 0, st>>>(a);
+    }
+    return hipGetLastError();
+}
+
+}  // namespace
+
+WgradPlan wgrad_plan(int dtype, int64_t tokens, int64_t out, int64_t in) {
+    WgradPlan p;
+    const int64_t tiles = ((out + kSmallTile - 1) / kSmallTile) * ((in + kSmallTile - 1) / kSmallTile);
+    const int64_t steps = (tokens + kSmallTokens - 1) / kSmallTokens;
+    // two workgroups for each of the 256 compute units, and at least 8 steps each
+    p.splits = (int32_t)std::max<int64_t>(1, std::min((512 + tiles - 1) / tiles, steps / 8));
+    p.part_bytes = p.splits > 1 ? (size_t)p.splits * out * in * 4 : 0;
+    p.bparts = (int32_t)std::max<int64_t>(1, std::min<int64_t>(64, tokens / 64));
+    p.bsum_bytes = (size_t)out * (p.bparts + 1) * 4;
+    return p;
+}
+
+hipError_t launch_wgrad(int dtype, int grad_dtype, const Wgrad& a, hipStream_t st) {
+    if (dtype == AL_DTYPE_BF16) return grad_dtype == AL_DTYPE_BF16 ? run<bf16, bf16>(a, st) : run<bf16, float>(a, st);
+    return grad_dtype == AL_DTYPE_BF16 ? run<float, bf16>(a, st) : run<float, float>(a, st);
+}
+
+}  // namespace al
