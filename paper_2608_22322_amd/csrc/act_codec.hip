@@ -69,7 +69,7 @@ __global__ __launch_bounds__(kThreads) void act_dequantize_kernel(Code k, CodeSh
 }
 
 // 1 / (1 + e^-x); 0 where e^-x overflows. The hardware's exponential and reciprocal: within |x| 2^-24 + 2^-22 of
-// the value, relative, far inside a bf16 output's 2^-9 and an fp32 one's use.
+// the value, relative, far inside a bf16 output's 2^-8.
 __device__ __forceinline__ float sigmoid(float x) { return __builtin_amdgcn_rcpf(1.0f + __expf(-x)); }
 
 template <typename T>

@@ -234,7 +234,7 @@ hipError_t run(const Wgrad& a, hipStream_t st) {
 
 WgradPlan wgrad_plan(int dtype, int64_t tokens, int64_t out, int64_t in) {
     WgradPlan p;
-    const int64_t tiles = ((out + kSmallTile - 1) / kSmallTile) * ((in + kSmallTile - 1) / kSmallTile);
+    const int64_t tiles = std::max<int64_t>(1, ((out + kSmallTile - 1) / kSmallTile) * ((in + kSmallTile - 1) / kSmallTile));
     const int64_t steps = (tokens + kSmallTokens - 1) / kSmallTokens;
     // two workgroups for each of the 256 compute units, and at least 8 steps each
     p.splits = (int32_t)std::max<int64_t>(1, std::min((512 + tiles - 1) / tiles, steps / 8));
