@@ -20,7 +20,7 @@ from dataclasses import dataclass
 
 import torch
 
-from . import DTYPE_BF16, DTYPE_F32, _stream, _ws_args, check, lib
+from . import DTYPE_BF16, DTYPE_F32, _ws_args, check, lib
 
 LAYER, RMS = 0, 1
 BLOCKS = (32, 64, 128)
@@ -71,7 +71,7 @@ def _mat(t, name: str, rows: int, cols: int, dtype):
     """(pointer, row pitch) of a rows x cols matrix of dtype; (None, 0) for None."""
     if t is None:
         return None, 0
-    if t.dtype != dtype or t.shape != (rows, cols) or not t.is_cuda:
+    if t.dtype is not dtype or t.shape != (rows, cols) or not t.is_cuda:
         raise ValueError(f"{name}: a {rows} x {cols} {dtype} GPU tensor is needed, got {tuple(t.shape)} {t.dtype} on {t.device}")
     ld, inner = t.stride()
     if inner != 1 and cols > 1:
@@ -96,6 +96,12 @@ def _code(c, name: str, rows: int, cols: int):
     return c.codes.data_ptr(), c.exps.data_ptr(), c.block
 
 
+def _queue(stream, t):
+    """The stream's handle; None: the current stream of t's device (read directly: torch's Stream object takes 2.6 us of
+    a 6 us call to build)."""
+    return stream.cuda_stream if stream is not None else torch._C._cuda_getCurrentRawStream(t.device.index)
+
+
 def _shape(t, name: str):
     if t.dim() != 2:
         raise ValueError(f"{name}: a matrix is needed, got {tuple(t.shape)}")
@@ -108,14 +114,14 @@ def quantize(x, code: ActCode, stream=None) -> None:
     rows, cols = _shape(x, "x")
     p, ld = _mat(x, "x", rows, cols, x.dtype)
     c, e, block = _code(code, "code", rows, cols)
-    check(lib().al_act_quantize(_dtype(x), p, ld, rows, cols, block, c, e, _stream(stream)))
+    check(lib().al_act_quantize(_dtype(x), p, ld, rows, cols, block, c, e, _queue(stream, x)))
 
 
 def dequantize(code: ActCode, out, stream=None) -> None:
     """out <- the values of the code (exact in bfloat16)."""
     p, ld = _mat(out, "out", code.rows, code.cols, out.dtype)
     check(lib().al_act_dequantize(code.codes.data_ptr(), code.exps.data_ptr(), code.rows, code.cols, code.block,
-                                  _dtype(out), p, ld, _stream(stream)))
+                                  _dtype(out), p, ld, _queue(stream, out)))
 
 
 # ---------------------------------------------------------------------------------------- norms
@@ -131,7 +137,7 @@ def norm_forward(kind: int, x, y, mean=None, rstd=None, gamma=None, beta=None, e
     c, e, block = _code(code, "code", rows, cols)
     check(lib().al_norm_forward(kind, _dtype(x), px, ldx, rows, cols, eps, _vec(gamma, "gamma", cols, f),
                                 _vec(beta, "beta", cols, f), py, ldy, _vec(mean, "mean", rows, f),
-                                _vec(rstd, "rstd", rows, f), block, c, e, _stream(stream)))
+                                _vec(rstd, "rstd", rows, f), block, c, e, _queue(stream, x)))
 
 
 def norm_backward_workspace_bytes(kind: int, rows: int, cols: int, dtype=torch.bfloat16) -> int:
@@ -162,7 +168,7 @@ def norm_backward(kind: int, dy, x, mean, rstd, dx, gamma=None, dgamma=None, dbe
                                  _vec(rstd, "rstd", rows, f), block, c, e, rows, cols, _vec(gamma, "gamma", cols, f),
                                  pa, lda, pdx, lddx, DTYPE_F32 if g is None else _dtype(g),
                                  _vec(dgamma, "dgamma", cols, gt), _vec(dbeta, "dbeta", cols, gt), *_ws_args(ws),
-                                 _stream(stream)))
+                                 _queue(stream, dy)))
 
 
 # ---------------------------------------------------------------------------- gated activation
@@ -180,7 +186,7 @@ def swiglu_forward(gate, up, h, gate_code: ActCode | None = None, up_code: ActCo
     if ub != block:
         raise ValueError("the codes of gate and up need one block")
     check(lib().al_swiglu_forward(_dtype(gate), pg, ldg, pu, ldu, rows, cols, ph, ldh, block, gc, ge, uc, ue,
-                                  _stream(stream)))
+                                  _queue(stream, gate)))
 
 
 def swiglu_backward(dh, gate_code: ActCode, up_code: ActCode, dgate, dup, h_code: ActCode | None = None,
@@ -197,7 +203,7 @@ def swiglu_backward(dh, gate_code: ActCode, up_code: ActCode, dgate, dup, h_code
     pg, ldg = _mat(dgate, "dgate", rows, cols, dt)
     pu, ldu = _mat(dup, "dup", rows, cols, dt)
     check(lib().al_swiglu_backward(_dtype(dh), pd, ldd, rows, cols, block, gc, ge, uc, ue, pg, ldg, pu, ldu, hc, he,
-                                   _stream(stream)))
+                                   _queue(stream, dh)))
 
 
 # ------------------------------------------------------------------------------ weight gradient
@@ -221,4 +227,4 @@ def linear_wgrad(dy, code: ActCode, dw, ws, gamma=None, beta=None, base=None, db
     check(lib().al_linear_wgrad(_dtype(dy), pdy, lddy, c, e, block, tokens, out, cols, _vec(gamma, "gamma", cols, f),
                                 _vec(beta, "beta", cols, f), _dtype(dw), _vec(base, "base", out * cols, gt),
                                 _vec(dw, "dw", out * cols, gt), _vec(dbias, "dbias", out, gt), *_ws_args(ws),
-                                _stream(stream)))
+                                _queue(stream, dy)))

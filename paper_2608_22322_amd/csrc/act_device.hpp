@@ -47,6 +47,7 @@ template <>
 struct Chunk<bf16> {
     u32x4 q;
     __device__ __forceinline__ void load(const bf16* p) { q = *reinterpret_cast<const u32x4_a2*>(p); }
+    __device__ __forceinline__ void load_nt(const bf16* p) { q = __builtin_nontemporal_load(reinterpret_cast<const u32x4_a2*>(p)); }
     // the first n of 8 elements, the others 0
     __device__ __forceinline__ void load(const bf16* p, int n) {
         uint32_t h[8];
@@ -70,6 +71,10 @@ struct Chunk<float> {
     __device__ __forceinline__ void load(const float* p) {
         a = *reinterpret_cast<const u32x4_a4*>(p);
         b = *reinterpret_cast<const u32x4_a4*>(p + 4);
+    }
+    __device__ __forceinline__ void load_nt(const float* p) {
+        a = __builtin_nontemporal_load(reinterpret_cast<const u32x4_a4*>(p));
+        b = __builtin_nontemporal_load(reinterpret_cast<const u32x4_a4*>(p + 4));
     }
     __device__ __forceinline__ void load(const float* p, int n) {
 #pragma unroll
@@ -112,6 +117,19 @@ __device__ __forceinline__ void store8(float* p, const float (&v)[8]) {
     *reinterpret_cast<u32x4_a4*>(p) = a;
     *reinterpret_cast<u32x4_a4*>(p + 4) = b;
 }
+__device__ __forceinline__ void store8_nt(bf16* p, const float (&v)[8]) {
+    u32x4 q;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) q[j] = pack_bf16(v[2 * j], v[2 * j + 1]);
+    __builtin_nontemporal_store(q, reinterpret_cast<u32x4_a2*>(p));
+}
+__device__ __forceinline__ void store8_nt(float* p, const float (&v)[8]) {
+    u32x4 a, b;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) a[j] = f_bits(v[j]), b[j] = f_bits(v[j + 4]);
+    __builtin_nontemporal_store(a, reinterpret_cast<u32x4_a4*>(p));
+    __builtin_nontemporal_store(b, reinterpret_cast<u32x4_a4*>(p + 4));
+}
 template <typename T>
 __device__ __forceinline__ void store_chunk(T* row, int c, int cols, const float (&v)[8]) {
     if (c + 8 <= cols) {
@@ -134,10 +152,10 @@ constexpr int kDppXor1 = 0xB1, kDppXor2 = 0x4E, kDppHalfMirror = 0x141, kDppMirr
 
 __device__ __forceinline__ uint32_t umax(uint32_t a, uint32_t b) { return a > b ? a : b; }
 
-// Largest value over aligned groups of 4, 8 or 16 lanes (lb: 2, 3 or 4; uniform).
+// Largest value over aligned groups of 2^lb lanes (1 to 4; uniform).
 __device__ __forceinline__ uint32_t group_max(uint32_t v, int lb) {
     v = umax(v, dpp<kDppXor1>(v));
-    v = umax(v, dpp<kDppXor2>(v));
+    if (lb >= 2) v = umax(v, dpp<kDppXor2>(v));
     if (lb >= 3) v = umax(v, dpp<kDppHalfMirror>(v));
     if (lb >= 4) v = umax(v, dpp<kDppMirror>(v));
     return v;
@@ -167,20 +185,23 @@ __device__ __forceinline__ uint32_t e8_exp(uint32_t bits) {
     const uint32_t f = bits >> 23;
     return f == 255u ? 255u : f > 7u ? f - 6u : 1u;
 }
-// 8 codes. x 2^(127 - E) is exact (or far below a half), at most 128 in magnitude; adding
-// 1.5 * 2^23 rounds it to an integer, ties to even, in the low byte's two's complement.
+// 8 codes. The product x 2^(127 - E) is exact (or far below a half) and at most 128 in magnitude; adding 1.5 * 2^23 in
+// the same instruction rounds it to an integer, ties to even, whose two's complement is the low byte. E = 255
+// (where the products mean nothing) gives codes 0.
 __device__ __forceinline__ u32x2 e8_encode(const float (&v)[8], uint32_t e) {
-    const float inv = bits_f((254u - e) << 23);  // E = 255 is caught below
+    constexpr float kMagic = 12582912.0f;
+    const float inv = bits_f((254u - e) << 23);
     uint32_t t[8];
 #pragma unroll
     for (int j = 0; j < 8; ++j)
-        t[j] = f_bits(__builtin_amdgcn_fmed3f(v[j] * inv, -127.0f, 127.0f) + 12582912.0f);
+        t[j] = f_bits(__builtin_amdgcn_fmed3f(__builtin_fmaf(v[j], inv, kMagic), kMagic - 127.0f, kMagic + 127.0f));
+    const uint32_t keep = e == 255u ? 0u : ~0u;
     u32x2 q;
 #pragma unroll
     for (int j = 0; j < 2; ++j) {
         const uint32_t lo = __builtin_amdgcn_perm(t[4 * j + 1], t[4 * j], 0x0c0c0400u);
         const uint32_t hi = __builtin_amdgcn_perm(t[4 * j + 3], t[4 * j + 2], 0x04000c0cu);
-        q[j] = e == 255u ? 0u : lo | hi;
+        q[j] = (lo | hi) & keep;
     }
     return q;
 }
@@ -193,6 +214,13 @@ __device__ __forceinline__ void e8_decode(u32x2 q, uint32_t e, float (&v)[8]) {
 #pragma unroll
         for (int i = 0; i < 4; ++i) v[4 * j + i] = (float)((int32_t)(q[j] << (24 - 8 * i)) >> 24) * s;
     }
+}
+
+// Workgroups go to the 8 XCDs in turn; this gives each XCD a contiguous eighth of the work, so that lines which
+// neighbouring workgroups share (exponent bytes, row ends) stay in one L2.
+__device__ __forceinline__ uint32_t xcd_block() {
+    const uint32_t n = gridDim.x, w = blockIdx.x, x = w & 7u, per = n >> 3, rest = n & 7u;
+    return x * per + (x < rest ? x : rest) + (w >> 3);
 }
 
 // Quotient by a fixed divisor d >= 1 of n < 2^31: (n + mulhi(n, m)) >> l.
