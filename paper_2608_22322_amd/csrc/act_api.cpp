@@ -344,6 +344,7 @@ al_status al_linear_wgrad(int32_t dtype, const void* dy, int64_t lddy, const voi
     a.base = base;
     a.dw = dw;
     a.dbias = dbias;
+    a.tile = p.tile;
     a.splits = p.splits;
     a.bparts = p.bparts;
     a.part = static_cast<float*>(ws);

@@ -84,11 +84,11 @@ struct Wgrad {
     void *dw, *dbias;
     float* part;   // workspace: [splits][out][cols] partial products
     float* bsum;   // workspace: out column sums of dy, then their partials
-    int32_t splits, bparts;
+    int32_t tile, splits, bparts;
 };
 // How a call is cut (tile variant, splits over the tokens), by its sizes alone.
 struct WgradPlan {
-    int32_t splits, bparts;
+    int32_t tile, splits, bparts;
     size_t part_bytes, bsum_bytes;
 };
 WgradPlan wgrad_plan(int dtype, int64_t tokens, int64_t out, int64_t in);

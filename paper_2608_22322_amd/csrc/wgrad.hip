@@ -167,6 +167,164 @@ __global__ __launch_bounds__(256) void wgrad_small_kernel(Wgrad a) {
     }
 }
 
+// Four finished sums of consecutive columns k.. of row n (in: how many of them lie inside).
+template <typename O>
+__device__ __forceinline__ void finish4(const Wgrad& a, int64_t n, int k, int in, f32x4 v) {
+    if (in < 4) {
+        for (int r = 0; r < in; ++r) finish<O>(a, n, k + r, v[r]);
+        return;
+    }
+    typedef float f32x4_a4 __attribute__((ext_vector_type(4), aligned(4)));
+    const int64_t i = n * a.s.cols + k;
+    if (a.gamma) v *= *reinterpret_cast<const f32x4_a4*>(a.gamma + k);
+    if (a.beta) {
+        const f32x4 b = *reinterpret_cast<const f32x4_a4*>(a.beta + k);
+        const float t = a.bsum[n];
+#pragma unroll
+        for (int r = 0; r < 4; ++r) v[r] += b[r] * t;
+    }
+    if constexpr (sizeof(O) == 4) {
+        if (a.base) v += *reinterpret_cast<const f32x4_a4*>(static_cast<const float*>(a.base) + i);
+        *reinterpret_cast<f32x4_a4*>(static_cast<float*>(a.dw) + i) = v;
+    } else {
+        typedef uint32_t u32x2_a2 __attribute__((ext_vector_type(2), aligned(2)));
+        if (a.base) {
+            const u32x2 b = *reinterpret_cast<const u32x2_a2*>(static_cast<const bf16*>(a.base) + i);
+#pragma unroll
+            for (int r = 0; r < 2; ++r) v[2 * r] += bits_f(b[r] << 16), v[2 * r + 1] += bits_f(b[r] & 0xffff0000u);
+        }
+        *reinterpret_cast<u32x2_a2*>(static_cast<bf16*>(a.dw) + i) = u32x2{pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3])};
+    }
+}
+
+// 256 x 256 outputs, 8 wavefronts of 128 x 64 (2 along n, 4 along k), for out_features and code pitches of at least 256: the
+// last tile of a side is moved back to end with it, so that no load needs a bounds check, and leaves what the tile
+// before it has written.
+constexpr int kBig = 256, kBigTokens = 32;
+
+__device__ __forceinline__ int big_at(int t, int c) { return t * kBig + ((((c >> 4) ^ (t & 15)) << 4) | (c & 15)); }
+
+__device__ __forceinline__ bf16x8 big_fragment(const uint16_t* tile, int at0, int at1) {
+    union {
+        s16x4 h[2];
+        bf16x8 f;
+    } u;
+    u.h[0] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4)(lds_u16)(uint16_t*)(tile + at0));
+    u.h[1] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4)(lds_u16)(uint16_t*)(tile + at1));
+    return u.f;
+}
+
+template <typename T, typename O>
+__global__ __launch_bounds__(512, 2) void wgrad_big_kernel(Wgrad a) {
+    constexpr int PARTS = sizeof(T) == 4 ? 3 : 1, BT = kBigTokens;
+    __shared__ __attribute__((aligned(16))) uint16_t dy_s[2][BT * kBig], x_s[2][BT * kBig];
+    const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
+    const int64_t n_first = (int64_t)blockIdx.y * kBig, n0 = std::min(n_first, a.out - kBig);
+    const int k_first = blockIdx.x * kBig, k0 = std::min(k_first, a.s.pitch - kBig);
+    const int64_t steps = (a.s.rows + BT - 1) / BT;
+    const int64_t s0 = steps * blockIdx.z / a.splits, s1 = steps * (blockIdx.z + 1) / a.splits;
+
+    // this thread stages columns 8 (tid % 32) .. + 7 of tokens tid / 32 and tid / 32 + 16
+    const int cc = (tid & 31) * 8, t0 = tid >> 5;
+    const T* const dyp = static_cast<const T*>(a.dy.p) + n0 + cc;
+    const int8_t* const xp = a.c.p + k0 + cc;
+    const uint8_t* const ep = a.c.e + ((k0 + cc) >> (3 + a.s.lb));
+    Chunk<T> dy[2];
+    u32x2 xq[2];
+    uint32_t xe[2];
+    const auto load = [&](int64_t step) {
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            const int64_t t = std::min<int64_t>(step * BT + t0 + 16 * i, a.s.rows - 1);
+            dy[i].load(dyp + t * a.dy.ld);
+            xq[i] = *reinterpret_cast<const u32x2*>(xp + t * a.s.pitch);
+            xe[i] = ep[t * a.s.nb];
+        }
+    };
+    // rows past the last token add nothing
+    const auto clip = [&](int64_t step) {
+        if ((step + 1) * BT <= a.s.rows) return;
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            if (step * BT + t0 + 16 * i < a.s.rows) continue;
+            dy[i].zero();
+            xq[i] = 0u;
+            xe[i] = 0u;
+        }
+    };
+    const auto stage_dy = [&](int b, int part) {
+#pragma unroll
+        for (int i = 0; i < 2; ++i) *reinterpret_cast<u32x4*>(&dy_s[b][big_at(t0 + 16 * i, cc)]) = as_bf16<T>(dy[i], part);
+    };
+    const auto stage_x = [&](int b) {
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            float v[8];
+            e8_decode(xq[i], xe[i], v);
+            u32x4 q;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) q[j] = __builtin_amdgcn_perm(f_bits(v[2 * j + 1]), f_bits(v[2 * j]), 0x07060302u);
+            *reinterpret_cast<u32x4*>(&x_s[b][big_at(t0 + 16 * i, cc)]) = q;
+        }
+    };
+
+    // fragment offsets: token 4 (l / 16) + (l / 4) % 4, columns 16 f + 4 (l % 4)
+    const int wn = (w >> 2) * 128, wk = (w & 3) * 64, ft = 4 * (lane >> 4) + ((lane >> 2) & 3), fc = 4 * (lane & 3);
+    f32x4 acc[8][4] = {};
+    if (s0 < s1) {
+        load(s0);
+        clip(s0);
+        stage_dy(0, 0);
+        stage_x(0);
+        if (PARTS == 1 && s0 + 1 < s1) load(s0 + 1);
+    }
+    __syncthreads();
+    int bd = 0, bx = 0;
+    for (int64_t s = s0; s < s1; ++s) {
+#pragma unroll
+        for (int part = 0; part < PARTS; ++part, bd ^= 1) {
+            bf16x8 fx[4];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) fx[j] = big_fragment(x_s[bx], big_at(ft, wk + 16 * j + fc), big_at(ft + 16, wk + 16 * j + fc));
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const bf16x8 fy = big_fragment(dy_s[bd], big_at(ft, wn + 16 * i + fc), big_at(ft + 16, wn + 16 * i + fc));
+#pragma unroll
+                for (int j = 0; j < 4; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fx[j], fy, acc[i][j], 0, 0, 0);
+            }
+            // meanwhile the next turn's tiles go into the other buffers, and the loads after that one are sent off
+            if (part + 1 < PARTS) {
+                stage_dy(bd ^ 1, part + 1);
+                if (part + 1 == PARTS - 1 && s + 1 < s1) load(s + 1);
+            } else if (s + 1 < s1) {
+                clip(s + 1);
+                stage_dy(bd ^ 1, 0);
+                stage_x(bx ^ 1);
+                if (PARTS == 1 && s + 2 < s1) load(s + 2);
+            }
+            __syncthreads();
+        }
+        bx ^= 1;
+    }
+    // lane: row n = l % 16, columns k = 4 (l / 16) + 0..3
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        const int64_t n = n0 + wn + 16 * i + (lane & 15);
+        if (n < n_first) continue;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const int k = k0 + wk + 16 * j + 4 * (lane >> 4), in = std::min(4, a.s.cols - k);
+            if (k < k_first || in <= 0) continue;
+            if (a.splits > 1) {
+                float* const p = a.part + ((int64_t)blockIdx.z * a.out + n) * a.s.cols + k;
+                for (int r = 0; r < in; ++r) p[r] = acc[i][j][r];
+            } else {
+                finish4<O>(a, n, k, in, acc[i][j]);
+            }
+        }
+    }
+}
+
 // The splits' partial products, added in order.
 template <typename O>
 __global__ __launch_bounds__(256) void wgrad_join_kernel(Wgrad a) {
@@ -220,9 +378,12 @@ hipError_t run(const Wgrad& a, hipStream_t st) {
         if (e != hipSuccess) return e;
     }
     if (a.s.cols == 0) return hipSuccess;
-    const dim3 n((uint32_t)((a.s.cols + kSmallTile - 1) / kSmallTile), (uint32_t)((a.out + kSmallTile - 1) / kSmallTile),
-                 (uint32_t)a.splits);
-    wgrad_small_kernel<T, O><<<n, 256, 0, st>>>(a);
+    const int tile = a.tile;
+    const dim3 n((uint32_t)((a.s.cols + tile - 1) / tile), (uint32_t)((a.out + tile - 1) / tile), (uint32_t)a.splits);
+    if (tile == kBig)
+        wgrad_big_kernel<T, O><<<n, 512, 0, st>>>(a);
+    else
+        wgrad_small_kernel<T, O><<<n, 256, 0, st>>>(a);
     if (a.splits > 1) {
         const int64_t total = a.out * a.s.cols;
         wgrad_join_kernel<O><<<dim3((uint32_t)std::min<int64_t>((total + 255) / 256, 4096)), 256, 0, st>>>(a);
@@ -234,10 +395,15 @@ hipError_t run(const Wgrad& a, hipStream_t st) {
 
 WgradPlan wgrad_plan(int dtype, int64_t tokens, int64_t out, int64_t in) {
     WgradPlan p;
-    const int64_t tiles = std::max<int64_t>(1, ((out + kSmallTile - 1) / kSmallTile) * ((in + kSmallTile - 1) / kSmallTile));
     const int64_t steps = (tokens + kSmallTokens - 1) / kSmallTokens;
+    const auto tiles = [&](int64_t t) { return std::max<int64_t>(1, ((out + t - 1) / t) * ((in + t - 1) / t)); };
+#ifndef BIGMIN
+#define BIGMIN 100
+#endif
+    p.tile = out >= kBig && in >= kBig && tiles(kBig) >= BIGMIN ? kBig : kSmallTile;
+    const int64_t n = tiles(p.tile), fill = p.tile == kBig ? 256 : 512;
     // two workgroups for each of the 256 compute units, and at least 8 steps each
-    p.splits = (int32_t)std::max<int64_t>(1, std::min((512 + tiles - 1) / tiles, steps / 8));
+    p.splits = (int32_t)std::max<int64_t>(1, std::min(fill / n, steps / 8));
     p.part_bytes = p.splits > 1 ? (size_t)p.splits * out * in * 4 : 0;
     p.bparts = (int32_t)std::max<int64_t>(1, std::min<int64_t>(64, tokens / 64));
     p.bsum_bytes = (size_t)out * (p.bparts + 1) * 4;
