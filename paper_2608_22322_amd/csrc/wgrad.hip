@@ -5,6 +5,7 @@
 // fp32 dy is the sum of three bf16 numbers, taken in three turns), so every
 // product is exact and the sums are the matrix cores' fp32 ones.
 #include <algorithm>
+#include <type_traits>
 
 #include "act_device.hpp"
 
@@ -171,7 +172,9 @@ __global__ __launch_bounds__(256) void wgrad_small_kernel(Wgrad a) {
 template <typename O>
 __device__ __forceinline__ void finish4(const Wgrad& a, int64_t n, int k, int in, f32x4 v) {
     if (in < 4) {
-        for (int r = 0; r < in; ++r) finish<O>(a, n, k + r, v[r]);
+#pragma unroll
+        for (int r = 0; r < 3; ++r)
+            if (r < in) finish<O>(a, n, k + r, v[r]);
         return;
     }
     typedef float f32x4_a4 __attribute__((ext_vector_type(4), aligned(4)));
@@ -200,7 +203,7 @@ __device__ __forceinline__ void finish4(const Wgrad& a, int64_t n, int k, int in
 // 256 x 256 outputs, 8 wavefronts of 128 x 64 (2 along n, 4 along k), for out_features and code pitches of at least 256: the
 // last tile of a side is moved back to end with it, so that no load needs a bounds check, and leaves what the tile
 // before it has written.
-constexpr int kBig = 256, kBigTokens = 32;
+constexpr int kBig = 256;
 
 __device__ __forceinline__ int big_at(int t, int c) { return t * kBig + ((((c >> 4) ^ (t & 15)) << 4) | (c & 15)); }
 
@@ -214,101 +217,174 @@ __device__ __forceinline__ bf16x8 big_fragment(const uint16_t* tile, int at0, in
     return u.f;
 }
 
+// Workgroup -> tile. An XCD takes a contiguous share of the tiles, in bands of 8 along n: the 32 that it works on at a time
+// are 8 x 4, so each of their rows and columns of tiles is read from memory once and by the others from the XCD's L2.
+struct BigTile {
+    int n, k, split;
+};
+#ifndef BAND
+#define BAND 8
+#endif
+__device__ __forceinline__ BigTile big_tile(const Wgrad& a) {
+    const uint32_t nt = (uint32_t)((a.out + kBig - 1) / kBig), kt = (uint32_t)((a.s.cols + kBig - 1) / kBig);
+    const uint32_t id = xcd_block(), split = id / (nt * kt), r = id - split * (nt * kt), band = r / (BAND * kt),
+                   rows = min((uint32_t)BAND, nt - band * BAND), q = r - band * BAND * kt, k = q / rows;
+    return {(int)(band * BAND + q - k * rows), (int)k, (int)split};
+}
+
+#ifndef SGV
+#define SGV 2
+#define SGN 3
+#endif
+#ifndef BTOK
+#define BTOK 32
+#endif
 template <typename T, typename O>
 __global__ __launch_bounds__(512, 2) void wgrad_big_kernel(Wgrad a) {
-    constexpr int PARTS = sizeof(T) == 4 ? 3 : 1, BT = kBigTokens;
+    constexpr int PARTS = sizeof(T) == 4 ? 3 : 1, BT = sizeof(T) == 4 ? 32 : BTOK, C = BT / 16;
     __shared__ __attribute__((aligned(16))) uint16_t dy_s[2][BT * kBig], x_s[2][BT * kBig];
     const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
-    const int64_t n_first = (int64_t)blockIdx.y * kBig, n0 = std::min(n_first, a.out - kBig);
-    const int k_first = blockIdx.x * kBig, k0 = std::min(k_first, a.s.pitch - kBig);
+    const BigTile tile = big_tile(a);
+    const int64_t n_first = (int64_t)tile.n * kBig, n0 = std::min(n_first, a.out - kBig);
+    const int k_first = tile.k * kBig, k0 = std::min(k_first, a.s.pitch - kBig);
     const int64_t steps = (a.s.rows + BT - 1) / BT;
-    const int64_t s0 = steps * blockIdx.z / a.splits, s1 = steps * (blockIdx.z + 1) / a.splits;
+    const int64_t s0 = steps * tile.split / a.splits, s1 = steps * (tile.split + 1) / a.splits;
 
-    // this thread stages columns 8 (tid % 32) .. + 7 of tokens tid / 32 and tid / 32 + 16
+    // this thread stages columns 8 (tid % 32) .. + 7 of tokens tid / 32 + 16 i: 32-bit offsets from a step's first token
     const int cc = (tid & 31) * 8, t0 = tid >> 5;
-    const T* const dyp = static_cast<const T*>(a.dy.p) + n0 + cc;
-    const int8_t* const xp = a.c.p + k0 + cc;
-    const uint8_t* const ep = a.c.e + ((k0 + cc) >> (3 + a.s.lb));
-    Chunk<T> dy[2];
-    u32x2 xq[2];
-    uint32_t xe[2];
-    const auto load = [&](int64_t step) {
+    uint32_t od[C], ox[C], oe[C];
+    const auto offsets = [&](int64_t step) __attribute__((always_inline)) {
+        const int last = (int)std::min<int64_t>(a.s.rows - 1 - step * BT, BT - 1);
 #pragma unroll
-        for (int i = 0; i < 2; ++i) {
-            const int64_t t = std::min<int64_t>(step * BT + t0 + 16 * i, a.s.rows - 1);
-            dy[i].load(dyp + t * a.dy.ld);
-            xq[i] = *reinterpret_cast<const u32x2*>(xp + t * a.s.pitch);
-            xe[i] = ep[t * a.s.nb];
+        for (int i = 0; i < C; ++i) {
+            const uint32_t t = (uint32_t)std::min(t0 + 16 * i, last);
+            od[i] = (t * (uint32_t)a.dy.ld + (uint32_t)cc) * (uint32_t)sizeof(T);
+            ox[i] = t * (uint32_t)a.s.pitch + (uint32_t)cc;
+            oe[i] = t * (uint32_t)a.s.nb + ((uint32_t)(k0 + cc) >> (3 + a.s.lb));
         }
     };
-    // rows past the last token add nothing
-    const auto clip = [&](int64_t step) {
-        if ((step + 1) * BT <= a.s.rows) return;
+    Chunk<T> dy[C];
+    u32x2 xq[C];
+    uint32_t xe[C];
+    const auto load = [&](int64_t step, bool whole) __attribute__((always_inline)) {
+        const char* const dyp = reinterpret_cast<const char*>(static_cast<const T*>(a.dy.p) + step * BT * a.dy.ld + n0);
+        const char* const xp = reinterpret_cast<const char*>(a.c.p) + step * BT * a.s.pitch + k0;
+        const uint8_t* const ep = a.c.e + step * BT * a.s.nb;
+        if (!whole && (step + 1) * BT > a.s.rows) offsets(step);  // the last step may be short
 #pragma unroll
-        for (int i = 0; i < 2; ++i) {
-            if (step * BT + t0 + 16 * i < a.s.rows) continue;
+        for (int i = 0; i < C; ++i) {
+            dy[i].load(reinterpret_cast<const T*>(dyp + od[i]));
+            xq[i] = *reinterpret_cast<const u32x2*>(xp + ox[i]);
+            xe[i] = ep[oe[i]];
+        }
+    };
+    // rows past the split's last token add nothing
+    const int64_t rows_end = std::min<int64_t>(a.s.rows, s1 * BT);
+    const auto clip = [&](int64_t step) __attribute__((always_inline)) {
+        if ((step + 1) * BT <= rows_end) return;
+#pragma unroll
+        for (int i = 0; i < C; ++i) {
+            if (step * BT + t0 + 16 * i < rows_end) continue;
             dy[i].zero();
             xq[i] = 0u;
             xe[i] = 0u;
         }
     };
-    const auto stage_dy = [&](int b, int part) {
+    const auto stage_dy = [&](uint16_t* tile, int part) __attribute__((always_inline)) {
 #pragma unroll
-        for (int i = 0; i < 2; ++i) *reinterpret_cast<u32x4*>(&dy_s[b][big_at(t0 + 16 * i, cc)]) = as_bf16<T>(dy[i], part);
+        for (int i = 0; i < C; ++i) *reinterpret_cast<u32x4*>(&tile[big_at(t0 + 16 * i, cc)]) = as_bf16<T>(dy[i], part);
     };
-    const auto stage_x = [&](int b) {
+    const auto stage_x = [&](uint16_t* tile) __attribute__((always_inline)) {
 #pragma unroll
-        for (int i = 0; i < 2; ++i) {
+        for (int i = 0; i < C; ++i) {
             float v[8];
             e8_decode(xq[i], xe[i], v);
             u32x4 q;
 #pragma unroll
             for (int j = 0; j < 4; ++j) q[j] = __builtin_amdgcn_perm(f_bits(v[2 * j + 1]), f_bits(v[2 * j]), 0x07060302u);
-            *reinterpret_cast<u32x4*>(&x_s[b][big_at(t0 + 16 * i, cc)]) = q;
+            *reinterpret_cast<u32x4*>(&tile[big_at(t0 + 16 * i, cc)]) = q;
         }
     };
 
     // fragment offsets: token 4 (l / 16) + (l / 4) % 4, columns 16 f + 4 (l % 4)
     const int wn = (w >> 2) * 128, wk = (w & 3) * 64, ft = 4 * (lane >> 4) + ((lane >> 2) & 3), fc = 4 * (lane & 3);
-    f32x4 acc[8][4] = {};
-    if (s0 < s1) {
-        load(s0);
-        clip(s0);
-        stage_dy(0, 0);
-        stage_x(0);
-        if (PARTS == 1 && s0 + 1 < s1) load(s0 + 1);
-    }
-    __syncthreads();
-    int bd = 0, bx = 0;
-    for (int64_t s = s0; s < s1; ++s) {
+    int ay[8], ax[4];
 #pragma unroll
-        for (int part = 0; part < PARTS; ++part, bd ^= 1) {
+    for (int i = 0; i < 8; ++i) ay[i] = big_at(ft, wn + 16 * i + fc);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) ax[j] = big_at(ft, wk + 16 * j + fc);
+    f32x4 acc[8][4] = {};
+    const auto multiply = [&](const uint16_t* ty, const uint16_t* tx) __attribute__((always_inline)) {
+#pragma unroll
+        for (int h = 0; h < BT / 32; ++h) {
             bf16x8 fx[4];
 #pragma unroll
-            for (int j = 0; j < 4; ++j) fx[j] = big_fragment(x_s[bx], big_at(ft, wk + 16 * j + fc), big_at(ft + 16, wk + 16 * j + fc));
+            for (int j = 0; j < 4; ++j) fx[j] = big_fragment(tx + h * 32 * kBig, ax[j], ax[j] + 16 * kBig);
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
-                const bf16x8 fy = big_fragment(dy_s[bd], big_at(ft, wn + 16 * i + fc), big_at(ft + 16, wn + 16 * i + fc));
+                const bf16x8 fy = big_fragment(ty + h * 32 * kBig, ay[i], ay[i] + 16 * kBig);
 #pragma unroll
                 for (int j = 0; j < 4; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fx[j], fy, acc[i][j], 0, 0, 0);
             }
-            // meanwhile the next turn's tiles go into the other buffers, and the loads after that one are sent off
-            if (part + 1 < PARTS) {
-                stage_dy(bd ^ 1, part + 1);
-                if (part + 1 == PARTS - 1 && s + 1 < s1) load(s + 1);
-            } else if (s + 1 < s1) {
-                clip(s + 1);
-                stage_dy(bd ^ 1, 0);
-                stage_x(bx ^ 1);
-                if (PARTS == 1 && s + 2 < s1) load(s + 2);
-            }
-            __syncthreads();
         }
-        bx ^= 1;
+    };
+    if (s0 < s1) {
+        offsets(s0);
+        load(s0, false);
+        clip(s0);
+        stage_dy(dy_s[0], 0);
+        stage_x(x_s[0]);
+        if (PARTS == 1 && s0 + 1 < s1) load(s0 + 1, false);
     }
-    // lane: row n = l % 16, columns k = 4 (l / 16) + 0..3
+    __syncthreads();
+    // One turn: this turn's products, and beside them the next turn's tiles into the other buffers and the loads after
+    // those. WHOLE: every step that the turn looks at is 32 tokens of this split.
+    const auto turn = [&](int64_t s, int part, int bd, int bx, auto whole) __attribute__((always_inline)) {
+        constexpr bool WHOLE = decltype(whole)::value;
+        multiply(dy_s[bd], x_s[bx]);
+        if (part + 1 < PARTS) {
+            stage_dy(dy_s[bd ^ 1], part + 1);
+            if (part + 1 == PARTS - 1 && (WHOLE || s + 1 < s1)) load(s + 1, WHOLE);
+        } else {
+            if (!WHOLE) clip(s + 1);
+            stage_dy(dy_s[bd ^ 1], 0);
+            stage_x(x_s[bx ^ 1]);
+            if (PARTS == 1 && (WHOLE || s + 2 < s1)) load(s + 2, WHOLE);
+        }
+        if constexpr (WHOLE) {
+            // matrix instructions with the fragments two ahead, the decoding and the LDS writes between them
+            __builtin_amdgcn_sched_group_barrier(0x100, 12, 0);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+                    if (j < 2 && i < 6) __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+                    if (i >= SGV) __builtin_amdgcn_sched_group_barrier(0x002, SGN, 0);
+                }
+                if (i >= 4) __builtin_amdgcn_sched_group_barrier(0x200, 1, 0);
+            }
+            __builtin_amdgcn_sched_group_barrier(0x020, 6, 0);
+        }
+        __syncthreads();
+    };
+    const auto trip = [&](int64_t s, auto whole) __attribute__((always_inline)) {
+#pragma unroll
+        for (int part = 0; part < PARTS; ++part) turn(s, part, part & 1, 0, whole);
+#pragma unroll
+        for (int part = 0; part < PARTS; ++part) turn(s + 1, part, (PARTS + part) & 1, 1, whole);
+    };
+    // two turns a trip, so that the buffers' addresses are constants; the second of a last odd one multiplies zeros
+    const int64_t whole_end = std::min<int64_t>(s1, a.s.rows / BT);
+    int64_t s = s0;
+    if constexpr (PARTS == 1)
+        for (; s + 3 < whole_end; s += 2) trip(s, std::true_type{});
+    for (; s < s1; s += 2) trip(s, std::false_type{});
+    // lane: row n = l % 16, columns k = 4 (l / 16) + 0..3. (One row of blocks at a time: with all their loads in flight at
+    // once the sums would not stay in registers.)
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
+        __builtin_amdgcn_sched_barrier(0);
         const int64_t n = n0 + wn + 16 * i + (lane & 15);
         if (n < n_first) continue;
 #pragma unroll
@@ -316,8 +392,10 @@ __global__ __launch_bounds__(512, 2) void wgrad_big_kernel(Wgrad a) {
             const int k = k0 + wk + 16 * j + 4 * (lane >> 4), in = std::min(4, a.s.cols - k);
             if (k < k_first || in <= 0) continue;
             if (a.splits > 1) {
-                float* const p = a.part + ((int64_t)blockIdx.z * a.out + n) * a.s.cols + k;
-                for (int r = 0; r < in; ++r) p[r] = acc[i][j][r];
+                float* const p = a.part + ((int64_t)tile.split * a.out + n) * a.s.cols + k;
+#pragma unroll
+                for (int r = 0; r < 4; ++r)
+                    if (r < in) p[r] = acc[i][j][r];
             } else {
                 finish4<O>(a, n, k, in, acc[i][j]);
             }
@@ -381,7 +459,7 @@ hipError_t run(const Wgrad& a, hipStream_t st) {
     const int tile = a.tile;
     const dim3 n((uint32_t)((a.s.cols + tile - 1) / tile), (uint32_t)((a.out + tile - 1) / tile), (uint32_t)a.splits);
     if (tile == kBig)
-        wgrad_big_kernel<T, O><<<n, 512, 0, st>>>(a);
+        wgrad_big_kernel<T, O><<<n.x * n.y * n.z, 512, 0, st>>>(a);
     else
         wgrad_small_kernel<T, O><<<n, 256, 0, st>>>(a);
     if (a.splits > 1) {
