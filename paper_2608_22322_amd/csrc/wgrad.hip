@@ -16,6 +16,7 @@ namespace {
 typedef short s16x4 __attribute__((ext_vector_type(4)));
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef float f32x16 __attribute__((ext_vector_type(16)));
 typedef __attribute__((address_space(3))) s16x4* lds_s16x4;
 typedef __attribute__((address_space(3))) uint16_t* lds_u16;
 
@@ -203,9 +204,47 @@ __device__ __forceinline__ void finish4(const Wgrad& a, int64_t n, int k, int in
 // 256 x 256 outputs, 8 wavefronts of 128 x 64 (2 along n, 4 along k), for out_features and code pitches of at least 256: the
 // last tile of a side is moved back to end with it, so that no load needs a bounds check, and leaves what the tile
 // before it has written.
-constexpr int kBig = 256;
+constexpr int kBig = 256, kBigTokens = 32;
 
-__device__ __forceinline__ int big_at(int t, int c) { return t * kBig + ((((c >> 4) ^ (t & 15)) << 4) | (c & 15)); }
+// The shape of the products, M x M. 16 x 16 x 32 takes more cycles than 32 x 32 x 16 and keeps a higher clock (8192 tokens and
+// features: 1.85M cycles at 2.13 GHz against 1.74M at 1.92 GHz), so bf16 dy takes it; fp32 dy, whose staging needs the
+// registers that fewer fragments in flight leave, takes 32 x 32 x 16 (4096^3: 842 and 400 us).
+template <int M>
+struct Product;
+template <>
+struct Product<16> {
+    typedef f32x4 acc_t;
+    static constexpr int kTokens = 32, kQuads = 1;
+    // unit u (32 bytes) of row t lies at u ^ t % 16: half a wavefront reads one unit of 8 rows, all 64 banks
+    static __device__ __forceinline__ int swizzle(int t) { return t & 15; }
+    // a transposing read gives lanes 16 g .. 16 g + 15 columns 0..15 of tokens 4 g .. 4 g + 3, a second one 16 tokens on
+    static __device__ __forceinline__ int token(int lane) { return 4 * (lane >> 4) + ((lane >> 2) & 3); }
+    static __device__ __forceinline__ int column(int lane) { return 4 * (lane & 3); }
+    // columns (k) of a lane's sums: 4 (l / 16) + 0..3
+    static __device__ __forceinline__ int quad(int lane, int) { return 4 * (lane >> 4); }
+    static __device__ __forceinline__ acc_t mul(bf16x8 x, bf16x8 y, acc_t c) {
+        return __builtin_amdgcn_mfma_f32_16x16x32_bf16(x, y, c, 0, 0, 0);
+    }
+};
+template <>
+struct Product<32> {
+    typedef f32x16 acc_t;
+    static constexpr int kTokens = 16, kQuads = 4;
+    // u ^ 2 (t % 8): half a wavefront reads two units of 4 rows
+    static __device__ __forceinline__ int swizzle(int t) { return (t & 7) << 1; }
+    // lanes 16 g ..: columns 16 (g % 2) .. of tokens 4 (g / 2) ..; a second one 8 tokens on
+    static __device__ __forceinline__ int token(int lane) { return 4 * (lane >> 5) + ((lane >> 2) & 3); }
+    static __device__ __forceinline__ int column(int lane) { return (lane & 16) + 4 * (lane & 3); }
+    static __device__ __forceinline__ int quad(int lane, int q) { return 8 * q + 4 * (lane >> 5); }
+    static __device__ __forceinline__ acc_t mul(bf16x8 x, bf16x8 y, acc_t c) {
+        return __builtin_amdgcn_mfma_f32_32x32x16_bf16(x, y, c, 0, 0, 0);
+    }
+};
+
+template <int M>
+__device__ __forceinline__ int big_at(int t, int c) {
+    return t * kBig + ((((c >> 4) ^ Product<M>::swizzle(t)) << 4) | (c & 15));
+}
 
 __device__ __forceinline__ bf16x8 big_fragment(const uint16_t* tile, int at0, int at1) {
     union {
@@ -222,26 +261,18 @@ __device__ __forceinline__ bf16x8 big_fragment(const uint16_t* tile, int at0, in
 struct BigTile {
     int n, k, split;
 };
-#ifndef BAND
-#define BAND 8
-#endif
+constexpr uint32_t kBand = 8;
 __device__ __forceinline__ BigTile big_tile(const Wgrad& a) {
     const uint32_t nt = (uint32_t)((a.out + kBig - 1) / kBig), kt = (uint32_t)((a.s.cols + kBig - 1) / kBig);
-    const uint32_t id = xcd_block(), split = id / (nt * kt), r = id - split * (nt * kt), band = r / (BAND * kt),
-                   rows = min((uint32_t)BAND, nt - band * BAND), q = r - band * BAND * kt, k = q / rows;
-    return {(int)(band * BAND + q - k * rows), (int)k, (int)split};
+    const uint32_t id = xcd_block(), split = id / (nt * kt), r = id - split * (nt * kt), band = r / (kBand * kt),
+                   rows = min(kBand, nt - band * kBand), q = r - band * kBand * kt, k = q / rows;
+    return {(int)(band * kBand + q - k * rows), (int)k, (int)split};
 }
 
-#ifndef SGV
-#define SGV 2
-#define SGN 3
-#endif
-#ifndef BTOK
-#define BTOK 32
-#endif
 template <typename T, typename O>
 __global__ __launch_bounds__(512, 2) void wgrad_big_kernel(Wgrad a) {
-    constexpr int PARTS = sizeof(T) == 4 ? 3 : 1, BT = sizeof(T) == 4 ? 32 : BTOK, C = BT / 16;
+    constexpr int PARTS = sizeof(T) == 4 ? 3 : 1, BT = kBigTokens, C = BT / 16;
+    constexpr int M = PARTS == 1 ? 16 : 32, FN = 128 / M, FK = 64 / M, H = BT / Product<M>::kTokens;
     __shared__ __attribute__((aligned(16))) uint16_t dy_s[2][BT * kBig], x_s[2][BT * kBig];
     const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
     const BigTile tile = big_tile(a);
@@ -292,7 +323,7 @@ __global__ __launch_bounds__(512, 2) void wgrad_big_kernel(Wgrad a) {
     };
     const auto stage_dy = [&](uint16_t* tile, int part) __attribute__((always_inline)) {
 #pragma unroll
-        for (int i = 0; i < C; ++i) *reinterpret_cast<u32x4*>(&tile[big_at(t0 + 16 * i, cc)]) = as_bf16<T>(dy[i], part);
+        for (int i = 0; i < C; ++i) *reinterpret_cast<u32x4*>(&tile[big_at<M>(t0 + 16 * i, cc)]) = as_bf16<T>(dy[i], part);
     };
     const auto stage_x = [&](uint16_t* tile) __attribute__((always_inline)) {
 #pragma unroll
@@ -302,29 +333,32 @@ __global__ __launch_bounds__(512, 2) void wgrad_big_kernel(Wgrad a) {
             u32x4 q;
 #pragma unroll
             for (int j = 0; j < 4; ++j) q[j] = __builtin_amdgcn_perm(f_bits(v[2 * j + 1]), f_bits(v[2 * j]), 0x07060302u);
-            *reinterpret_cast<u32x4*>(&tile[big_at(t0 + 16 * i, cc)]) = q;
+            *reinterpret_cast<u32x4*>(&tile[big_at<M>(t0 + 16 * i, cc)]) = q;
         }
     };
 
-    // fragment offsets: token 4 (l / 16) + (l / 4) % 4, columns 16 f + 4 (l % 4)
-    const int wn = (w >> 2) * 128, wk = (w & 3) * 64, ft = 4 * (lane >> 4) + ((lane >> 2) & 3), fc = 4 * (lane & 3);
-    int ay[8], ax[4];
+    const int wn = (w >> 2) * 128, wk = (w & 3) * 64, ft = Product<M>::token(lane), fc = Product<M>::column(lane);
+    int ay[FN][2], ax[FK][2];  // a fragment's two reads
 #pragma unroll
-    for (int i = 0; i < 8; ++i) ay[i] = big_at(ft, wn + 16 * i + fc);
+    for (int r = 0; r < 2; ++r) {
 #pragma unroll
-    for (int j = 0; j < 4; ++j) ax[j] = big_at(ft, wk + 16 * j + fc);
-    f32x4 acc[8][4] = {};
+        for (int i = 0; i < FN; ++i) ay[i][r] = big_at<M>(ft + r * Product<M>::kTokens / 2, wn + M * i + fc);
+#pragma unroll
+        for (int j = 0; j < FK; ++j) ax[j][r] = big_at<M>(ft + r * Product<M>::kTokens / 2, wk + M * j + fc);
+    }
+    typename Product<M>::acc_t acc[FN][FK] = {};
     const auto multiply = [&](const uint16_t* ty, const uint16_t* tx) __attribute__((always_inline)) {
 #pragma unroll
-        for (int h = 0; h < BT / 32; ++h) {
-            bf16x8 fx[4];
+        for (int h = 0; h < H; ++h) {
+            const int at = h * Product<M>::kTokens * kBig;
+            bf16x8 fx[FK];
 #pragma unroll
-            for (int j = 0; j < 4; ++j) fx[j] = big_fragment(tx + h * 32 * kBig, ax[j], ax[j] + 16 * kBig);
+            for (int j = 0; j < FK; ++j) fx[j] = big_fragment(tx + at, ax[j][0], ax[j][1]);
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                const bf16x8 fy = big_fragment(ty + h * 32 * kBig, ay[i], ay[i] + 16 * kBig);
+            for (int i = 0; i < FN; ++i) {
+                const bf16x8 fy = big_fragment(ty + at, ay[i][0], ay[i][1]);
 #pragma unroll
-                for (int j = 0; j < 4; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fx[j], fy, acc[i][j], 0, 0, 0);
+                for (int j = 0; j < FK; ++j) acc[i][j] = Product<M>::mul(fx[j], fy, acc[i][j]);
             }
         }
     };
@@ -351,8 +385,8 @@ __global__ __launch_bounds__(512, 2) void wgrad_big_kernel(Wgrad a) {
             stage_x(x_s[bx ^ 1]);
             if (PARTS == 1 && (WHOLE || s + 2 < s1)) load(s + 2, WHOLE);
         }
-        if constexpr (WHOLE) {
-            // matrix instructions with the fragments two ahead, the decoding and the LDS writes between them
+        if constexpr (WHOLE && M == 16) {
+            // the matrix instructions with fragments two ahead, the decoding and the LDS writes between them, then the loads
             __builtin_amdgcn_sched_group_barrier(0x100, 12, 0);
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
@@ -360,7 +394,7 @@ __global__ __launch_bounds__(512, 2) void wgrad_big_kernel(Wgrad a) {
                 for (int j = 0; j < 4; ++j) {
                     __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
                     if (j < 2 && i < 6) __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
-                    if (i >= SGV) __builtin_amdgcn_sched_group_barrier(0x002, SGN, 0);
+                    if (i >= 4) __builtin_amdgcn_sched_group_barrier(0x002, 5, 0);
                 }
                 if (i >= 4) __builtin_amdgcn_sched_group_barrier(0x200, 1, 0);
             }
@@ -377,27 +411,32 @@ __global__ __launch_bounds__(512, 2) void wgrad_big_kernel(Wgrad a) {
     // two turns a trip, so that the buffers' addresses are constants; the second of a last odd one multiplies zeros
     const int64_t whole_end = std::min<int64_t>(s1, a.s.rows / BT);
     int64_t s = s0;
-    if constexpr (PARTS == 1)
-        for (; s + 3 < whole_end; s += 2) trip(s, std::true_type{});
+    for (; s + 3 < whole_end; s += 2) trip(s, std::true_type{});
     for (; s < s1; s += 2) trip(s, std::false_type{});
-    // lane: row n = l % 16, columns k = 4 (l / 16) + 0..3. (One row of blocks at a time: with all their loads in flight at
-    // once the sums would not stay in registers.)
+    // lane: row n = l % M, four columns k a quad. (One row of blocks at a time: with all their loads in flight at once the
+    // sums would not stay in registers.)
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
+    for (int i = 0; i < FN; ++i) {
         __builtin_amdgcn_sched_barrier(0);
-        const int64_t n = n0 + wn + 16 * i + (lane & 15);
+        const int64_t n = n0 + wn + M * i + (lane & (M - 1));
         if (n < n_first) continue;
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            const int k = k0 + wk + 16 * j + 4 * (lane >> 4), in = std::min(4, a.s.cols - k);
-            if (k < k_first || in <= 0) continue;
-            if (a.splits > 1) {
-                float* const p = a.part + ((int64_t)tile.split * a.out + n) * a.s.cols + k;
+        for (int j = 0; j < FK; ++j) {
 #pragma unroll
-                for (int r = 0; r < 4; ++r)
-                    if (r < in) p[r] = acc[i][j][r];
-            } else {
-                finish4<O>(a, n, k, in, acc[i][j]);
+            for (int q = 0; q < Product<M>::kQuads; ++q) {
+                const int k = k0 + wk + M * j + Product<M>::quad(lane, q), in = std::min(4, a.s.cols - k);
+                if (k < k_first || in <= 0) continue;
+                f32x4 v;
+#pragma unroll
+                for (int r = 0; r < 4; ++r) v[r] = acc[i][j][4 * q + r];
+                if (a.splits > 1) {
+                    float* const p = a.part + ((int64_t)tile.split * a.out + n) * a.s.cols + k;
+#pragma unroll
+                    for (int r = 0; r < 4; ++r)
+                        if (r < in) p[r] = v[r];
+                } else {
+                    finish4<O>(a, n, k, in, v);
+                }
             }
         }
     }
@@ -456,7 +495,8 @@ hipError_t run(const Wgrad& a, hipStream_t st) {
         if (e != hipSuccess) return e;
     }
     if (a.s.cols == 0) return hipSuccess;
-    const int tile = a.tile;
+    // the large tiles' 32-bit offsets span 32 rows
+    const int tile = a.dy.ld < (1 << 25) && a.s.pitch < (1 << 26) ? a.tile : kSmallTile;
     const dim3 n((uint32_t)((a.s.cols + tile - 1) / tile), (uint32_t)((a.out + tile - 1) / tile), (uint32_t)a.splits);
     if (tile == kBig)
         wgrad_big_kernel<T, O><<<n.x * n.y * n.z, 512, 0, st>>>(a);
