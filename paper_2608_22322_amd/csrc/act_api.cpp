@@ -318,7 +318,7 @@ al_status al_linear_wgrad(int32_t dtype, const void* dy, int64_t lddy, const voi
     AL_TRY(check_shape(tokens, in_features, who));
     AL_TRY(check_shape(tokens, out_features, who));
     AL_TRY(check_block(block, who));
-    if (out_features > (int64_t(1) << 22)) return fail(AL_EUNSUPPORTED, "%s: more than 2^22 out_features", who);
+    if (out_features >= (int64_t(1) << 22)) return fail(AL_EUNSUPPORTED, "%s: 2^22 out_features or more", who);
     if (out_features == 0) return AL_OK;
     if (in_features > 0) {
         if (!dw) return fail(AL_EINVAL, "%s: dw is NULL", who);

@@ -23,10 +23,12 @@ typedef __attribute__((address_space(3))) uint16_t* lds_u16;
 // Both tiles lie in LDS as they do in memory, a row per token. A transposing read gives lane l of
 // a wavefront the 4 tokens 4 (l / 16) + 0..3 of column l % 16: two of them make the 8-token fragment of
 // a 16 x 16 x 32 product (which token comes at which place does not matter, as both factors
-// agree). The 16 rows that one read touches lie in different 32-byte units: unit u of row t is at u ^ (t & 7).
-constexpr int kSmallTile = 128, kSmallTokens = 32;
+// agree). Half a wavefront reads one 32-byte unit of each of 8 rows at once; the units of a row are exchanged so that
+// these lie in different banks.
+constexpr int kTurn = 32;  // tokens a turn
+constexpr int kEdge = 64;
 
-__device__ __forceinline__ int small_at(int t, int c) { return t * kSmallTile + ((((c >> 4) ^ (t & 7)) << 4) | (c & 15)); }
+__device__ __forceinline__ int edge_at(int t, int c) { return t * kEdge + ((((c >> 4) ^ ((t >> 1) & 3)) << 4) | (c & 15)); }
 
 // The bf16 part `which` (0, 1, 2) of fp32 values: x = x0 + x1 + x2 exactly, by truncation; infinities and NaN
 // are in part 0 alone.
@@ -58,15 +60,24 @@ __device__ __forceinline__ u32x4 as_bf16<float>(const Chunk<float>& k, int which
     return q;
 }
 
-__device__ __forceinline__ bf16x8 fragment(const uint16_t* tile, int c0, int lane) {
-    const int t = 4 * (lane >> 4) + ((lane >> 2) & 3), c = c0 + 4 * (lane & 3);
+__device__ __forceinline__ bf16x8 tile_fragment(const uint16_t* tile, int at0, int at1) {
     union {
         s16x4 h[2];
         bf16x8 f;
     } u;
-    u.h[0] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4)(lds_u16)(uint16_t*)(tile + small_at(t, c)));
-    u.h[1] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4)(lds_u16)(uint16_t*)(tile + small_at(t + 16, c)));
+    u.h[0] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4)(lds_u16)(uint16_t*)(tile + at0));
+    u.h[1] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4)(lds_u16)(uint16_t*)(tile + at1));
     return u.f;
+}
+
+// Eight codes as bf16 numbers.
+__device__ __forceinline__ u32x4 decode_bf16(u32x2 codes, uint32_t e) {
+    float v[8];
+    e8_decode(codes, e, v);
+    u32x4 q;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) q[j] = __builtin_amdgcn_perm(f_bits(v[2 * j + 1]), f_bits(v[2 * j]), 0x07060302u);
+    return q;
 }
 
 __device__ __forceinline__ float grad_at(const bf16* p, int64_t i) { return to_f(p[i]); }
@@ -80,93 +91,6 @@ __device__ __forceinline__ void finish(const Wgrad& a, int64_t n, int k, float v
     if (a.beta) v += a.beta[k] * a.bsum[n];
     if (a.base) v += grad_at(static_cast<const O*>(a.base), i);
     put(static_cast<O*>(a.dw) + i, v);
-}
-
-// 128 x 128 outputs, 4 wavefronts of 64 x 64, 32 tokens a step, any size and alignment.
-template <typename T, typename O>
-__global__ __launch_bounds__(256) void wgrad_small_kernel(Wgrad a) {
-    __shared__ __attribute__((aligned(16))) uint16_t dy_s[2][kSmallTokens * kSmallTile], x_s[2][kSmallTokens * kSmallTile];
-    constexpr int PARTS = sizeof(T) == 4 ? 3 : 1;
-    const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
-    const int64_t n0 = (int64_t)blockIdx.y * kSmallTile;
-    const int k0 = blockIdx.x * kSmallTile;
-    // this split's tokens
-    const int64_t steps = (a.s.rows + kSmallTokens - 1) / kSmallTokens;
-    const int64_t s0 = steps * blockIdx.z / a.splits, s1 = steps * (blockIdx.z + 1) / a.splits;
-
-    Chunk<T> dy[2];
-    u32x2 xq[2];
-    uint32_t xe[2];
-    const int cc = (tid & 15) * 8;  // this thread's columns; tokens tid / 16 and tid / 16 + 16
-    const int out = (int)std::min<int64_t>(a.out - n0, kSmallTile);
-    const auto load = [&](int64_t step) {
-#pragma unroll
-        for (int i = 0; i < 2; ++i) {
-            const int64_t t = step * kSmallTokens + (tid >> 4) + 16 * i;
-            dy[i].zero();
-            xq[i] = 0u;
-            xe[i] = 0u;
-            if (t >= a.s.rows) continue;
-            load_chunk(dy[i], static_cast<const T*>(a.dy.p) + t * a.dy.ld + n0, cc, out);
-            if (k0 + cc < a.s.pitch) {
-                xq[i] = *reinterpret_cast<const u32x2*>(a.c.p + t * a.s.pitch + k0 + cc);
-                xe[i] = a.c.e[t * a.s.nb + ((k0 + cc) >> (3 + a.s.lb))];
-            }
-        }
-    };
-    const auto stage = [&](int b, int part) {
-#pragma unroll
-        for (int i = 0; i < 2; ++i) {
-            const int t = (tid >> 4) + 16 * i;
-            *reinterpret_cast<u32x4*>(&dy_s[b][small_at(t, cc)]) = as_bf16<T>(dy[i], part);
-            float v[8];
-            e8_decode(xq[i], xe[i], v);
-            u32x4 q;
-#pragma unroll
-            for (int j = 0; j < 4; ++j) q[j] = (f_bits(v[2 * j]) >> 16) | (f_bits(v[2 * j + 1]) & 0xffff0000u);
-            *reinterpret_cast<u32x4*>(&x_s[b][small_at(t, cc)]) = q;
-        }
-    };
-    const int wn = (w >> 1) * 64, wk = (w & 1) * 64;
-    f32x4 acc[4][4] = {};
-    int b = 0;
-    if (s0 < s1) load(s0);
-    for (int64_t s = s0; s < s1; ++s) {
-        for (int part = 0; part < PARTS; ++part, b ^= 1) {
-            stage(b, part);
-            __syncthreads();
-            if (part == PARTS - 1 && s + 1 < s1) load(s + 1);
-            bf16x8 fx[4], fy[4];
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                fx[i] = fragment(x_s[b], wk + 16 * i, lane);
-                fy[i] = fragment(dy_s[b], wn + 16 * i, lane);
-            }
-#pragma unroll
-            for (int i = 0; i < 4; ++i)
-#pragma unroll
-                for (int j = 0; j < 4; ++j)
-                    acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fx[j], fy[i], acc[i][j], 0, 0, 0);
-        }
-    }
-    // lane: row n = l % 16, columns k = 4 (l / 16) + 0..3
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const int64_t n = n0 + wn + 16 * i + (lane & 15);
-        if (n >= a.out) continue;
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            const int k = k0 + wk + 16 * j + 4 * (lane >> 4);
-#pragma unroll
-            for (int r = 0; r < 4; ++r) {
-                if (k + r >= a.s.cols) continue;
-                if (a.splits > 1)
-                    a.part[((int64_t)blockIdx.z * a.out + n) * a.s.cols + k + r] = acc[i][j][r];
-                else
-                    finish<O>(a, n, k + r, acc[i][j][r]);
-            }
-        }
-    }
 }
 
 // Four finished sums of consecutive columns k.. of row n (in: how many of them lie inside).
@@ -201,10 +125,93 @@ __device__ __forceinline__ void finish4(const Wgrad& a, int64_t n, int k, int in
     }
 }
 
-// 256 x 256 outputs, 8 wavefronts of 128 x 64 (2 along n, 4 along k), for out_features and code pitches of at least 256: the
-// last tile of a side is moved back to end with it, so that no load needs a bounds check, and leaves what the tile
-// before it has written.
-constexpr int kBig = 256, kBigTokens = 32;
+// A lane's four sums: into this split's partial products, or finished.
+template <typename O>
+__device__ __forceinline__ void write4(const Wgrad& a, int split, int64_t n, int k, int in, f32x4 v) {
+    if (in <= 0) return;
+    if (a.splits > 1) {
+        float* const p = a.part + ((int64_t)split * a.out + n) * a.s.cols + k;
+#pragma unroll
+        for (int r = 0; r < 4; ++r)
+            if (r < in) p[r] = v[r];
+    } else {
+        finish4<O>(a, n, k, in, v);
+    }
+}
+
+// 64 x 64 outputs, 4 wavefronts of 32 x 32, any size and alignment.
+template <typename T, typename O>
+__global__ __launch_bounds__(256) void wgrad_edge_kernel(Wgrad a) {
+    __shared__ __attribute__((aligned(16))) uint16_t dy_s[2][kTurn * kEdge], x_s[2][kTurn * kEdge];
+    constexpr int PARTS = sizeof(T) == 4 ? 3 : 1;
+    const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
+    const int64_t n0 = (int64_t)blockIdx.y * kEdge;
+    const int k0 = blockIdx.x * kEdge;
+    // this split's tokens
+    const int64_t steps = (a.s.rows + kTurn - 1) / kTurn;
+    const int64_t s0 = steps * blockIdx.z / a.splits, s1 = steps * (blockIdx.z + 1) / a.splits;
+
+    Chunk<T> dy;
+    u32x2 xq;
+    uint32_t xe;
+    const int cc = (tid & 7) * 8, t0 = tid >> 3;  // this thread's columns and token of a step
+    const int out = (int)std::min<int64_t>(a.out - n0, kEdge);
+    const auto load = [&](int64_t step) {
+        const int64_t t = step * kTurn + t0;
+        dy.zero();
+        xq = 0u;
+        xe = 0u;
+        if (t >= a.s.rows) return;
+        load_chunk(dy, static_cast<const T*>(a.dy.p) + t * a.dy.ld + n0, cc, out);
+        if (k0 + cc < a.s.pitch) {
+            xq = *reinterpret_cast<const u32x2*>(a.c.p + t * a.s.pitch + k0 + cc);
+            xe = a.c.e[t * a.s.nb + ((k0 + cc) >> (3 + a.s.lb))];
+        }
+    };
+    const auto fragment = [&](const uint16_t* tile, int c0) {
+        const int t = 4 * (lane >> 4) + ((lane >> 2) & 3), c = c0 + 4 * (lane & 3);
+        return tile_fragment(tile, edge_at(t, c), edge_at(t + 16, c));
+    };
+    const int wn = (w >> 1) * 32, wk = (w & 1) * 32;
+    f32x4 acc[2][2] = {};
+    int b = 0;
+    if (s0 < s1) load(s0);
+    for (int64_t s = s0; s < s1; ++s) {
+        for (int part = 0; part < PARTS; ++part, b ^= 1) {
+            *reinterpret_cast<u32x4*>(&dy_s[b][edge_at(t0, cc)]) = as_bf16<T>(dy, part);
+            *reinterpret_cast<u32x4*>(&x_s[b][edge_at(t0, cc)]) = decode_bf16(xq, xe);
+            __syncthreads();
+            if (part == PARTS - 1 && s + 1 < s1) load(s + 1);
+            bf16x8 fx[2], fy[2];
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                fx[i] = fragment(x_s[b], wk + 16 * i);
+                fy[i] = fragment(dy_s[b], wn + 16 * i);
+            }
+#pragma unroll
+            for (int i = 0; i < 2; ++i)
+#pragma unroll
+                for (int j = 0; j < 2; ++j)
+                    acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fx[j], fy[i], acc[i][j], 0, 0, 0);
+        }
+    }
+    // lane: row n = l % 16, columns k = 4 (l / 16) + 0..3
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        const int64_t n = n0 + wn + 16 * i + (lane & 15);
+        if (n >= a.out) continue;
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+            const int k = k0 + wk + 16 * j + 4 * (lane >> 4);
+            write4<O>(a, blockIdx.z, n, k, std::min(4, a.s.cols - k), acc[i][j]);
+        }
+    }
+}
+
+// B x B outputs, for out_features and in_features of at least B: the last tile of a side is moved back to end with it, so that no
+// load needs a bounds check, and leaves what the tile before it has written. B = 256: 8 wavefronts of 128 x 64 (2 along n, 4 along
+// k), one workgroup per compute unit; B = 128: 4 wavefronts of 64 x 64, up to four.
+constexpr int kBig = 256, kMid = 128;
 
 // The shape of the products, M x M. 16 x 16 x 32 takes more cycles than 32 x 32 x 16 and keeps a higher clock (8192 tokens and
 // features: 1.85M cycles at 2.13 GHz against 1.74M at 1.92 GHz), so bf16 dy takes it; fp32 dy, whose staging needs the
@@ -241,48 +248,40 @@ struct Product<32> {
     }
 };
 
-template <int M>
-__device__ __forceinline__ int big_at(int t, int c) {
-    return t * kBig + ((((c >> 4) ^ Product<M>::swizzle(t)) << 4) | (c & 15));
-}
-
-__device__ __forceinline__ bf16x8 big_fragment(const uint16_t* tile, int at0, int at1) {
-    union {
-        s16x4 h[2];
-        bf16x8 f;
-    } u;
-    u.h[0] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4)(lds_u16)(uint16_t*)(tile + at0));
-    u.h[1] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4)(lds_u16)(uint16_t*)(tile + at1));
-    return u.f;
+template <int B, int M>
+__device__ __forceinline__ int tile_at(int t, int c) {
+    return t * B + ((((c >> 4) ^ (Product<M>::swizzle(t) & (B / 16 - 1))) << 4) | (c & 15));
 }
 
 // Workgroup -> tile. An XCD takes a contiguous share of the tiles, in bands of 8 along n: the 32 that it works on at a time
 // are 8 x 4, so each of their rows and columns of tiles is read from memory once and by the others from the XCD's L2.
-struct BigTile {
+struct TileId {
     int n, k, split;
 };
 constexpr uint32_t kBand = 8;
-__device__ __forceinline__ BigTile big_tile(const Wgrad& a) {
-    const uint32_t nt = (uint32_t)((a.out + kBig - 1) / kBig), kt = (uint32_t)((a.s.cols + kBig - 1) / kBig);
+template <int B>
+__device__ __forceinline__ TileId tile_id(const Wgrad& a) {
+    const uint32_t nt = (uint32_t)((a.out + B - 1) / B), kt = (uint32_t)((a.s.cols + B - 1) / B);
     const uint32_t id = xcd_block(), split = id / (nt * kt), r = id - split * (nt * kt), band = r / (kBand * kt),
                    rows = min(kBand, nt - band * kBand), q = r - band * kBand * kt, k = q / rows;
     return {(int)(band * kBand + q - k * rows), (int)k, (int)split};
 }
 
-template <typename T, typename O>
-__global__ __launch_bounds__(512, 2) void wgrad_big_kernel(Wgrad a) {
-    constexpr int PARTS = sizeof(T) == 4 ? 3 : 1, BT = kBigTokens, C = BT / 16;
-    constexpr int M = PARTS == 1 ? 16 : 32, FN = 128 / M, FK = 64 / M, H = BT / Product<M>::kTokens;
-    __shared__ __attribute__((aligned(16))) uint16_t dy_s[2][BT * kBig], x_s[2][BT * kBig];
+template <typename T, typename O, int B>
+__global__ __launch_bounds__(2 * B, B == kBig ? 2 : 3) void wgrad_tile_kernel(Wgrad a) {
+    constexpr int PARTS = sizeof(T) == 4 ? 3 : 1, BT = kTurn, C = BT / 16;
+    constexpr int WN = B / 2, WK = 64, M = PARTS == 1 ? 16 : 32, FN = WN / M, FK = WK / M, H = BT / Product<M>::kTokens;
+    __shared__ __attribute__((aligned(16))) uint16_t dy_s[2][BT * B], x_s[2][BT * B];
     const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
-    const BigTile tile = big_tile(a);
-    const int64_t n_first = (int64_t)tile.n * kBig, n0 = std::min(n_first, a.out - kBig);
-    const int k_first = tile.k * kBig, k0 = std::min(k_first, a.s.pitch - kBig);
+    const TileId tile = tile_id<B>(a);
+    const int64_t n_first = (int64_t)tile.n * B, n0 = std::min(n_first, a.out - B);
+    const int k_first = tile.k * B, k0 = std::min(k_first, a.s.pitch - B);
     const int64_t steps = (a.s.rows + BT - 1) / BT;
     const int64_t s0 = steps * tile.split / a.splits, s1 = steps * (tile.split + 1) / a.splits;
 
-    // this thread stages columns 8 (tid % 32) .. + 7 of tokens tid / 32 + 16 i: 32-bit offsets from a step's first token
-    const int cc = (tid & 31) * 8, t0 = tid >> 5;
+    // this thread stages columns 8 (tid % (B / 8)) .. + 7 of tokens tid / (B / 8) + 16 i: 32-bit offsets from a step's
+    // first token
+    const int cc = tid % (B / 8) * 8, t0 = tid / (B / 8);
     uint32_t od[C], ox[C], oe[C];
     const auto offsets = [&](int64_t step) __attribute__((always_inline)) {
         const int last = (int)std::min<int64_t>(a.s.rows - 1 - step * BT, BT - 1);
@@ -323,40 +322,35 @@ __global__ __launch_bounds__(512, 2) void wgrad_big_kernel(Wgrad a) {
     };
     const auto stage_dy = [&](uint16_t* tile, int part) __attribute__((always_inline)) {
 #pragma unroll
-        for (int i = 0; i < C; ++i) *reinterpret_cast<u32x4*>(&tile[big_at<M>(t0 + 16 * i, cc)]) = as_bf16<T>(dy[i], part);
+        for (int i = 0; i < C; ++i) *reinterpret_cast<u32x4*>(&tile[tile_at<B, M>(t0 + 16 * i, cc)]) = as_bf16<T>(dy[i], part);
     };
     const auto stage_x = [&](uint16_t* tile) __attribute__((always_inline)) {
 #pragma unroll
         for (int i = 0; i < C; ++i) {
-            float v[8];
-            e8_decode(xq[i], xe[i], v);
-            u32x4 q;
-#pragma unroll
-            for (int j = 0; j < 4; ++j) q[j] = __builtin_amdgcn_perm(f_bits(v[2 * j + 1]), f_bits(v[2 * j]), 0x07060302u);
-            *reinterpret_cast<u32x4*>(&tile[big_at<M>(t0 + 16 * i, cc)]) = q;
+            *reinterpret_cast<u32x4*>(&tile[tile_at<B, M>(t0 + 16 * i, cc)]) = decode_bf16(xq[i], xe[i]);
         }
     };
 
-    const int wn = (w >> 2) * 128, wk = (w & 3) * 64, ft = Product<M>::token(lane), fc = Product<M>::column(lane);
+    const int wn = w / (B / WK) * WN, wk = w % (B / WK) * WK, ft = Product<M>::token(lane), fc = Product<M>::column(lane);
     int ay[FN][2], ax[FK][2];  // a fragment's two reads
 #pragma unroll
     for (int r = 0; r < 2; ++r) {
 #pragma unroll
-        for (int i = 0; i < FN; ++i) ay[i][r] = big_at<M>(ft + r * Product<M>::kTokens / 2, wn + M * i + fc);
+        for (int i = 0; i < FN; ++i) ay[i][r] = tile_at<B, M>(ft + r * Product<M>::kTokens / 2, wn + M * i + fc);
 #pragma unroll
-        for (int j = 0; j < FK; ++j) ax[j][r] = big_at<M>(ft + r * Product<M>::kTokens / 2, wk + M * j + fc);
+        for (int j = 0; j < FK; ++j) ax[j][r] = tile_at<B, M>(ft + r * Product<M>::kTokens / 2, wk + M * j + fc);
     }
     typename Product<M>::acc_t acc[FN][FK] = {};
     const auto multiply = [&](const uint16_t* ty, const uint16_t* tx) __attribute__((always_inline)) {
 #pragma unroll
         for (int h = 0; h < H; ++h) {
-            const int at = h * Product<M>::kTokens * kBig;
+            const int at = h * Product<M>::kTokens * B;
             bf16x8 fx[FK];
 #pragma unroll
-            for (int j = 0; j < FK; ++j) fx[j] = big_fragment(tx + at, ax[j][0], ax[j][1]);
+            for (int j = 0; j < FK; ++j) fx[j] = tile_fragment(tx + at, ax[j][0], ax[j][1]);
 #pragma unroll
             for (int i = 0; i < FN; ++i) {
-                const bf16x8 fy = big_fragment(ty + at, ay[i][0], ay[i][1]);
+                const bf16x8 fy = tile_fragment(ty + at, ay[i][0], ay[i][1]);
 #pragma unroll
                 for (int j = 0; j < FK; ++j) acc[i][j] = Product<M>::mul(fx[j], fy, acc[i][j]);
             }
@@ -389,14 +383,14 @@ __global__ __launch_bounds__(512, 2) void wgrad_big_kernel(Wgrad a) {
             // the matrix instructions with fragments two ahead, the decoding and the LDS writes between them, then the loads
             __builtin_amdgcn_sched_group_barrier(0x100, 12, 0);
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
+            for (int i = 0; i < FN; ++i) {
 #pragma unroll
-                for (int j = 0; j < 4; ++j) {
+                for (int j = 0; j < FK; ++j) {
                     __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
-                    if (j < 2 && i < 6) __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
-                    if (i >= 4) __builtin_amdgcn_sched_group_barrier(0x002, 5, 0);
+                    if (j < 2 && i < FN - 2) __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+                    if (i >= FN / 2) __builtin_amdgcn_sched_group_barrier(0x002, 5, 0);
+                    if (i >= FN / 2 && j % 2 == 1 && (B != kBig || j == 3)) __builtin_amdgcn_sched_group_barrier(0x200, 1, 0);
                 }
-                if (i >= 4) __builtin_amdgcn_sched_group_barrier(0x200, 1, 0);
             }
             __builtin_amdgcn_sched_group_barrier(0x020, 6, 0);
         }
@@ -425,33 +419,45 @@ __global__ __launch_bounds__(512, 2) void wgrad_big_kernel(Wgrad a) {
 #pragma unroll
             for (int q = 0; q < Product<M>::kQuads; ++q) {
                 const int k = k0 + wk + M * j + Product<M>::quad(lane, q), in = std::min(4, a.s.cols - k);
-                if (k < k_first || in <= 0) continue;
+                if (k < k_first) continue;
                 f32x4 v;
 #pragma unroll
                 for (int r = 0; r < 4; ++r) v[r] = acc[i][j][4 * q + r];
-                if (a.splits > 1) {
-                    float* const p = a.part + ((int64_t)tile.split * a.out + n) * a.s.cols + k;
-#pragma unroll
-                    for (int r = 0; r < 4; ++r)
-                        if (r < in) p[r] = v[r];
-                } else {
-                    finish4<O>(a, n, k, in, v);
-                }
+                write4<O>(a, tile.split, n, k, in, v);
             }
         }
     }
 }
 
-// The splits' partial products, added in order.
+// The splits' partial products, added in order: four columns a lane, up to 8 splits' loads in flight.
 template <typename O>
-__global__ __launch_bounds__(256) void wgrad_join_kernel(Wgrad a) {
-    const int64_t total = a.out * a.s.cols;
-    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < total; i += (int64_t)gridDim.x * 256) {
-        float v = 0.0f;
-        for (int s = 0; s < a.splits; ++s) v += a.part[(int64_t)s * total + i];
-        const int64_t n = i / a.s.cols;
-        finish<O>(a, n, (int)(i - n * a.s.cols), v);
+__global__ __launch_bounds__(256) void wgrad_join_kernel(Wgrad a, FastDiv quads, uint32_t total) {
+    const uint32_t i = xcd_block() * 256 + threadIdx.x;
+    if (i >= total) return;
+    const uint32_t n = quotient(i, quads);
+    const int k = (int)(i - n * quads.d) * 4, in = std::min(4, a.s.cols - k);
+    const int64_t size = a.out * a.s.cols;
+    const float* p = a.part + (int64_t)n * a.s.cols + k;
+    typedef float f32x4_a4 __attribute__((ext_vector_type(4), aligned(4)));
+    f32x4 v = {};
+    if (in == 4) {
+        int s = 0;
+        for (; s + 8 <= a.splits; s += 8) {
+            f32x4 t[8];
+#pragma unroll
+            for (int r = 0; r < 8; ++r) t[r] = *reinterpret_cast<const f32x4_a4*>(p + r * size);
+            p += 8 * size;
+#pragma unroll
+            for (int r = 0; r < 8; ++r) v += t[r];
+        }
+        for (; s < a.splits; ++s, p += size) v += *reinterpret_cast<const f32x4_a4*>(p);
+    } else {
+        for (int s = 0; s < a.splits; ++s, p += size)
+#pragma unroll
+            for (int r = 0; r < 3; ++r)
+                if (r < in) v[r] += p[r];
     }
+    finish4<O>(a, n, k, in, v);
 }
 
 // Column sums of dy over every bparts-th slab of 64 rows: 8 columns a lane, 4 wavefronts a workgroup.
@@ -496,15 +502,17 @@ hipError_t run(const Wgrad& a, hipStream_t st) {
     }
     if (a.s.cols == 0) return hipSuccess;
     // the large tiles' 32-bit offsets span 32 rows
-    const int tile = a.dy.ld < (1 << 25) && a.s.pitch < (1 << 26) ? a.tile : kSmallTile;
+    const int tile = a.dy.ld < (1 << 25) && a.s.pitch < (1 << 26) ? a.tile : kEdge;
     const dim3 n((uint32_t)((a.s.cols + tile - 1) / tile), (uint32_t)((a.out + tile - 1) / tile), (uint32_t)a.splits);
     if (tile == kBig)
-        wgrad_big_kernel<T, O><<<n.x * n.y * n.z, 512, 0, st>>>(a);
+        wgrad_tile_kernel<T, O, kBig><<<n.x * n.y * n.z, 2 * kBig, 0, st>>>(a);
+    else if (tile == kMid)
+        wgrad_tile_kernel<T, O, kMid><<<n.x * n.y * n.z, 2 * kMid, 0, st>>>(a);
     else
-        wgrad_small_kernel<T, O><<<n, 256, 0, st>>>(a);
+        wgrad_edge_kernel<T, O><<<n, 256, 0, st>>>(a);
     if (a.splits > 1) {
-        const int64_t total = a.out * a.s.cols;
-        wgrad_join_kernel<O><<<dim3((uint32_t)std::min<int64_t>((total + 255) / 256, 4096)), 256, 0, st>>>(a);
+        const uint32_t quads = (uint32_t)((a.s.cols + 3) / 4), total = (uint32_t)a.out * quads;
+        wgrad_join_kernel<O><<<(total + 255) / 256, 256, 0, st>>>(a, fast_div(quads), total);
     }
     return hipGetLastError();
 }
@@ -513,12 +521,9 @@ hipError_t run(const Wgrad& a, hipStream_t st) {
 
 WgradPlan wgrad_plan(int dtype, int64_t tokens, int64_t out, int64_t in) {
     WgradPlan p;
-    const int64_t steps = (tokens + kSmallTokens - 1) / kSmallTokens;
+    const int64_t steps = (tokens + kTurn - 1) / kTurn;
     const auto tiles = [&](int64_t t) { return std::max<int64_t>(1, ((out + t - 1) / t) * ((in + t - 1) / t)); };
-#ifndef BIGMIN
-#define BIGMIN 100
-#endif
-    p.tile = out >= kBig && in >= kBig && tiles(kBig) >= BIGMIN ? kBig : kSmallTile;
+    p.tile = std::min(out, in) < kMid ? kEdge : std::min(out, in) < kBig || tiles(kBig) < 100 ? kMid : kBig;
     const int64_t n = tiles(p.tile), fill = p.tile == kBig ? 256 : 512;
     // two workgroups for each of the 256 compute units, and at least 8 steps each
     p.splits = (int32_t)std::max<int64_t>(1, std::min(fill / n, steps / 8));
