@@ -76,13 +76,13 @@ def _mat(t, name: str, rows: int, cols: int, dtype):
     ld, inner = t.stride()
     if inner != 1 and cols > 1:
         raise ValueError(f"{name}: rows must be contiguous (strides {t.stride()})")
-    return t.data_ptr(), max(ld, cols)
+    return t.data_ptr(), ld if ld > cols else cols
 
 
 def _vec(t, name: str, n: int, dtype):
     if t is None:
         return None
-    if t.dtype != dtype or t.numel() != n or not t.is_contiguous() or not t.is_cuda:
+    if t.dtype is not dtype or t.numel() != n or not t.is_contiguous() or not t.is_cuda:
         raise ValueError(f"{name}: a contiguous {dtype} GPU tensor of {n} is needed")
     return t.data_ptr()
 

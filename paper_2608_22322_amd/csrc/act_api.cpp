@@ -95,9 +95,9 @@ al_status check_kind(int32_t kind, const char* who) {
     return AL_OK;
 }
 
-size_t norm_ws(int32_t kind, int32_t dtype, int64_t rows, int64_t cols) {
+size_t norm_ws(int32_t kind, int64_t rows, int64_t cols) {
     const bool layer = kind == AL_NORM_LAYER;
-    return align256((size_t)al::norm_backward_parts(dtype, layer, rows, cols) * cols * 4 * (layer ? 2 : 1));
+    return align256((size_t)al::norm_backward_parts(rows, cols) * cols * 4 * (layer ? 2 : 1));
 }
 
 }  // namespace
@@ -190,7 +190,7 @@ al_status al_norm_backward_workspace_bytes(int32_t kind, int32_t dtype, int64_t 
     AL_TRY(check_kind(kind, who));
     AL_TRY(check_dtype(dtype, who, "dtype"));
     AL_TRY(check_shape(rows, cols, who));
-    *bytes = norm_ws(kind, dtype, rows, cols);
+    *bytes = norm_ws(kind, rows, cols);
     return AL_OK;
 }
 
@@ -229,7 +229,7 @@ al_status al_norm_backward(int32_t kind, int32_t dtype, const void* dy, int64_t 
         if (!rstd || (layer && !coded && !mean)) return fail(AL_EINVAL, "%s: mean or rstd is NULL", who);
     }
     const bool weights = dgamma || dbeta;
-    if (weights) AL_TRY(check_ws(ws, ws_bytes, norm_ws(kind, dtype, rows, cols), who));
+    if (weights) AL_TRY(check_ws(ws, ws_bytes, norm_ws(kind, rows, cols), who));
     al::NormBackward a;
     std::memset(&a, 0, sizeof(a));
     a.dy = mat(dy, lddy);
@@ -244,7 +244,8 @@ al_status al_norm_backward(int32_t kind, int32_t dtype, const void* dy, int64_t 
     a.dgamma = dgamma;
     a.dbeta = dbeta;
     a.part = weights ? static_cast<float*>(ws) : nullptr;
-    a.parts = al::norm_backward_parts(dtype, layer, rows, cols);
+    a.parts = al::norm_backward_parts(rows, cols);
+    a.grad_bf16 = grad_dtype == AL_DTYPE_BF16;
     return launched(al::launch_norm_backward(dtype, layer, grad_dtype, a, as_stream(stream)), who);
 }
 

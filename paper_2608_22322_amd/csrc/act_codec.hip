@@ -41,20 +41,11 @@ struct Place {
 // activation 20.7 -> 17.7 and 143 -> 122); codes are stored for a later reader, who finds small ones in the last-level cache.
 template <typename T>
 __device__ __forceinline__ void load_mat(Chunk<T>& k, const Mat& m, const Place& at, int cols) {
-    const T* const row = static_cast<const T*>(m.p) + at.row * m.ld;
-    if (at.c + 8 <= cols)
-        k.load_nt(row + at.c);
-    else
-        load_chunk(k, row, at.c, cols);
+    load_chunk<T, true>(k, static_cast<const T*>(m.p) + at.row * m.ld, at.c, cols);
 }
 template <typename T>
 __device__ __forceinline__ void store_mat(const Mat& m, const Place& at, int cols, const float (&v)[8]) {
-    T* const row = static_cast<T*>(m.p) + at.row * m.ld;
-    if (!at.in) return;
-    if (at.c + 8 <= cols)
-        store8_nt(row + at.c, v);
-    else
-        store_chunk(row, at.c, cols, v);
+    if (at.in) store_chunk<true>(static_cast<T*>(m.p) + at.row * m.ld, at.c, cols, v);
 }
 
 struct Coded {

@@ -68,10 +68,11 @@ struct NormBackward {
     void *dgamma, *dbeta;
     float* part;  // workspace: [2][parts][cols] partial sums of dgamma, dbeta
     int32_t parts;
+    bool grad_bf16;
     int64_t row0;  // set by the launcher: a call's first row
 };
 // Rows of partial sums that a call writes: a rule on the sizes alone.
-int32_t norm_backward_parts(int dtype, bool layer, int64_t rows, int64_t cols);
+int32_t norm_backward_parts(int64_t rows, int64_t cols);
 hipError_t launch_norm_backward(int dtype, bool layer, int grad_dtype, const NormBackward& a, hipStream_t st);
 
 struct Wgrad {
@@ -94,7 +95,12 @@ struct WgradPlan {
 WgradPlan wgrad_plan(int dtype, int64_t tokens, int64_t out, int64_t in);
 hipError_t launch_wgrad(int dtype, int grad_dtype, const Wgrad& a, hipStream_t st);
 
-// Sums over the rows of a [parts][cols] fp32 array in a fixed order, written as grad_dtype.
-hipError_t launch_fold(int grad_dtype, const float* part, int32_t parts, int64_t cols, void* out, hipStream_t st);
+// Sums over the rows of `count` [parts][cols] fp32 arrays, one behind the other, in a fixed order: written as
+// grad_dtype to g and as fp32 to f (each where it is not NULL).
+struct FoldOut {
+    void* g;
+    float* f;
+};
+hipError_t launch_fold(int grad_dtype, const float* part, int32_t parts, int64_t cols, const FoldOut* out, int count, hipStream_t st);
 
 }  // namespace al

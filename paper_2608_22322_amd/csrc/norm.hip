@@ -59,7 +59,7 @@ __global__ __launch_bounds__(G < 256 ? 256 : G) void norm_forward_kernel(NormFor
     const T* const x = static_cast<const T*>(a.x.p) + row * a.x.ld;
     Chunk<T> raw[K];
 #pragma unroll
-    for (int k = 0; k < K; ++k) load_chunk(raw[k], x, (k * G + lane) * 8, cols);
+    for (int k = 0; k < K; ++k) load_chunk<T, true>(raw[k], x, (k * G + lane) * 8, cols);
     float v[K][8], sum = 0.0f;
 #pragma unroll
     for (int k = 0; k < K; ++k) {
@@ -115,7 +115,7 @@ __global__ __launch_bounds__(G < 256 ? 256 : G) void norm_forward_kernel(NormFor
 #pragma unroll
                 for (int j = 0; j < 8; ++j) v[k][j] += w[j];
             }
-            store_chunk(y, c, cols, v[k]);
+            store_chunk<true>(y, c, cols, v[k]);
         }
     }
 }
@@ -193,7 +193,7 @@ struct RowChunk {
     uint32_t e;
     __device__ __forceinline__ void load(const NormBackward& a, int64_t row, int c) {
         const int cols = a.s.cols;
-        load_chunk(dy, static_cast<const T*>(a.dy.p) + row * a.dy.ld, c, cols);
+        load_chunk<T, true>(dy, static_cast<const T*>(a.dy.p) + row * a.dy.ld, c, cols);
         if constexpr (CODE) {
             q = 0u;
             e = 0u;
@@ -202,9 +202,9 @@ struct RowChunk {
                 e = a.c.e[row * a.s.nb + (c >> (3 + a.s.lb))];
             }
         } else {
-            load_chunk(x, static_cast<const T*>(a.x.p) + row * a.x.ld, c, cols);
+            load_chunk<T, true>(x, static_cast<const T*>(a.x.p) + row * a.x.ld, c, cols);
         }
-        if (a.add.p) load_chunk(add, static_cast<const T*>(a.add.p) + row * a.add.ld, c, cols);
+        if (a.add.p) load_chunk<T, true>(add, static_cast<const T*>(a.add.p) + row * a.add.ld, c, cols);
     }
     // xhat; columns past the width give 0
     __device__ __forceinline__ void xhat(float mean, float rstd, int n, float (&v)[8]) const {
@@ -218,11 +218,30 @@ struct RowChunk {
     }
 };
 
-// Rows r0, r0 + gridDim * R, ...: dx of each, and the group's sums over its rows of dy xhat and dy.
+// Two sums at once over the G lanes of a group; buf: 2 G / 64 floats.
+template <int G>
+__device__ __forceinline__ void group_sum2(float& u, float& v, float* buf) {
+    u = wave_sum(u);
+    v = wave_sum(v);
+    if constexpr (G > 64) {
+        if ((threadIdx.x & 63) == 0) {
+            buf[threadIdx.x >> 6] = u;
+            buf[G / 64 + (threadIdx.x >> 6)] = v;
+        }
+        __syncthreads();
+        u = v = 0.0f;
+#pragma unroll
+        for (int w = 0; w < G / 64; ++w) u += buf[w], v += buf[G / 64 + w];
+    }
+}
+
+// Rows r0, r0 + gridDim * R, ...: dx of each, and the group's sums over its rows of dy xhat and dy. The next row is
+// on its way while one is reduced.
 template <typename T, int G, int K, bool CODE, bool LAYER>
 __global__ __launch_bounds__(G < 256 ? 256 : G) void norm_backward_kernel(NormBackward a) {
     constexpr int R = G < 256 ? 256 / G : 1;  // rows at a time
-    __shared__ float buf[2][2][16];
+    constexpr bool LEAN = K > 2;              // registers for one row: none ahead, gamma read for each
+    __shared__ float buf[2][2 * 16];
     __shared__ float fold[R > 1 ? R * G * 8 : 1];
     const int lane = threadIdx.x % G, group = threadIdx.x / G, cols = a.s.cols;
     const float inv_n = 1.0f / (float)cols;
@@ -232,14 +251,29 @@ __global__ __launch_bounds__(G < 256 ? 256 : G) void norm_backward_kernel(NormBa
         const int c = (k * G + lane) * 8;
 #pragma unroll
         for (int j = 0; j < 8; ++j) gam[k][j] = 1.0f, dg[k][j] = db[k][j] = 0.0f;
-        if (a.gamma) load8f(a.gamma, c, cols, 0.0f, gam[k]);
+        if (!LEAN && a.gamma) load8f(a.gamma, c, cols, 0.0f, gam[k]);
     }
-    int turn = 0;
-    for (int64_t row = (int64_t)blockIdx.x * R + group; row < a.s.rows; row += (int64_t)gridDim.x * R, turn ^= 1) {
+    RowChunk<T, CODE> next[K];
+    float next_rstd = 0.0f, next_mean = 0.0f;
+    const auto fetch = [&](int64_t row) {
+#pragma unroll
+        for (int k = 0; k < K; ++k) next[k].load(a, row, (k * G + lane) * 8);
+        next_rstd = a.rstd[row];
+        if (LAYER && !CODE) next_mean = a.mean[row];
+    };
+    const int64_t step = (int64_t)gridDim.x * R;
+    int64_t row = (int64_t)blockIdx.x * R + group;
+    if (!LEAN && row < a.s.rows) fetch(row);
+    for (int turn = 0; row < a.s.rows; row += step, turn ^= 1) {
+        if (LEAN) fetch(row);
         RowChunk<T, CODE> r[K];
 #pragma unroll
-        for (int k = 0; k < K; ++k) r[k].load(a, row, (k * G + lane) * 8);
-        const float rstd = a.rstd[row], mean = LAYER && !CODE ? a.mean[row] : 0.0f;
+        for (int k = 0; k < K; ++k) {
+            r[k] = next[k];
+            if (LEAN && a.gamma) load8f(a.gamma, (k * G + lane) * 8, cols, 0.0f, gam[k]);
+        }
+        const float rstd = next_rstd, mean = next_mean;
+        if (!LEAN && row + step < a.s.rows) fetch(row + step);
         float s1 = 0.0f, s2 = 0.0f;
 #pragma unroll
         for (int k = 0; k < K; ++k) {
@@ -256,8 +290,12 @@ __global__ __launch_bounds__(G < 256 ? 256 : G) void norm_backward_kernel(NormBa
             s1 += sum8(t);
             s2 += sum8(u);
         }
-        if (LAYER) s1 = group_sum<G>(s1, buf[turn][0]) * inv_n;
-        s2 = group_sum<G>(s2, buf[turn][1]) * inv_n;
+        if (LAYER)
+            group_sum2<G>(s1, s2, buf[turn]);
+        else
+            s2 = group_sum<G>(s2, buf[turn]);
+        s1 *= inv_n;
+        s2 *= inv_n;
         T* const dx = static_cast<T*>(a.dx.p) + row * a.dx.ld;
 #pragma unroll
         for (int k = 0; k < K; ++k) {
@@ -277,13 +315,15 @@ __global__ __launch_bounds__(G < 256 ? 256 : G) void norm_backward_kernel(NormBa
 #pragma unroll
                 for (int j = 0; j < 8; ++j) v[j] += w[j];
             }
-            if (c < cols) store_chunk(dx, c, cols, v);
+            if (c < cols) store_chunk<true>(dx, c, cols, v);
         }
     }
     if (!a.part) return;
-    // the workgroup's sums: its R groups in order, then one row of partials each for dgamma and dbeta
+    // the workgroup's sums: its R groups in order, then one row of partials each for dgamma and dbeta (or, of a single
+    // workgroup, the gradients themselves)
     for (int which = 0; which < (LAYER ? 2 : 1); ++which) {
         float* const out = a.part + ((int64_t)which * a.parts + blockIdx.x) * cols;
+        void* const grad = which ? a.dbeta : a.dgamma;
 #pragma unroll
         for (int k = 0; k < K; ++k) {
             const int c = (k * G + lane) * 8;
@@ -302,7 +342,13 @@ __global__ __launch_bounds__(G < 256 ? 256 : G) void norm_backward_kernel(NormBa
                         for (int j = 0; j < 8; ++j) v[j] += fold[(g * 8 + j) * G + lane];
                 }
             }
-            if (group == 0 && c < cols) store_chunk(out, c, cols, v);
+            if (group != 0 || c >= cols) continue;
+            if (a.parts > 1)
+                store_chunk(out, c, cols, v);
+            else if (grad && a.grad_bf16)
+                store_chunk(static_cast<bf16*>(grad), c, cols, v);
+            else if (grad)
+                store_chunk(static_cast<float*>(grad), c, cols, v);
         }
     }
 }
@@ -370,25 +416,35 @@ __global__ __launch_bounds__(64) void norm_weights_wide_kernel(NormBackward a) {
     if (LAYER) store_chunk(a.part + ((int64_t)a.parts + blockIdx.y) * cols, c, cols, db);
 }
 
-// out[c] = sum over p of part[p][c]: 64 columns a workgroup, 4 wavefronts taking every fourth row.
+// Column sums of partial sums: 64 columns a workgroup, wavefront w of 16 takes rows w, w + 16, ..., 8 of them in flight.
 template <typename O>
-__global__ __launch_bounds__(256) void fold_kernel(const float* part, int32_t parts, int64_t cols, O* out) {
-    __shared__ float buf[4][64];
+__global__ __launch_bounds__(1024) void fold_kernel(const float* part, int32_t parts, int64_t cols, FoldOut o0, FoldOut o1) {
+    __shared__ float buf[16][64];
     const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
     const int64_t c = (int64_t)blockIdx.x * 64 + lane;
+    const FoldOut o = blockIdx.y ? o1 : o0;
+    const float* const p0 = part + (int64_t)blockIdx.y * parts * cols + c;
     float s = 0.0f;
     if (c < cols) {
-        float t[4] = {};
         int p = w;
-        for (; p + 12 < parts; p += 16)
+        float t[8] = {};
+        for (; p + 112 < parts; p += 128)
 #pragma unroll
-            for (int i = 0; i < 4; ++i) t[i] += part[(int64_t)(p + 4 * i) * cols + c];
-        for (; p < parts; p += 4) t[0] += part[(int64_t)p * cols + c];
-        s = (t[0] + t[1]) + (t[2] + t[3]);
+            for (int i = 0; i < 8; ++i) t[i] += p0[(int64_t)(p + 16 * i) * cols];
+#pragma unroll
+        for (int i = 0; i < 7; ++i)
+            if (p + 16 * i < parts) t[i] += p0[(int64_t)(p + 16 * i) * cols];
+        s = sum8(t);
     }
     buf[w][lane] = s;
     __syncthreads();
-    if (w == 0 && c < cols) put(out + c, (buf[0][lane] + buf[1][lane]) + (buf[2][lane] + buf[3][lane]));
+    if (w > 0 || c >= cols) return;
+    float a[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) a[i] = buf[i][lane] + buf[i + 8][lane];
+    s = sum8(a);
+    if (o.g) put(static_cast<O*>(o.g) + c, s);
+    if (o.f) o.f[c] = s;
 }
 
 // Lanes and chunks per lane that hold a row of `chunks` chunks.
@@ -396,11 +452,11 @@ struct Shape {
     int g, k;
 };
 Shape row_shape(int64_t chunks) {
-    for (int k = 1; k <= 4; k *= 2)
-        if (chunks <= 64 * k) return {64, k};
-    for (int k = 2; k <= 4; k *= 2)
-        if (chunks <= 256 * k) return {256, k};
-    return {1024, 2};
+    if (chunks <= 64) return {64, 1};
+    if (chunks <= 128) return {64, 2};
+    if (chunks <= 256) return {256, 1};
+    if (chunks <= 512) return {256, 2};
+    return {512, chunks <= 1024 ? 2 : chunks <= 1536 ? 3 : 4};
 }
 
 constexpr int64_t kSlab = 1 << 21;  // rows of one launch (a grid holds fewer than 2^32 threads)
@@ -417,14 +473,16 @@ hipError_t forward_slab(bool layer, const NormForward& a, int64_t rows, hipStrea
         norm_forward_kernel<T, 64, 1><<<n, 256, 0, st>>>(a, layer);
     else if (s.g == 64 && s.k == 2)
         norm_forward_kernel<T, 64, 2><<<n, 256, 0, st>>>(a, layer);
-    else if (s.g == 64)
-        norm_forward_kernel<T, 64, 4><<<n, 256, 0, st>>>(a, layer);
+    else if (s.g == 256 && s.k == 1)
+        norm_forward_kernel<T, 256, 1><<<n, 256, 0, st>>>(a, layer);
     else if (s.g == 256 && s.k == 2)
         norm_forward_kernel<T, 256, 2><<<n, 256, 0, st>>>(a, layer);
-    else if (s.g == 256)
-        norm_forward_kernel<T, 256, 4><<<n, 256, 0, st>>>(a, layer);
-    else
-        norm_forward_kernel<T, 1024, 2><<<n, 1024, 0, st>>>(a, layer);
+    else if (s.g == 512 && s.k == 2)
+        norm_forward_kernel<T, 512, 2><<<n, 512, 0, st>>>(a, layer);
+    else if (s.g == 512 && s.k == 3)
+        norm_forward_kernel<T, 512, 3><<<n, 512, 0, st>>>(a, layer);
+    else if (s.g == 512 && s.k == 4)
+        norm_forward_kernel<T, 512, 4><<<n, 512, 0, st>>>(a, layer);
     return hipGetLastError();
 }
 
@@ -451,14 +509,16 @@ hipError_t backward(NormBackward a, hipStream_t st) {
         norm_backward_kernel<T, 64, 1, CODE, LAYER><<<n, 256, 0, st>>>(a);
     else if (s.g == 64 && s.k == 2)
         norm_backward_kernel<T, 64, 2, CODE, LAYER><<<n, 256, 0, st>>>(a);
-    else if (s.g == 64)
-        norm_backward_kernel<T, 64, 4, CODE, LAYER><<<n, 256, 0, st>>>(a);
+    else if (s.g == 256 && s.k == 1)
+        norm_backward_kernel<T, 256, 1, CODE, LAYER><<<n, 256, 0, st>>>(a);
     else if (s.g == 256 && s.k == 2)
         norm_backward_kernel<T, 256, 2, CODE, LAYER><<<n, 256, 0, st>>>(a);
-    else if (s.g == 256)
-        norm_backward_kernel<T, 256, 4, CODE, LAYER><<<n, 256, 0, st>>>(a);
-    else
-        norm_backward_kernel<T, 1024, 2, CODE, LAYER><<<n, 1024, 0, st>>>(a);
+    else if (s.g == 512 && s.k == 2)
+        norm_backward_kernel<T, 512, 2, CODE, LAYER><<<n, 512, 0, st>>>(a);
+    else if (s.g == 512 && s.k == 3)
+        norm_backward_kernel<T, 512, 3, CODE, LAYER><<<n, 512, 0, st>>>(a);
+    else if (s.g == 512 && s.k == 4)
+        norm_backward_kernel<T, 512, 4, CODE, LAYER><<<n, 512, 0, st>>>(a);
     return hipGetLastError();
 }
 
@@ -470,12 +530,13 @@ hipError_t backward(bool layer, const NormBackward& a, hipStream_t st) {
 
 }  // namespace
 
-hipError_t launch_fold(int grad_dtype, const float* part, int32_t parts, int64_t cols, void* out, hipStream_t st) {
-    const dim3 n((uint32_t)((cols + 63) / 64));
+hipError_t launch_fold(int grad_dtype, const float* part, int32_t parts, int64_t cols, const FoldOut* out, int count, hipStream_t st) {
+    const dim3 n((uint32_t)((cols + 63) / 64), (uint32_t)count);
+    const FoldOut &a = out[0], &b = out[count - 1];
     if (grad_dtype == AL_DTYPE_BF16)
-        fold_kernel<bf16><<<n, 256, 0, st>>>(part, parts, cols, static_cast<bf16*>(out));
+        fold_kernel<bf16><<<n, 1024, 0, st>>>(part, parts, cols, a, b);
     else
-        fold_kernel<float><<<n, 256, 0, st>>>(part, parts, cols, static_cast<float*>(out));
+        fold_kernel<float><<<n, 1024, 0, st>>>(part, parts, cols, a, b);
     return hipGetLastError();
 }
 
@@ -483,18 +544,24 @@ hipError_t launch_norm_forward(int dtype, bool layer, const NormForward& a, hipS
     return dtype == AL_DTYPE_BF16 ? forward<bf16>(layer, a, st) : forward<float>(layer, a, st);
 }
 
-int32_t norm_backward_parts(int dtype, bool layer, int64_t rows, int64_t cols) {
-    const Shape s = row_shape((cols + 7) / 8);
-    const int64_t at_a_time = s.g == 64 ? 4 : 1, most = cols > kRowMax ? 64 : 1024;
-    return (int32_t)std::min((rows + at_a_time - 1) / at_a_time, most);
+// Workgroups of the backward pass, each of which leaves a row of partial weight gradients: few enough that these stay a small part
+// of what moves, enough to keep rows in flight (8192 x 4096 bf16: 384 workgroups 42 us, 512 39, 768 40, 1024 44; rows held by
+// a wavefront, 16384 x 500: 512 37, 1024 29, 2048 36). Up to 8 turns go to one workgroup, which needs no second
+// launch (8 rows of 4096: 11.3 and 12.1 us a call).
+int32_t norm_backward_parts(int64_t rows, int64_t cols) {
+    if (cols > kRowMax) return (int32_t)std::min<int64_t>(rows, 64);
+    const bool waves = row_shape((cols + 7) / 8).g == 64;
+    const int64_t turns = waves ? (rows + 3) / 4 : rows, most = waves ? 1024 : 512;
+    return (int32_t)(turns <= 8 ? std::min<int64_t>(turns, 1) : std::min(turns, most));
 }
 
 hipError_t launch_norm_backward(int dtype, bool layer, int grad_dtype, const NormBackward& a, hipStream_t st) {
     hipError_t e = hipSuccess;
     if (a.s.rows > 0) e = dtype == AL_DTYPE_BF16 ? backward<bf16>(layer, a, st) : backward<float>(layer, a, st);
-    if (e == hipSuccess && a.dgamma) e = launch_fold(grad_dtype, a.part, a.parts, a.s.cols, a.dgamma, st);
-    if (e == hipSuccess && a.dbeta)
-        e = launch_fold(grad_dtype, a.part + (int64_t)a.parts * a.s.cols, a.parts, a.s.cols, a.dbeta, st);
+    if (e == hipSuccess && a.part && (a.parts != 1 || a.s.cols > kRowMax)) {
+        const FoldOut out[2] = {{a.dgamma, nullptr}, {a.dbeta, nullptr}};
+        e = launch_fold(grad_dtype, a.part, a.parts, a.s.cols, out, layer ? 2 : 1, st);
+    }
     return e;
 }
 

@@ -5,6 +5,7 @@
 // fp32 dy is the sum of three bf16 numbers, taken in three turns), so every
 // product is exact and the sums are the matrix cores' fp32 ones.
 #include <algorithm>
+#include <cmath>
 #include <type_traits>
 
 #include "act_device.hpp"
@@ -155,14 +156,13 @@ __global__ __launch_bounds__(256) void wgrad_edge_kernel(Wgrad a) {
     u32x2 xq;
     uint32_t xe;
     const int cc = (tid & 7) * 8, t0 = tid >> 3;  // this thread's columns and token of a step
-    const int out = (int)std::min<int64_t>(a.out - n0, kEdge);
     const auto load = [&](int64_t step) {
         const int64_t t = step * kTurn + t0;
         dy.zero();
         xq = 0u;
         xe = 0u;
         if (t >= a.s.rows) return;
-        load_chunk(dy, static_cast<const T*>(a.dy.p) + t * a.dy.ld + n0, cc, out);
+        load_chunk(dy, static_cast<const T*>(a.dy.p) + t * a.dy.ld, (int)n0 + cc, (int)a.out);
         if (k0 + cc < a.s.pitch) {
             xq = *reinterpret_cast<const u32x2*>(a.c.p + t * a.s.pitch + k0 + cc);
             xe = a.c.e[t * a.s.nb + ((k0 + cc) >> (3 + a.s.lb))];
@@ -460,44 +460,50 @@ __global__ __launch_bounds__(256) void wgrad_join_kernel(Wgrad a, FastDiv quads,
     finish4<O>(a, n, k, in, v);
 }
 
-// Column sums of dy over every bparts-th slab of 64 rows: 8 columns a lane, 4 wavefronts a workgroup.
+// Column sums of dy over each of bparts slabs of tokens: 8 columns a lane, 4 wavefronts a workgroup, 4 rows at a time.
 template <typename T>
 __global__ __launch_bounds__(256) void dy_sum_kernel(Wgrad a) {
     __shared__ float buf[3][64 * 8];
     const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
-    const int64_t c = ((int64_t)blockIdx.x * 64 + lane) * 8;
+    const int c = (blockIdx.x * 64 + lane) * 8, out = (int)a.out;
     float s[8] = {};
-    if (c < a.out) {
+    if (c < out) {
         const int64_t r0 = a.s.rows * blockIdx.y / a.bparts, r1 = a.s.rows * (blockIdx.y + 1) / a.bparts;
-        for (int64_t r = r0 + w; r < r1; r += 4) {
-            Chunk<T> k;
-            const T* const row = static_cast<const T*>(a.dy.p) + r * a.dy.ld + c;
-            load_chunk(k, row, 0, (int)std::min<int64_t>(8, a.out - c));
-            float v[8];
-            k.get(v);
+        for (int64_t r = r0 + w; r < r1; r += 16) {
+            Chunk<T> k[4];
 #pragma unroll
-            for (int j = 0; j < 8; ++j) s[j] += v[j];
+            for (int i = 0; i < 4; ++i) {
+                const int64_t t = r + 4 * i;
+                k[i].zero();
+                if (t < r1) load_chunk(k[i], static_cast<const T*>(a.dy.p) + t * a.dy.ld, c, out);
+            }
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                float v[8];
+                k[i].get(v);
+#pragma unroll
+                for (int j = 0; j < 8; ++j) s[j] += v[j];
+            }
         }
     }
     if (w > 0)
+#pragma unroll
         for (int j = 0; j < 8; ++j) buf[w - 1][j * 64 + lane] = s[j];
     __syncthreads();
-    if (w > 0 || c >= a.out) return;
-    for (int i = 0; i < 3; ++i)
-        for (int j = 0; j < 8; ++j) s[j] += buf[i][j * 64 + lane];
-    float* const p = a.bsum + a.out * (1 + (int64_t)blockIdx.y) + c;  // behind the whole sums
+    if (w > 0 || c >= out) return;
 #pragma unroll
-    for (int j = 0; j < 8; ++j)
-        if (c + j < a.out) p[j] = s[j];
+    for (int i = 0; i < 3; ++i)
+#pragma unroll
+        for (int j = 0; j < 8; ++j) s[j] += buf[i][j * 64 + lane];
+    store_chunk(a.bsum + a.out * (1 + (int64_t)blockIdx.y), c, out, s);  // behind the whole sums
 }
 
 template <typename T, typename O>
 hipError_t run(const Wgrad& a, hipStream_t st) {
     if (a.bsum) {
         dy_sum_kernel<T><<<dim3((uint32_t)((a.out + 511) / 512), (uint32_t)a.bparts), 256, 0, st>>>(a);
-        hipError_t e = launch_fold(AL_DTYPE_F32, a.bsum + a.out, a.bparts, a.out, a.bsum, st);
-        if (e == hipSuccess && a.dbias)
-            e = launch_fold(sizeof(O) == 2 ? AL_DTYPE_BF16 : AL_DTYPE_F32, a.bsum, 1, a.out, a.dbias, st);
+        const FoldOut out = {a.dbias, a.bsum};
+        const hipError_t e = launch_fold(sizeof(O) == 2 ? AL_DTYPE_BF16 : AL_DTYPE_F32, a.bsum + a.out, a.bparts, a.out, &out, 1, st);
         if (e != hipSuccess) return e;
     }
     if (a.s.cols == 0) return hipSuccess;
@@ -519,16 +525,38 @@ hipError_t run(const Wgrad& a, hipStream_t st) {
 
 }  // namespace
 
+// The tile and the splits over the tokens that a measured model of the time finds shortest (us, one MI355X, fitted to 52 cases
+// of both types, 1 to 16384 tokens and 64 x 64 to 11008 x 4096 outputs, each at every tile and up to 13 splits; its choices took 2%
+// longer on average than each case's best, 15% at most):
+//   a turn of a workgroup alone on its compute unit takes `alone`, of as many as fit beside each other `each` per workgroup, of
+//   64-wide ones `ragged` where rows of dy straddle cache lines; starting and ending take as long as `ends` turns;
+//   fp32 dy takes 3 turns for one, each 15% longer; joining takes a launch and the partial products' way out and back.
+// Measured: 8192 tokens, 11008 x 4096: 256-wide 666, 128-wide 844; 2048 x 2048: 256-wide 4 splits 98, 128-wide 2 splits 103; 1024 x
+// 1024: 128-wide 8 splits 46, 64-wide 6 splits 54; 512 tokens, 1024 x 1024: 64-wide 8, 128-wide 13, 64-wide 2 splits 16.
 WgradPlan wgrad_plan(int dtype, int64_t tokens, int64_t out, int64_t in) {
+    static constexpr struct {
+        int tile, fit, ends;
+        double alone, each, ragged;
+    } kinds[] = {{kEdge, 6, 2, 0.37, 0.11, 0.16}, {kMid, 3, 2, 0.44, 0.26, 0.26}, {kBig, 1, 4, 0.85, 0.85, 0.85}};
+    static constexpr int counts[] = {1, 2, 3, 4, 6, 8, 12, 16, 24, 32, 48, 64, 96, 128};
+    const int64_t steps = std::max<int64_t>(1, (tokens + kTurn - 1) / kTurn);
     WgradPlan p;
-    const int64_t steps = (tokens + kTurn - 1) / kTurn;
-    const auto tiles = [&](int64_t t) { return std::max<int64_t>(1, ((out + t - 1) / t) * ((in + t - 1) / t)); };
-    p.tile = std::min(out, in) < kMid ? kEdge : std::min(out, in) < kBig || tiles(kBig) < 100 ? kMid : kBig;
-    const int64_t n = tiles(p.tile), fill = p.tile == kBig ? 256 : 512;
-    // two workgroups for each of the 256 compute units, and at least 8 steps each
-    p.splits = (int32_t)std::max<int64_t>(1, std::min(fill / n, steps / 8));
+    double best = 0;
+    for (const auto& k : kinds) {
+        if (k.tile != kEdge && std::min(out, in) < k.tile) continue;
+        const int64_t n = std::max<int64_t>(1, ((out + k.tile - 1) / k.tile) * ((in + k.tile - 1) / k.tile));
+        const double each = out % 64 ? k.ragged : k.each;
+        for (const int s : counts) {
+            if (s > 1 && (2 * s > steps || n * s > 2048)) break;
+            const double load = (double)(n * s) / 256, whole = std::ceil(load),
+                         turns = (double)((steps + s - 1) / s) * (dtype == AL_DTYPE_BF16 ? 1 : 3.45) + k.ends,
+                         turn = k.fit == 1 ? each * whole : load > k.fit ? each * load : std::max(k.alone, each * whole),
+                         t = turns * turn + (s > 1 ? 2 + 0.02 * s + 0.6e-6 * 4 * s * (double)out * (double)in : 0);
+            if (best == 0 || t < best) best = t, p.tile = k.tile, p.splits = s;
+        }
+    }
     p.part_bytes = p.splits > 1 ? (size_t)p.splits * out * in * 4 : 0;
-    p.bparts = (int32_t)std::max<int64_t>(1, std::min<int64_t>(64, tokens / 64));
+    p.bparts = (int32_t)std::max<int64_t>(1, std::min<int64_t>(256, tokens / 32));
     p.bsum_bytes = (size_t)out * (p.bparts + 1) * 4;
     return p;
 }
