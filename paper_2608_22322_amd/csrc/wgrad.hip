@@ -27,7 +27,7 @@ typedef __attribute__((address_space(3))) uint16_t* lds_u16;
 // agree). Half a wavefront reads one 32-byte unit of each of 8 rows at once; the units of a row are exchanged so that
 // these lie in different banks.
 constexpr int kTurn = 32;  // tokens a turn
-constexpr int kEdge = 64;
+constexpr int kBig = 256, kMid = 128, kEdge = 64;  // tile widths
 
 __device__ __forceinline__ int edge_at(int t, int c) { return t * kEdge + ((((c >> 4) ^ ((t >> 1) & 3)) << 4) | (c & 15)); }
 
@@ -126,93 +126,6 @@ __device__ __forceinline__ void finish4(const Wgrad& a, int64_t n, int k, int in
     }
 }
 
-// A lane's four sums: into this split's partial products, or finished.
-template <typename O>
-__device__ __forceinline__ void write4(const Wgrad& a, int split, int64_t n, int k, int in, f32x4 v) {
-    if (in <= 0) return;
-    if (a.splits > 1) {
-        float* const p = a.part + ((int64_t)split * a.out + n) * a.s.cols + k;
-#pragma unroll
-        for (int r = 0; r < 4; ++r)
-            if (r < in) p[r] = v[r];
-    } else {
-        finish4<O>(a, n, k, in, v);
-    }
-}
-
-// 64 x 64 outputs, 4 wavefronts of 32 x 32, any size and alignment.
-template <typename T, typename O>
-__global__ __launch_bounds__(256) void wgrad_edge_kernel(Wgrad a) {
-    __shared__ __attribute__((aligned(16))) uint16_t dy_s[2][kTurn * kEdge], x_s[2][kTurn * kEdge];
-    constexpr int PARTS = sizeof(T) == 4 ? 3 : 1;
-    const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
-    const int64_t n0 = (int64_t)blockIdx.y * kEdge;
-    const int k0 = blockIdx.x * kEdge;
-    // this split's tokens
-    const int64_t steps = (a.s.rows + kTurn - 1) / kTurn;
-    const int64_t s0 = steps * blockIdx.z / a.splits, s1 = steps * (blockIdx.z + 1) / a.splits;
-
-    Chunk<T> dy;
-    u32x2 xq;
-    uint32_t xe;
-    const int cc = (tid & 7) * 8, t0 = tid >> 3;  // this thread's columns and token of a step
-    const auto load = [&](int64_t step) {
-        const int64_t t = step * kTurn + t0;
-        dy.zero();
-        xq = 0u;
-        xe = 0u;
-        if (t >= a.s.rows) return;
-        load_chunk(dy, static_cast<const T*>(a.dy.p) + t * a.dy.ld, (int)n0 + cc, (int)a.out);
-        if (k0 + cc < a.s.pitch) {
-            xq = *reinterpret_cast<const u32x2*>(a.c.p + t * a.s.pitch + k0 + cc);
-            xe = a.c.e[t * a.s.nb + ((k0 + cc) >> (3 + a.s.lb))];
-        }
-    };
-    const auto fragment = [&](const uint16_t* tile, int c0) {
-        const int t = 4 * (lane >> 4) + ((lane >> 2) & 3), c = c0 + 4 * (lane & 3);
-        return tile_fragment(tile, edge_at(t, c), edge_at(t + 16, c));
-    };
-    const int wn = (w >> 1) * 32, wk = (w & 1) * 32;
-    f32x4 acc[2][2] = {};
-    int b = 0;
-    if (s0 < s1) load(s0);
-    for (int64_t s = s0; s < s1; ++s) {
-        for (int part = 0; part < PARTS; ++part, b ^= 1) {
-            *reinterpret_cast<u32x4*>(&dy_s[b][edge_at(t0, cc)]) = as_bf16<T>(dy, part);
-            *reinterpret_cast<u32x4*>(&x_s[b][edge_at(t0, cc)]) = decode_bf16(xq, xe);
-            __syncthreads();
-            if (part == PARTS - 1 && s + 1 < s1) load(s + 1);
-            bf16x8 fx[2], fy[2];
-#pragma unroll
-            for (int i = 0; i < 2; ++i) {
-                fx[i] = fragment(x_s[b], wk + 16 * i);
-                fy[i] = fragment(dy_s[b], wn + 16 * i);
-            }
-#pragma unroll
-            for (int i = 0; i < 2; ++i)
-#pragma unroll
-                for (int j = 0; j < 2; ++j)
-                    acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fx[j], fy[i], acc[i][j], 0, 0, 0);
-        }
-    }
-    // lane: row n = l % 16, columns k = 4 (l / 16) + 0..3
-#pragma unroll
-    for (int i = 0; i < 2; ++i) {
-        const int64_t n = n0 + wn + 16 * i + (lane & 15);
-        if (n >= a.out) continue;
-#pragma unroll
-        for (int j = 0; j < 2; ++j) {
-            const int k = k0 + wk + 16 * j + 4 * (lane >> 4);
-            write4<O>(a, blockIdx.z, n, k, std::min(4, a.s.cols - k), acc[i][j]);
-        }
-    }
-}
-
-// B x B outputs, for out_features and in_features of at least B: the last tile of a side is moved back to end with it, so that no
-// load needs a bounds check, and leaves what the tile before it has written. B = 256: 8 wavefronts of 128 x 64 (2 along n, 4 along
-// k), one workgroup per compute unit; B = 128: 4 wavefronts of 64 x 64, up to four.
-constexpr int kBig = 256, kMid = 128;
-
 // The shape of the products, M x M. 16 x 16 x 32 takes more cycles than 32 x 32 x 16 and keeps a higher clock (8192 tokens and
 // features: 1.85M cycles at 2.13 GHz against 1.74M at 1.92 GHz), so bf16 dy takes it; fp32 dy, whose staging needs the
 // registers that fewer fragments in flight leave, takes 32 x 32 x 16 (4096^3: 842 and 400 us).
@@ -248,6 +161,161 @@ struct Product<32> {
     }
 };
 
+// A B x B tile's outputs: wavefront w holds rows WN (w / (B / WK)) .., columns WK (w % (B / WK)) .. as FN x FK blocks of M x M, a lane
+// four consecutive columns of one row in each of a block's quads.
+template <int B, int M>
+struct Tile {
+    static constexpr int WN = B / 2, WK = B == kEdge ? 32 : 64, FN = WN / M, FK = WK / M, kQuads = Product<M>::kQuads,
+                         kWaves = (B / WN) * (B / WK), kSlots = FN * FK * kQuads;
+    int n_first, n0, k_first, k0;  // what the tile is answerable for begins at n_first, k_first; its first output is n0, k0
+    __device__ __forceinline__ Tile(const Wgrad& a, int n, int k) {
+        n_first = n0 = n * B;
+        k_first = k0 = k * B;
+        if (B != kEdge) n0 = std::min(n0, (int)a.out - B), k0 = std::min(k0, a.s.pitch - B);
+    }
+    static __device__ __forceinline__ int wave_n(int w) { return w / (B / WK) * WN; }
+    static __device__ __forceinline__ int wave_k(int w) { return w % (B / WK) * WK; }
+    // row, first column and number of columns of a lane's quad (0: none of this tile's)
+    __device__ __forceinline__ int quad(const Wgrad& a, int w, int i, int j, int q, int lane, int& n, int& k) const {
+        n = n0 + wave_n(w) + M * i + (lane & (M - 1));
+        k = k0 + wave_k(w) + M * j + Product<M>::quad(lane, q);
+        return n < n_first || n >= a.out || k < k_first ? 0 : std::min(4, a.s.cols - k);
+    }
+};
+
+// The sums of a workgroup's tile: finished, or, where the tokens are split, as partial products in the order in which the lanes hold
+// them (whole lines; the outputs' own order takes 16-byte pieces and 3 times as long): [split][tile][wavefront][slot][lane].
+template <typename O, int B, int M, typename ACC>
+__device__ __forceinline__ void write_tile(const Wgrad& a, const Tile<B, M>& t, int64_t tile, int64_t tiles, int split, int w, int lane,
+                                           const ACC& acc) {
+    typedef Tile<B, M> G;
+    f32x4* const part = reinterpret_cast<f32x4*>(a.part) + ((split * tiles + tile) * G::kWaves + w) * G::kSlots * 64 + lane;
+    // (One row of blocks at a time: with all their loads in flight at once the sums would not stay in registers.)
+#pragma unroll
+    for (int i = 0; i < G::FN; ++i) {
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int j = 0; j < G::FK; ++j) {
+#pragma unroll
+            for (int q = 0; q < G::kQuads; ++q) {
+                f32x4 v;
+#pragma unroll
+                for (int r = 0; r < 4; ++r) v[r] = acc[i][j][4 * q + r];
+                if (a.splits > 1) {
+                    part[((i * G::FK + j) * G::kQuads + q) * 64] = v;
+                } else {
+                    int n, k;
+                    const int in = t.quad(a, w, i, j, q, lane, n, k);
+                    if (in > 0) finish4<O>(a, n, k, in, v);
+                }
+            }
+        }
+    }
+}
+
+// The splits' partial products, added in order, 8 splits' loads in flight.
+template <typename O, int B, int M>
+__global__ __launch_bounds__(256) void wgrad_join_kernel(Wgrad a, FastDiv kt, uint32_t tiles) {
+    typedef Tile<B, M> G;
+    constexpr uint32_t kBlocks = B * B / 1024;  // workgroups a tile
+    const uint32_t id = xcd_block(), tile = id / kBlocks, at = id % kBlocks * 256 + threadIdx.x, lane = at & 63, slot = at >> 6;
+    const int64_t size = (int64_t)tiles * (B * B / 4);
+    const f32x4* p = reinterpret_cast<const f32x4*>(a.part) + (int64_t)tile * (B * B / 4) + at;
+    f32x4 v = {};
+    int s = 0;
+    for (; s + 8 <= a.splits; s += 8, p += 8 * size) {
+        f32x4 t[8];
+#pragma unroll
+        for (int r = 0; r < 8; ++r) t[r] = p[r * size];
+#pragma unroll
+        for (int r = 0; r < 8; ++r) v += t[r];
+    }
+    for (; s < a.splits; ++s, p += size) v += *p;
+    const int w = slot / G::kSlots, e = slot % G::kSlots, tn = (int)quotient(tile, kt);
+    int n, k;
+    const int in = G(a, tn, (int)(tile - (uint32_t)tn * kt.d))
+                       .quad(a, w, e / (G::FK * G::kQuads), e / G::kQuads % G::FK, e % G::kQuads, (int)lane, n, k);
+    if (in > 0) finish4<O>(a, n, k, in, v);
+}
+
+// 64 x 64 outputs, 4 wavefronts of 32 x 32, any size and alignment. A turn is short here, so the loads of AHEAD of them are
+// in flight. Loads are never masked: rows past the last are the last one's and columns past a side's end its last ones, of which
+// the former are cleared on the way to LDS and the latter make sums that are not written.
+template <typename T, typename O>
+__global__ __launch_bounds__(256) void wgrad_edge_kernel(Wgrad a) {
+    __shared__ __attribute__((aligned(16))) uint16_t dy_s[2][kTurn * kEdge], x_s[2][kTurn * kEdge];
+    constexpr int PARTS = sizeof(T) == 4 ? 3 : 1, AHEAD = 4;
+    const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
+    const int64_t n0 = (int64_t)blockIdx.y * kEdge;
+    const int k0 = blockIdx.x * kEdge;
+    // this split's tokens
+    const int64_t steps = (a.s.rows + kTurn - 1) / kTurn;
+    const int64_t s0 = steps * blockIdx.z / a.splits, s1 = steps * (blockIdx.z + 1) / a.splits;
+
+    const int cc = (tid & 7) * 8, t0 = tid >> 3;  // this thread's columns and token of a step
+    const int out = (int)a.out, c = (int)n0 + cc, from = std::max(0, std::min(c, out - 8)), shift = std::min(c - from, 8);
+    const int xc = std::min(k0 + cc, a.s.pitch - 8);
+    const T* const dyp = static_cast<const T*>(a.dy.p) + from;
+    Chunk<T> dy[AHEAD];
+    u32x2 xq[AHEAD];
+    uint32_t xe[AHEAD];
+    const auto load = [&](int i, int64_t step) __attribute__((always_inline)) {
+        const int64_t t = std::min(step * kTurn + t0, a.s.rows - 1);
+        if (out >= 8)
+            dy[i].load(dyp + t * a.dy.ld);
+        else
+            dy[i].load(dyp + t * a.dy.ld, out);
+        xq[i] = *reinterpret_cast<const u32x2*>(a.c.p + t * a.s.pitch + xc);
+        xe[i] = a.c.e[t * a.s.nb + (xc >> (3 + a.s.lb))];
+    };
+    const auto fragment = [&](const uint16_t* tile, int c0) __attribute__((always_inline)) {
+        const int t = 4 * (lane >> 4) + ((lane >> 2) & 3), f = c0 + 4 * (lane & 3);
+        return tile_fragment(tile, edge_at(t, f), edge_at(t + 16, f));
+    };
+    const int wn = Tile<kEdge, 16>::wave_n(w), wk = Tile<kEdge, 16>::wave_k(w);
+    f32x4 acc[2][2] = {};
+    int b = 0;
+#pragma unroll
+    for (int i = 0; i < AHEAD; ++i)
+        if (s0 + i < s1) load(i, s0 + i);
+    for (int64_t s = s0; s < s1; s += AHEAD) {
+#pragma unroll
+        for (int i = 0; i < AHEAD; ++i) {
+            if (s + i >= s1) break;
+            if (shift > 0 && out >= 8) dy[i].drop(shift & 7);
+            if ((s + i) * kTurn + t0 >= a.s.rows) {
+                dy[i].zero();
+                xq[i] = 0u;
+                xe[i] = 0u;
+            }
+#pragma unroll
+            for (int part = 0; part < PARTS; ++part, b ^= 1) {
+                *reinterpret_cast<u32x4*>(&dy_s[b][edge_at(t0, cc)]) = as_bf16<T>(dy[i], part);
+                *reinterpret_cast<u32x4*>(&x_s[b][edge_at(t0, cc)]) = decode_bf16(xq[i], xe[i]);
+                if (part == PARTS - 1 && s + i + AHEAD < s1) load(i, s + i + AHEAD);
+                __syncthreads();
+                bf16x8 fx[2], fy[2];
+#pragma unroll
+                for (int r = 0; r < 2; ++r) {
+                    fx[r] = fragment(x_s[b], wk + 16 * r);
+                    fy[r] = fragment(dy_s[b], wn + 16 * r);
+                }
+#pragma unroll
+                for (int r = 0; r < 2; ++r)
+#pragma unroll
+                    for (int j = 0; j < 2; ++j)
+                        acc[r][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fx[j], fy[r], acc[r][j], 0, 0, 0);
+            }
+        }
+    }
+    write_tile<O>(a, Tile<kEdge, 16>(a, blockIdx.y, blockIdx.x), (int64_t)blockIdx.y * gridDim.x + blockIdx.x, (int64_t)gridDim.x * gridDim.y,
+                  blockIdx.z, w, lane, acc);
+}
+
+// B x B outputs, for out_features and in_features of at least B: the last tile of a side is moved back to end with it, so that no
+// load needs a bounds check, and leaves what the tile before it has written. B = 256: 8 wavefronts of 128 x 64 (2 along n, 4 along
+// k), one workgroup per compute unit; B = 128: 4 wavefronts of 64 x 64, up to four.
+
 template <int B, int M>
 __device__ __forceinline__ int tile_at(int t, int c) {
     return t * B + ((((c >> 4) ^ (Product<M>::swizzle(t) & (B / 16 - 1))) << 4) | (c & 15));
@@ -270,12 +338,13 @@ __device__ __forceinline__ TileId tile_id(const Wgrad& a) {
 template <typename T, typename O, int B>
 __global__ __launch_bounds__(2 * B, B == kBig ? 2 : 3) void wgrad_tile_kernel(Wgrad a) {
     constexpr int PARTS = sizeof(T) == 4 ? 3 : 1, BT = kTurn, C = BT / 16;
-    constexpr int WN = B / 2, WK = 64, M = PARTS == 1 ? 16 : 32, FN = WN / M, FK = WK / M, H = BT / Product<M>::kTokens;
+    constexpr int M = PARTS == 1 ? 16 : 32, FN = Tile<B, M>::FN, FK = Tile<B, M>::FK, H = BT / Product<M>::kTokens;
     __shared__ __attribute__((aligned(16))) uint16_t dy_s[2][BT * B], x_s[2][BT * B];
     const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
     const TileId tile = tile_id<B>(a);
-    const int64_t n_first = (int64_t)tile.n * B, n0 = std::min(n_first, a.out - B);
-    const int k_first = tile.k * B, k0 = std::min(k_first, a.s.pitch - B);
+    typedef Tile<B, PARTS == 1 ? 16 : 32> G;
+    const G t(a, tile.n, tile.k);
+    const int n0 = t.n0, k0 = t.k0;
     const int64_t steps = (a.s.rows + BT - 1) / BT;
     const int64_t s0 = steps * tile.split / a.splits, s1 = steps * (tile.split + 1) / a.splits;
 
@@ -287,10 +356,10 @@ __global__ __launch_bounds__(2 * B, B == kBig ? 2 : 3) void wgrad_tile_kernel(Wg
         const int last = (int)std::min<int64_t>(a.s.rows - 1 - step * BT, BT - 1);
 #pragma unroll
         for (int i = 0; i < C; ++i) {
-            const uint32_t t = (uint32_t)std::min(t0 + 16 * i, last);
-            od[i] = (t * (uint32_t)a.dy.ld + (uint32_t)cc) * (uint32_t)sizeof(T);
-            ox[i] = t * (uint32_t)a.s.pitch + (uint32_t)cc;
-            oe[i] = t * (uint32_t)a.s.nb + ((uint32_t)(k0 + cc) >> (3 + a.s.lb));
+            const uint32_t row = (uint32_t)std::min(t0 + 16 * i, last);
+            od[i] = (row * (uint32_t)a.dy.ld + (uint32_t)cc) * (uint32_t)sizeof(T);
+            ox[i] = row * (uint32_t)a.s.pitch + (uint32_t)cc;
+            oe[i] = row * (uint32_t)a.s.nb + ((uint32_t)(k0 + cc) >> (3 + a.s.lb));
         }
     };
     Chunk<T> dy[C];
@@ -331,7 +400,7 @@ __global__ __launch_bounds__(2 * B, B == kBig ? 2 : 3) void wgrad_tile_kernel(Wg
         }
     };
 
-    const int wn = w / (B / WK) * WN, wk = w % (B / WK) * WK, ft = Product<M>::token(lane), fc = Product<M>::column(lane);
+    const int wn = G::wave_n(w), wk = G::wave_k(w), ft = Product<M>::token(lane), fc = Product<M>::column(lane);
     int ay[FN][2], ax[FK][2];  // a fragment's two reads
 #pragma unroll
     for (int r = 0; r < 2; ++r) {
@@ -407,57 +476,8 @@ __global__ __launch_bounds__(2 * B, B == kBig ? 2 : 3) void wgrad_tile_kernel(Wg
     int64_t s = s0;
     for (; s + 3 < whole_end; s += 2) trip(s, std::true_type{});
     for (; s < s1; s += 2) trip(s, std::false_type{});
-    // lane: row n = l % M, four columns k a quad. (One row of blocks at a time: with all their loads in flight at once the
-    // sums would not stay in registers.)
-#pragma unroll
-    for (int i = 0; i < FN; ++i) {
-        __builtin_amdgcn_sched_barrier(0);
-        const int64_t n = n0 + wn + M * i + (lane & (M - 1));
-        if (n < n_first) continue;
-#pragma unroll
-        for (int j = 0; j < FK; ++j) {
-#pragma unroll
-            for (int q = 0; q < Product<M>::kQuads; ++q) {
-                const int k = k0 + wk + M * j + Product<M>::quad(lane, q), in = std::min(4, a.s.cols - k);
-                if (k < k_first) continue;
-                f32x4 v;
-#pragma unroll
-                for (int r = 0; r < 4; ++r) v[r] = acc[i][j][4 * q + r];
-                write4<O>(a, tile.split, n, k, in, v);
-            }
-        }
-    }
-}
-
-// The splits' partial products, added in order: four columns a lane, up to 8 splits' loads in flight.
-template <typename O>
-__global__ __launch_bounds__(256) void wgrad_join_kernel(Wgrad a, FastDiv quads, uint32_t total) {
-    const uint32_t i = xcd_block() * 256 + threadIdx.x;
-    if (i >= total) return;
-    const uint32_t n = quotient(i, quads);
-    const int k = (int)(i - n * quads.d) * 4, in = std::min(4, a.s.cols - k);
-    const int64_t size = a.out * a.s.cols;
-    const float* p = a.part + (int64_t)n * a.s.cols + k;
-    typedef float f32x4_a4 __attribute__((ext_vector_type(4), aligned(4)));
-    f32x4 v = {};
-    if (in == 4) {
-        int s = 0;
-        for (; s + 8 <= a.splits; s += 8) {
-            f32x4 t[8];
-#pragma unroll
-            for (int r = 0; r < 8; ++r) t[r] = *reinterpret_cast<const f32x4_a4*>(p + r * size);
-            p += 8 * size;
-#pragma unroll
-            for (int r = 0; r < 8; ++r) v += t[r];
-        }
-        for (; s < a.splits; ++s, p += size) v += *reinterpret_cast<const f32x4_a4*>(p);
-    } else {
-        for (int s = 0; s < a.splits; ++s, p += size)
-#pragma unroll
-            for (int r = 0; r < 3; ++r)
-                if (r < in) v[r] += p[r];
-    }
-    finish4<O>(a, n, k, in, v);
+    const int64_t kt = (a.s.cols + B - 1) / B;
+    write_tile<O>(a, t, tile.n * kt + tile.k, kt * ((a.out + B - 1) / B), tile.split, w, lane, acc);
 }
 
 // Column sums of dy over each of bparts slabs of tokens: 8 columns a lane, 4 wavefronts a workgroup, 4 rows at a time.
@@ -498,6 +518,15 @@ __global__ __launch_bounds__(256) void dy_sum_kernel(Wgrad a) {
     store_chunk(a.bsum + a.out * (1 + (int64_t)blockIdx.y), c, out, s);  // behind the whole sums
 }
 
+template <typename T, typename O, int B>
+hipError_t launch_tile(const Wgrad& a, hipStream_t st) {
+    const uint32_t kt = (uint32_t)((a.s.cols + B - 1) / B), tiles = kt * (uint32_t)((a.out + B - 1) / B);
+    wgrad_tile_kernel<T, O, B><<<tiles * (uint32_t)a.splits, 2 * B, 0, st>>>(a);
+    if (a.splits > 1)
+        wgrad_join_kernel<O, B, sizeof(T) == 2 ? 16 : 32><<<tiles * (B * B / 1024), 256, 0, st>>>(a, fast_div(kt), tiles);
+    return hipGetLastError();
+}
+
 template <typename T, typename O>
 hipError_t run(const Wgrad& a, hipStream_t st) {
     if (a.bsum) {
@@ -507,18 +536,14 @@ hipError_t run(const Wgrad& a, hipStream_t st) {
         if (e != hipSuccess) return e;
     }
     if (a.s.cols == 0) return hipSuccess;
-    // the large tiles' 32-bit offsets span 32 rows
-    const int tile = a.dy.ld < (1 << 25) && a.s.pitch < (1 << 26) ? a.tile : kEdge;
-    const dim3 n((uint32_t)((a.s.cols + tile - 1) / tile), (uint32_t)((a.out + tile - 1) / tile), (uint32_t)a.splits);
-    if (tile == kBig)
-        wgrad_tile_kernel<T, O, kBig><<<n.x * n.y * n.z, 2 * kBig, 0, st>>>(a);
-    else if (tile == kMid)
-        wgrad_tile_kernel<T, O, kMid><<<n.x * n.y * n.z, 2 * kMid, 0, st>>>(a);
-    else
-        wgrad_edge_kernel<T, O><<<n, 256, 0, st>>>(a);
+    // a plan's partial products have the layout of its tile; the large tiles' 32-bit offsets span 32 rows
+    if (a.tile != kEdge && a.dy.ld < (1 << 25) && a.s.pitch < (1 << 26))
+        return a.tile == kBig ? launch_tile<T, O, kBig>(a, st) : launch_tile<T, O, kMid>(a, st);
+    const dim3 n((uint32_t)((a.s.cols + kEdge - 1) / kEdge), (uint32_t)((a.out + kEdge - 1) / kEdge), (uint32_t)a.splits);
+    wgrad_edge_kernel<T, O><<<n, 256, 0, st>>>(a);
     if (a.splits > 1) {
-        const uint32_t quads = (uint32_t)((a.s.cols + 3) / 4), total = (uint32_t)a.out * quads;
-        wgrad_join_kernel<O><<<(total + 255) / 256, 256, 0, st>>>(a, fast_div(quads), total);
+        const uint32_t tiles = n.x * n.y;
+        wgrad_join_kernel<O, kEdge, 16><<<tiles * (kEdge * kEdge / 1024), 256, 0, st>>>(a, fast_div(n.x), tiles);
     }
     return hipGetLastError();
 }
@@ -527,17 +552,18 @@ hipError_t run(const Wgrad& a, hipStream_t st) {
 
 // The tile and the splits over the tokens that a measured model of the time finds shortest (us, one MI355X, fitted to 52 cases
 // of both types, 1 to 16384 tokens and 64 x 64 to 11008 x 4096 outputs, each at every tile and up to 13 splits; its choices took 2%
-// longer on average than each case's best, 15% at most):
-//   a turn of a workgroup alone on its compute unit takes `alone`, of as many as fit beside each other `each` per workgroup, of
-//   64-wide ones `ragged` where rows of dy straddle cache lines; starting and ending take as long as `ends` turns;
-//   fp32 dy takes 3 turns for one, each 15% longer; joining takes a launch and the partial products' way out and back.
-// Measured: 8192 tokens, 11008 x 4096: 256-wide 666, 128-wide 844; 2048 x 2048: 256-wide 4 splits 98, 128-wide 2 splits 103; 1024 x
-// 1024: 128-wide 8 splits 46, 64-wide 6 splits 54; 512 tokens, 1024 x 1024: 64-wide 8, 128-wide 13, 64-wide 2 splits 16.
+// longer on average than each case's best, 16% at most):
+//   a turn of a workgroup alone on its compute unit takes `alone`, of as many as fit beside each other `each` per workgroup;
+//   starting and ending take as long as `ends` turns; fp32 dy takes 3 turns for one, each 10% longer; joining takes a launch
+//   and the partial products' way out and back.
+// Measured: 8192 tokens, 11008 x 4096: 256-wide 651, 128-wide 854; 2048 x 2048: 256-wide 4 splits 78, 128-wide 3 splits 93; 1024 x
+// 1024: 128-wide 8 splits 35, 256-wide 12 splits 37; 6001 tokens, 256 x 2048: 64-wide 8 splits 24, 128-wide 12 splits 27; 512 tokens,
+// 1024 x 1024: 64-wide 9, 128-wide 13, 64-wide 2 splits 13.
 WgradPlan wgrad_plan(int dtype, int64_t tokens, int64_t out, int64_t in) {
     static constexpr struct {
         int tile, fit, ends;
-        double alone, each, ragged;
-    } kinds[] = {{kEdge, 6, 2, 0.37, 0.11, 0.16}, {kMid, 3, 2, 0.44, 0.26, 0.26}, {kBig, 1, 4, 0.85, 0.85, 0.85}};
+        double alone, each;
+    } kinds[] = {{kEdge, 6, 1, 0.37, 0.13}, {kMid, 3, 2, 0.44, 0.28}, {kBig, 1, 6, 0.8, 0.8}};
     static constexpr int counts[] = {1, 2, 3, 4, 6, 8, 12, 16, 24, 32, 48, 64, 96, 128};
     const int64_t steps = std::max<int64_t>(1, (tokens + kTurn - 1) / kTurn);
     WgradPlan p;
@@ -545,17 +571,15 @@ WgradPlan wgrad_plan(int dtype, int64_t tokens, int64_t out, int64_t in) {
     for (const auto& k : kinds) {
         if (k.tile != kEdge && std::min(out, in) < k.tile) continue;
         const int64_t n = std::max<int64_t>(1, ((out + k.tile - 1) / k.tile) * ((in + k.tile - 1) / k.tile));
-        const double each = out % 64 ? k.ragged : k.each;
         for (const int s : counts) {
             if (s > 1 && (2 * s > steps || n * s > 2048)) break;
             const double load = (double)(n * s) / 256, whole = std::ceil(load),
-                         turns = (double)((steps + s - 1) / s) * (dtype == AL_DTYPE_BF16 ? 1 : 3.45) + k.ends,
-                         turn = k.fit == 1 ? each * whole : load > k.fit ? each * load : std::max(k.alone, each * whole),
-                         t = turns * turn + (s > 1 ? 2 + 0.02 * s + 0.6e-6 * 4 * s * (double)out * (double)in : 0);
-            if (best == 0 || t < best) best = t, p.tile = k.tile, p.splits = s;
+                         turns = (double)((steps + s - 1) / s) * (dtype == AL_DTYPE_BF16 ? 1 : 3.3) + k.ends,
+                         turn = k.fit == 1 ? k.each * whole : load > k.fit ? k.each * load : std::max(k.alone, k.each * whole),
+                         t = turns * turn + (s > 1 ? 2 + 0.02 * s + 0.34e-6 * 4 * s * (double)out * (double)in : 0);
+            if (best == 0 || t < best) best = t, p.tile = k.tile, p.splits = s, p.part_bytes = s > 1 ? (size_t)(s * n) * k.tile * k.tile * 4 : 0;
         }
     }
-    p.part_bytes = p.splits > 1 ? (size_t)p.splits * out * in * 4 : 0;
     p.bparts = (int32_t)std::max<int64_t>(1, std::min<int64_t>(256, tokens / 32));
     p.bsum_bytes = (size_t)out * (p.bparts + 1) * 4;
     return p;
