@@ -362,7 +362,7 @@ al_status al_act_dequantize(const void* codes, const void* exps, int64_t rows, i
  * biased variance about the mean (AL_NORM_RMS: mean = 0, var = the mean
  * square), y = xhat gamma + beta. gamma, beta: cols floats, NULL = 1 and 0;
  * beta only for AL_NORM_LAYER. x and y have dtype; y may be x itself (same
- * ld). mean (AL_NORM_LAYER only, else NULL) and rstd: rows floats, NULL where not
+ * ld). eps >= 0; a row without variance needs eps > 0. mean (AL_NORM_LAYER only, else NULL) and rstd: rows floats, NULL where not
  * wanted. codes, exps: the E8 code of xhat, both NULL where it is not saved
  * (block is then ignored). xhat is what a backward pass needs of x, and a
  * linear layer that reads y needs nothing else either (al_linear_wgrad). */
@@ -370,7 +370,8 @@ al_status al_norm_forward(int32_t kind, int32_t dtype, const void* x, int64_t ld
                           double eps, const float* gamma, const float* beta, void* y, int64_t ldy, float* mean,
                           float* rstd, int32_t block, void* codes, void* exps, void* stream);
 
-/* Workspace bytes of al_norm_backward: partial sums of the weight gradients (0 if neither is asked for). */
+/* Workspace bytes of an al_norm_backward that is asked for dgamma or dbeta:
+ * partial sums of the weight gradients. */
 al_status al_norm_backward_workspace_bytes(int32_t kind, int32_t dtype, int64_t rows, int64_t cols, size_t* bytes);
 
 /* Backward pass of al_norm_forward. With a = dy gamma and n = cols,
@@ -418,7 +419,10 @@ al_status al_linear_wgrad_workspace_bytes(int32_t dtype, int64_t tokens, int64_t
  * out_features x in_features of grad_dtype; base NULL = 0, base may be dw
  * itself (gradient accumulation). dbias: out_features values of grad_dtype or
  * NULL. The products are exact (both factors are bf16 numbers, an fp32 dy is three
- * of them) and summed in fp32 on the matrix cores. tokens == 0: dw = base, dbias = 0. */
+ * of them) and summed in fp32 on the matrix cores. tokens == 0: dw = base, dbias = 0.
+ * out_features below 2^22, in_features below 2^29 (AL_EUNSUPPORTED otherwise).
+ * One launch where the outputs fill the device; fewer outputs split the tokens,
+ * and a second launch adds the parts in order; beta or dbias take two more. */
 al_status al_linear_wgrad(int32_t dtype, const void* dy, int64_t lddy, const void* codes, const void* exps,
                           int32_t block, int64_t tokens, int64_t out_features, int64_t in_features,
                           const float* gamma, const float* beta, int32_t grad_dtype, const void* base, void* dw,

@@ -95,6 +95,13 @@ al_status check_kind(int32_t kind, const char* who) {
     return AL_OK;
 }
 
+// The grids of the products hold these.
+al_status check_product(int64_t out, int64_t in, const char* who) {
+    if (out >= (int64_t(1) << 22) || in >= (int64_t(1) << 29))
+        return fail(AL_EUNSUPPORTED, "%s: %lld out_features (below 2^22) or %lld in_features (below 2^29)", who, (long long)out, (long long)in);
+    return AL_OK;
+}
+
 size_t norm_ws(int32_t kind, int64_t rows, int64_t cols) {
     const bool layer = kind == AL_NORM_LAYER;
     return align256((size_t)al::norm_backward_parts(rows, cols) * cols * 4 * (layer ? 2 : 1));
@@ -303,6 +310,7 @@ al_status al_linear_wgrad_workspace_bytes(int32_t dtype, int64_t tokens, int64_t
     AL_TRY(check_dtype(dtype, who, "dtype"));
     AL_TRY(check_shape(tokens, in_features, who));
     AL_TRY(check_shape(tokens, out_features, who));
+    AL_TRY(check_product(out_features, in_features, who));
     const al::WgradPlan p = al::wgrad_plan(dtype, tokens, out_features, in_features);
     *bytes = align256(p.part_bytes) + align256(p.bsum_bytes);
     return AL_OK;
@@ -319,7 +327,7 @@ al_status al_linear_wgrad(int32_t dtype, const void* dy, int64_t lddy, const voi
     AL_TRY(check_shape(tokens, in_features, who));
     AL_TRY(check_shape(tokens, out_features, who));
     AL_TRY(check_block(block, who));
-    if (out_features >= (int64_t(1) << 22)) return fail(AL_EUNSUPPORTED, "%s: 2^22 out_features or more", who);
+    AL_TRY(check_product(out_features, in_features, who));
     if (out_features == 0) return AL_OK;
     if (in_features > 0) {
         if (!dw) return fail(AL_EINVAL, "%s: dw is NULL", who);

@@ -3,7 +3,9 @@
 //
 // Both factors are bf16 numbers (a code is 7 bits and a sign times a power of two; an
 // fp32 dy is the sum of three bf16 numbers, taken in three turns), so every
-// product is exact and the sums are the matrix cores' fp32 ones.
+// product is exact and the sums are the matrix cores' fp32 ones. A workgroup
+// decodes each code once, on its way to LDS (2.5 instructions a value: convert a
+// byte, multiply, pack; the fragments' readers would do it twice or four times).
 #include <algorithm>
 #include <cmath>
 #include <type_traits>
@@ -312,10 +314,6 @@ __global__ __launch_bounds__(256) void wgrad_edge_kernel(Wgrad a) {
                   blockIdx.z, w, lane, acc);
 }
 
-// B x B outputs, for out_features and in_features of at least B: the last tile of a side is moved back to end with it, so that no
-// load needs a bounds check, and leaves what the tile before it has written. B = 256: 8 wavefronts of 128 x 64 (2 along n, 4 along
-// k), one workgroup per compute unit; B = 128: 4 wavefronts of 64 x 64, up to four.
-
 template <int B, int M>
 __device__ __forceinline__ int tile_at(int t, int c) {
     return t * B + ((((c >> 4) ^ (Product<M>::swizzle(t) & (B / 16 - 1))) << 4) | (c & 15));
@@ -335,6 +333,15 @@ __device__ __forceinline__ TileId tile_id(const Wgrad& a) {
     return {(int)(band * kBand + q - k * rows), (int)k, (int)split};
 }
 
+// B x B outputs, for out_features and in_features of at least B: the last tile of a side is moved back to end with it, so that no
+// load needs a bounds check, and leaves what the tile before it has written. B = 256: 8 wavefronts of 128 x 64 (2 along n, 4 along
+// k), one workgroup per compute unit; B = 128: 4 wavefronts of 64 x 64, up to three.
+//
+// 8192^3 bf16: 905 us, 1.21 PFLOP/s (a library product of bf16 matrices in these orders: 1.15; 1.27 in its best order). The matrix
+// units are busy 57% of the cycles at 2.13 GHz; 100% of them at the nominal 2.4 would be 2.5 PFLOP/s. Of the rest a part is
+// power: the same products in fewer cycles (32 x 32 x 16, 60%) ran at 1.92 GHz and took longer. What got it there, us for 8192 tokens,
+// 11008 x 4096: 128 x 128 tiles 1045; 256 x 256 with the next tiles staged beside the products 819; offsets from scalar bases and
+// no branches in the turns 780; fragments two ahead and the decoding between matrix instructions 683; bands per XCD 670.
 template <typename T, typename O, int B>
 __global__ __launch_bounds__(2 * B, B == kBig ? 2 : 3) void wgrad_tile_kernel(Wgrad a) {
     constexpr int PARTS = sizeof(T) == 4 ? 3 : 1, BT = kTurn, C = BT / 16;

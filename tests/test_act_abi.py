@@ -127,3 +127,14 @@ def test_wgrad_refusals():
     assert w(dy=A + 1) == 2 and w(gamma=A + 1) == 2 and w(db=A + 2) == 2
     assert w(out=(1 << 22) + 1, ld=1 << 23) == 4
     assert w(out=0) == 0
+
+
+def test_wgrad_sizes_past_the_grids():
+    need = ctypes.c_size_t(0)
+    for out, cols, want in ((1 << 22, 8, 4), ((1 << 22) - 1, 8, 0), (8, 1 << 29, 4), (8, (1 << 29) - 1, 0)):
+        assert _status("al_linear_wgrad_workspace_bytes", 1, 64, out, cols, ctypes.byref(need)) == want
+    # splits only where outputs are few: the workspace of a large product is the bias sums alone
+    assert _status("al_linear_wgrad_workspace_bytes", 1, 8192, 11008, 4096, ctypes.byref(need)) == 0
+    assert need.value <= 11008 * 4 * 257 + 256
+    assert _status("al_linear_wgrad_workspace_bytes", 1, 8192, 256, 256, ctypes.byref(need)) == 0
+    assert need.value <= 64 << 20

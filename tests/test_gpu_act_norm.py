@@ -282,3 +282,25 @@ def test_refusals():
         act.norm_backward(act.LAYER, x, y, None, r, torch.empty_like(x))
     with pytest.raises(al.ALError):  # in place over dy
         act.norm_backward(act.RMS, x, y, None, r, x)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("cols", [513, 1025, 4097, 12289, 16385, 16901, 24577])
+def test_in_place_where_a_row_ends_in_another_wavefront(cols, dtype):
+    """The chunk that a row ends in belongs to another wavefront than the one before it: y over x, dx over add."""
+    from paper_2608_22322_amd import activations as act
+
+    rows = 33
+    x, gamma, _ = _inputs(rows, cols, dtype, cols)
+    d, apart, rstd, gd = x.cuda(), torch.empty(rows, cols, dtype=DT[dtype], device="cuda"), torch.empty(rows, device="cuda"), gamma.cuda()
+    act.norm_forward(act.RMS, d, apart, rstd=rstd, gamma=gd)
+    dy, add = torch.randn(rows, cols).to(DT[dtype]).cuda(), torch.randn(rows, cols).to(DT[dtype]).cuda()
+    want = torch.empty_like(add)
+    act.norm_backward(act.RMS, dy, d, None, rstd, want, gamma=gd, add=add)
+    for _ in range(5):
+        over = add.clone()
+        act.norm_backward(act.RMS, dy, d, None, rstd, over, gamma=gd, add=over)
+        assert torch.equal(over, want)
+        y = d.clone()
+        act.norm_forward(act.RMS, y, y, gamma=gd)
+        assert torch.equal(y, apart)
