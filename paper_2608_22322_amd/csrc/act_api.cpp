@@ -356,6 +356,7 @@ al_status al_linear_wgrad(int32_t dtype, const void* dy, int64_t lddy, const voi
     a.tile = p.tile;
     a.splits = p.splits;
     a.bparts = p.bparts;
+    a.beside = p.beside;
     a.part = static_cast<float*>(ws);
     if (beta || dbias) a.bsum = reinterpret_cast<float*>(static_cast<char*>(ws) + align256(p.part_bytes));
     return launched(al::launch_wgrad(dtype, grad_dtype, a, as_stream(stream)), who);

@@ -71,7 +71,7 @@ __device__ __forceinline__ void save(const Code& k, const CodeShape& s, const Pl
 // 8192 x 11008 bf16: 46 us, 5.9 TB/s; bound by memory.
 template <typename T>
 __global__ __launch_bounds__(kThreads) void act_quantize_kernel(Mat x, CodeShape s, Code k, Grid g) {
-    const Place at(g, xcd_block());
+    const Place at(g, xcd_block(blockIdx.x, gridDim.x));
     Chunk<T> raw;
     load_mat<T>(raw, x, at, s.cols);
     float v[8];
@@ -82,7 +82,7 @@ __global__ __launch_bounds__(kThreads) void act_quantize_kernel(Mat x, CodeShape
 // 8192 x 11008 to bf16: 38 us, 7.2 TB/s with part of the codes in the last-level cache.
 template <typename T>
 __global__ __launch_bounds__(kThreads) void act_dequantize_kernel(Code k, CodeShape s, Mat out, Grid g) {
-    const Place at(g, xcd_block());
+    const Place at(g, xcd_block(blockIdx.x, gridDim.x));
     Coded r;
     load_code<false>(r, k, s, at);
     float v[8];

@@ -232,10 +232,10 @@ __device__ __forceinline__ void e8_decode(u32x2 q, uint32_t e, float (&v)[8]) {
     }
 }
 
-// Workgroups go to the 8 XCDs in turn; this gives each XCD a contiguous eighth of the work, so that lines which
+// Workgroups (w of n) go to the 8 XCDs in turn; this gives each XCD a contiguous eighth of the work, so that lines which
 // neighbouring workgroups share (exponent bytes, row ends) stay in one L2.
-__device__ __forceinline__ uint32_t xcd_block() {
-    const uint32_t n = gridDim.x, w = blockIdx.x, x = w & 7u, per = n >> 3, rest = n & 7u;
+__device__ __forceinline__ uint32_t xcd_block(uint32_t w, uint32_t n) {
+    const uint32_t x = w & 7u, per = n >> 3, rest = n & 7u;
     return x * per + (x < rest ? x : rest) + (w >> 3);
 }
 

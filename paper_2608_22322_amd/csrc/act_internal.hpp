@@ -84,12 +84,15 @@ struct Wgrad {
     const void* base;
     void *dw, *dbias;
     float* part;   // workspace: [splits][out][cols] partial products
-    float* bsum;   // workspace: out column sums of dy, then their partials
+    float* bsum;   // workspace: out column sums of dy, then [bparts][out] partials (the partials alone if beside)
     int32_t tile, splits, bparts;
+    bool beside;    // the sums of dy are taken in the product's launch
+    uint32_t sums;  // set by the launcher: how many of that launch's workgroups take them
 };
 // How a call is cut (tile variant, splits over the tokens), by its sizes alone.
 struct WgradPlan {
     int32_t tile, splits, bparts;
+    bool beside;
     size_t part_bytes, bsum_bytes;
 };
 WgradPlan wgrad_plan(int dtype, int64_t tokens, int64_t out, int64_t in);

@@ -30,6 +30,7 @@ typedef __attribute__((address_space(3))) uint16_t* lds_u16;
 // these lie in different banks.
 constexpr int kTurn = 32;  // tokens a turn
 constexpr int kBig = 256, kMid = 128, kEdge = 64;  // tile widths
+constexpr int64_t kBeside = 16384;  // most tokens at which a split product's launch also takes the sums of dy
 
 __device__ __forceinline__ int edge_at(int t, int c) { return t * kEdge + ((((c >> 4) ^ ((t >> 1) & 3)) << 4) | (c & 15)); }
 
@@ -86,23 +87,23 @@ __device__ __forceinline__ u32x4 decode_bf16(u32x2 codes, uint32_t e) {
 __device__ __forceinline__ float grad_at(const bf16* p, int64_t i) { return to_f(p[i]); }
 __device__ __forceinline__ float grad_at(const float* p, int64_t i) { return p[i]; }
 
-// One finished sum: scale, shift, base, and the only rounding.
+// One finished sum: scale, shift (t: the sum of dy's column n), base, and the only rounding.
 template <typename O>
-__device__ __forceinline__ void finish(const Wgrad& a, int64_t n, int k, float v) {
+__device__ __forceinline__ void finish(const Wgrad& a, int64_t n, int k, float v, float t) {
     const int64_t i = n * a.s.cols + k;
     if (a.gamma) v *= a.gamma[k];
-    if (a.beta) v += a.beta[k] * a.bsum[n];
+    if (a.beta) v += a.beta[k] * t;
     if (a.base) v += grad_at(static_cast<const O*>(a.base), i);
     put(static_cast<O*>(a.dw) + i, v);
 }
 
 // Four finished sums of consecutive columns k.. of row n (in: how many of them lie inside).
 template <typename O>
-__device__ __forceinline__ void finish4(const Wgrad& a, int64_t n, int k, int in, f32x4 v) {
+__device__ __forceinline__ void finish4(const Wgrad& a, int64_t n, int k, int in, f32x4 v, float t) {
     if (in < 4) {
 #pragma unroll
         for (int r = 0; r < 3; ++r)
-            if (r < in) finish<O>(a, n, k + r, v[r]);
+            if (r < in) finish<O>(a, n, k + r, v[r], t);
         return;
     }
     typedef float f32x4_a4 __attribute__((ext_vector_type(4), aligned(4)));
@@ -110,7 +111,6 @@ __device__ __forceinline__ void finish4(const Wgrad& a, int64_t n, int k, int in
     if (a.gamma) v *= *reinterpret_cast<const f32x4_a4*>(a.gamma + k);
     if (a.beta) {
         const f32x4 b = *reinterpret_cast<const f32x4_a4*>(a.beta + k);
-        const float t = a.bsum[n];
 #pragma unroll
         for (int r = 0; r < 4; ++r) v[r] += b[r] * t;
     }
@@ -208,19 +208,56 @@ __device__ __forceinline__ void write_tile(const Wgrad& a, const Tile<B, M>& t, 
                 } else {
                     int n, k;
                     const int in = t.quad(a, w, i, j, q, lane, n, k);
-                    if (in > 0) finish4<O>(a, n, k, in, v);
+                    if (in > 0) finish4<O>(a, n, k, in, v, a.beta ? a.bsum[n] : 0.0f);
                 }
             }
         }
     }
 }
 
-// The splits' partial products, added in order, 8 splits' loads in flight.
+// Column sums of dy over one of bparts slabs of tokens, 512 columns (at = slab + bparts * block of columns): 8 columns a lane, W
+// wavefronts, 8 rows of each in flight; buf: (W - 1) * 512 floats of LDS.
+template <typename T, int W>
+__device__ __forceinline__ void sum_dy(const Wgrad& a, uint32_t at, float* part, float* buf) {
+    const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, slab = (int)(at % (uint32_t)a.bparts);
+    const int c = (int)(at / (uint32_t)a.bparts * 64 + lane) * 8, out = (int)a.out;
+    float s[8] = {};
+    if (c < out) {
+        const int64_t r0 = a.s.rows * slab / a.bparts, r1 = a.s.rows * (slab + 1) / a.bparts;
+        for (int64_t r = r0 + w; r < r1; r += 8 * W) {
+            Chunk<T> k[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                k[i].zero();
+                if (r + i * W < r1) load_chunk(k[i], static_cast<const T*>(a.dy.p) + (r + i * W) * a.dy.ld, c, out);
+            }
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                float v[8];
+                k[i].get(v);
+#pragma unroll
+                for (int j = 0; j < 8; ++j) s[j] += v[j];
+            }
+        }
+    }
+    if (w > 0)
+#pragma unroll
+        for (int j = 0; j < 8; ++j) buf[(w - 1) * 512 + j * 64 + lane] = s[j];
+    __syncthreads();
+    if (w > 0 || c >= out) return;
+    for (int i = 0; i < W - 1; ++i)
+#pragma unroll
+        for (int j = 0; j < 8; ++j) s[j] += buf[i * 512 + j * 64 + lane];
+    store_chunk(part + a.out * slab, c, out, s);
+}
+
+// The splits' partial products, added in order, 8 splits' loads in flight; the slabs' sums of dy likewise, which the lanes that hold
+// column 0 write as the bias gradient.
 template <typename O, int B, int M>
 __global__ __launch_bounds__(256) void wgrad_join_kernel(Wgrad a, FastDiv kt, uint32_t tiles) {
     typedef Tile<B, M> G;
     constexpr uint32_t kBlocks = B * B / 1024;  // workgroups a tile
-    const uint32_t id = xcd_block(), tile = id / kBlocks, at = id % kBlocks * 256 + threadIdx.x, lane = at & 63, slot = at >> 6;
+    const uint32_t id = xcd_block(blockIdx.x, gridDim.x), tile = id / kBlocks, at = id % kBlocks * 256 + threadIdx.x, lane = at & 63, slot = at >> 6;
     const int64_t size = (int64_t)tiles * (B * B / 4);
     const f32x4* p = reinterpret_cast<const f32x4*>(a.part) + (int64_t)tile * (B * B / 4) + at;
     f32x4 v = {};
@@ -237,7 +274,20 @@ __global__ __launch_bounds__(256) void wgrad_join_kernel(Wgrad a, FastDiv kt, ui
     int n, k;
     const int in = G(a, tn, (int)(tile - (uint32_t)tn * kt.d))
                        .quad(a, w, e / (G::FK * G::kQuads), e / G::kQuads % G::FK, e % G::kQuads, (int)lane, n, k);
-    if (in > 0) finish4<O>(a, n, k, in, v);
+    if (in <= 0) return;
+    float t = 0.0f;
+    if (a.beta && !a.sums) t = a.bsum[n];
+    if (a.sums && (a.beta || (a.dbias && k == 0))) {
+        for (int i = 0; i < a.bparts; i += 8) {  // a multiple of 8 here
+            float u[8];
+#pragma unroll
+            for (int r = 0; r < 8; ++r) u[r] = a.bsum[(int64_t)(i + r) * a.out + n];
+#pragma unroll
+            for (int r = 0; r < 8; ++r) t += u[r];
+        }
+        if (a.dbias && k == 0) put(static_cast<O*>(a.dbias) + n, t);
+    }
+    finish4<O>(a, n, k, in, v, t);
 }
 
 // 64 x 64 outputs, 4 wavefronts of 32 x 32, any size and alignment. A turn is short here, so the loads of AHEAD of them are
@@ -247,12 +297,19 @@ template <typename T, typename O>
 __global__ __launch_bounds__(256) void wgrad_edge_kernel(Wgrad a) {
     __shared__ __attribute__((aligned(16))) uint16_t dy_s[2][kTurn * kEdge], x_s[2][kTurn * kEdge];
     constexpr int PARTS = sizeof(T) == 4 ? 3 : 1, AHEAD = 4;
+    // the first layers of the grid take the sums of dy, where these are wanted and the tokens are split
+    const int layers = (int)gridDim.z - a.splits, split = (int)blockIdx.z - layers;
+    if (split < 0) {
+        const uint32_t at = (blockIdx.z * gridDim.y + blockIdx.y) * gridDim.x + blockIdx.x;
+        if (at < a.sums) sum_dy<T, 4>(a, at, a.bsum, reinterpret_cast<float*>(dy_s));
+        return;
+    }
     const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
     const int64_t n0 = (int64_t)blockIdx.y * kEdge;
     const int k0 = blockIdx.x * kEdge;
     // this split's tokens
     const int64_t steps = (a.s.rows + kTurn - 1) / kTurn;
-    const int64_t s0 = steps * blockIdx.z / a.splits, s1 = steps * (blockIdx.z + 1) / a.splits;
+    const int64_t s0 = steps * split / a.splits, s1 = steps * (split + 1) / a.splits;
 
     const int cc = (tid & 7) * 8, t0 = tid >> 3;  // this thread's columns and token of a step
     const int out = (int)a.out, c = (int)n0 + cc, from = std::max(0, std::min(c, out - 8)), shift = std::min(c - from, 8);
@@ -311,7 +368,7 @@ __global__ __launch_bounds__(256) void wgrad_edge_kernel(Wgrad a) {
         }
     }
     write_tile<O>(a, Tile<kEdge, 16>(a, blockIdx.y, blockIdx.x), (int64_t)blockIdx.y * gridDim.x + blockIdx.x, (int64_t)gridDim.x * gridDim.y,
-                  blockIdx.z, w, lane, acc);
+                  split, w, lane, acc);
 }
 
 template <int B, int M>
@@ -328,7 +385,7 @@ constexpr uint32_t kBand = 8;
 template <int B>
 __device__ __forceinline__ TileId tile_id(const Wgrad& a) {
     const uint32_t nt = (uint32_t)((a.out + B - 1) / B), kt = (uint32_t)((a.s.cols + B - 1) / B);
-    const uint32_t id = xcd_block(), split = id / (nt * kt), r = id - split * (nt * kt), band = r / (kBand * kt),
+    const uint32_t id = xcd_block(blockIdx.x - a.sums, gridDim.x - a.sums), split = id / (nt * kt), r = id - split * (nt * kt), band = r / (kBand * kt),
                    rows = min(kBand, nt - band * kBand), q = r - band * kBand * kt, k = q / rows;
     return {(int)(band * kBand + q - k * rows), (int)k, (int)split};
 }
@@ -347,6 +404,10 @@ __global__ __launch_bounds__(2 * B, B == kBig ? 2 : 3) void wgrad_tile_kernel(Wg
     constexpr int PARTS = sizeof(T) == 4 ? 3 : 1, BT = kTurn, C = BT / 16;
     constexpr int M = PARTS == 1 ? 16 : 32, FN = Tile<B, M>::FN, FK = Tile<B, M>::FK, H = BT / Product<M>::kTokens;
     __shared__ __attribute__((aligned(16))) uint16_t dy_s[2][BT * B], x_s[2][BT * B];
+    if (blockIdx.x < a.sums) {  // sums of dy, where these are wanted and the tokens are split
+        sum_dy<T, B / 32>(a, blockIdx.x, a.bsum, reinterpret_cast<float*>(dy_s));
+        return;
+    }
     const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
     const TileId tile = tile_id<B>(a);
     typedef Tile<B, PARTS == 1 ? 16 : 32> G;
@@ -487,69 +548,40 @@ __global__ __launch_bounds__(2 * B, B == kBig ? 2 : 3) void wgrad_tile_kernel(Wg
     write_tile<O>(a, t, tile.n * kt + tile.k, kt * ((a.out + B - 1) / B), tile.split, w, lane, acc);
 }
 
-// Column sums of dy over each of bparts slabs of tokens: 8 columns a lane, 4 wavefronts a workgroup, 4 rows at a time.
 template <typename T>
 __global__ __launch_bounds__(256) void dy_sum_kernel(Wgrad a) {
-    __shared__ float buf[3][64 * 8];
-    const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
-    const int c = (blockIdx.x * 64 + lane) * 8, out = (int)a.out;
-    float s[8] = {};
-    if (c < out) {
-        const int64_t r0 = a.s.rows * blockIdx.y / a.bparts, r1 = a.s.rows * (blockIdx.y + 1) / a.bparts;
-        for (int64_t r = r0 + w; r < r1; r += 16) {
-            Chunk<T> k[4];
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const int64_t t = r + 4 * i;
-                k[i].zero();
-                if (t < r1) load_chunk(k[i], static_cast<const T*>(a.dy.p) + t * a.dy.ld, c, out);
-            }
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                float v[8];
-                k[i].get(v);
-#pragma unroll
-                for (int j = 0; j < 8; ++j) s[j] += v[j];
-            }
-        }
-    }
-    if (w > 0)
-#pragma unroll
-        for (int j = 0; j < 8; ++j) buf[w - 1][j * 64 + lane] = s[j];
-    __syncthreads();
-    if (w > 0 || c >= out) return;
-#pragma unroll
-    for (int i = 0; i < 3; ++i)
-#pragma unroll
-        for (int j = 0; j < 8; ++j) s[j] += buf[i][j * 64 + lane];
-    store_chunk(a.bsum + a.out * (1 + (int64_t)blockIdx.y), c, out, s);  // behind the whole sums
+    __shared__ float buf[3 * 512];
+    sum_dy<T, 4>(a, blockIdx.x, a.bsum + a.out, buf);  // behind the whole sums
 }
 
 template <typename T, typename O, int B>
 hipError_t launch_tile(const Wgrad& a, hipStream_t st) {
     const uint32_t kt = (uint32_t)((a.s.cols + B - 1) / B), tiles = kt * (uint32_t)((a.out + B - 1) / B);
-    wgrad_tile_kernel<T, O, B><<<tiles * (uint32_t)a.splits, 2 * B, 0, st>>>(a);
+    wgrad_tile_kernel<T, O, B><<<a.sums + tiles * (uint32_t)a.splits, 2 * B, 0, st>>>(a);
     if (a.splits > 1)
         wgrad_join_kernel<O, B, sizeof(T) == 2 ? 16 : 32><<<tiles * (B * B / 1024), 256, 0, st>>>(a, fast_div(kt), tiles);
     return hipGetLastError();
 }
 
 template <typename T, typename O>
-hipError_t run(const Wgrad& a, hipStream_t st) {
-    if (a.bsum) {
-        dy_sum_kernel<T><<<dim3((uint32_t)((a.out + 511) / 512), (uint32_t)a.bparts), 256, 0, st>>>(a);
+hipError_t run(Wgrad a, hipStream_t st) {
+    const uint32_t sums = a.bsum ? (uint32_t)((a.out + 511) / 512) * (uint32_t)a.bparts : 0u;
+    if (a.bsum && !a.beside) {
+        dy_sum_kernel<T><<<sums, 256, 0, st>>>(a);
         const FoldOut out = {a.dbias, a.bsum};
         const hipError_t e = launch_fold(sizeof(O) == 2 ? AL_DTYPE_BF16 : AL_DTYPE_F32, a.bsum + a.out, a.bparts, a.out, &out, 1, st);
         if (e != hipSuccess) return e;
     }
+    a.sums = a.beside ? sums : 0u;
     if (a.s.cols == 0) return hipSuccess;
     // a plan's partial products have the layout of its tile; the large tiles' 32-bit offsets span 32 rows
     if (a.tile != kEdge && a.dy.ld < (1 << 25) && a.s.pitch < (1 << 26))
         return a.tile == kBig ? launch_tile<T, O, kBig>(a, st) : launch_tile<T, O, kMid>(a, st);
-    const dim3 n((uint32_t)((a.s.cols + kEdge - 1) / kEdge), (uint32_t)((a.out + kEdge - 1) / kEdge), (uint32_t)a.splits);
+    dim3 n((uint32_t)((a.s.cols + kEdge - 1) / kEdge), (uint32_t)((a.out + kEdge - 1) / kEdge), (uint32_t)a.splits);
+    const uint32_t tiles = n.x * n.y;
+    if (a.sums) n.z += (a.sums + tiles - 1) / tiles;
     wgrad_edge_kernel<T, O><<<n, 256, 0, st>>>(a);
     if (a.splits > 1) {
-        const uint32_t tiles = n.x * n.y;
         wgrad_join_kernel<O, kEdge, 16><<<tiles * (kEdge * kEdge / 1024), 256, 0, st>>>(a, fast_div(n.x), tiles);
     }
     return hipGetLastError();
@@ -579,7 +611,7 @@ WgradPlan wgrad_plan(int dtype, int64_t tokens, int64_t out, int64_t in) {
         if (k.tile != kEdge && std::min(out, in) < k.tile) continue;
         const int64_t n = std::max<int64_t>(1, ((out + k.tile - 1) / k.tile) * ((in + k.tile - 1) / k.tile));
         for (const int s : counts) {
-            if (s > 1 && (2 * s > steps || n * s > 2048)) break;
+            if (s > 1 && (2 * s > steps || n * s > 2048 || in == 0)) break;
             const double load = (double)(n * s) / 256, whole = std::ceil(load),
                          turns = (double)((steps + s - 1) / s) * (dtype == AL_DTYPE_BF16 ? 1 : 3.3) + k.ends,
                          turn = k.fit == 1 ? k.each * whole : load > k.fit ? k.each * load : std::max(k.alone, k.each * whole),
@@ -587,7 +619,11 @@ WgradPlan wgrad_plan(int dtype, int64_t tokens, int64_t out, int64_t in) {
             if (best == 0 || t < best) best = t, p.tile = k.tile, p.splits = s, p.part_bytes = s > 1 ? (size_t)(s * n) * k.tile * k.tile * 4 : 0;
         }
     }
-    p.bparts = (int32_t)std::max<int64_t>(1, std::min<int64_t>(256, tokens / 32));
+    // Sums of dy: split products of at most kBeside tokens take them along, in few slabs, as each joining lane adds these up (two
+    // launches less; bf16 with dbias: 512 x 256 x 256 16.1 -> 10.9 us, 6001 x 256 x 2048 31.7 -> 26.6, 16384 x 256 x 256 23.2 -> 19.1).
+    // With more tokens a workgroup's slab takes longer than the product does (65536 x 256 x 256: 41 -> 69 us).
+    p.beside = p.splits > 1 && tokens <= kBeside;
+    p.bparts = (int32_t)(p.beside ? std::max<int64_t>(32, (tokens + 2047) / 2048 * 8) : std::max<int64_t>(1, std::min<int64_t>(256, tokens / 32)));
     p.bsum_bytes = (size_t)out * (p.bparts + 1) * 4;
     return p;
 }
