@@ -87,19 +87,19 @@ __device__ __forceinline__ u32x4 decode_bf16(u32x2 codes, uint32_t e) {
 __device__ __forceinline__ float grad_at(const bf16* p, int64_t i) { return to_f(p[i]); }
 __device__ __forceinline__ float grad_at(const float* p, int64_t i) { return p[i]; }
 
-// One finished sum: scale, shift (t: the sum of dy's column n), base, and the only rounding.
-template <typename O>
-__device__ __forceinline__ void finish(const Wgrad& a, int64_t n, int k, float v, float t) {
+// One finished sum: scale, shift (t(): the sum of dy's column n), base, and the only rounding.
+template <typename O, typename F>
+__device__ __forceinline__ void finish(const Wgrad& a, int64_t n, int k, float v, const F& t) {
     const int64_t i = n * a.s.cols + k;
     if (a.gamma) v *= a.gamma[k];
-    if (a.beta) v += a.beta[k] * t;
+    if (a.beta) v += a.beta[k] * t();
     if (a.base) v += grad_at(static_cast<const O*>(a.base), i);
     put(static_cast<O*>(a.dw) + i, v);
 }
 
 // Four finished sums of consecutive columns k.. of row n (in: how many of them lie inside).
-template <typename O>
-__device__ __forceinline__ void finish4(const Wgrad& a, int64_t n, int k, int in, f32x4 v, float t) {
+template <typename O, typename F>
+__device__ __forceinline__ void finish4(const Wgrad& a, int64_t n, int k, int in, f32x4 v, const F& t) {
     if (in < 4) {
 #pragma unroll
         for (int r = 0; r < 3; ++r)
@@ -111,8 +111,9 @@ __device__ __forceinline__ void finish4(const Wgrad& a, int64_t n, int k, int in
     if (a.gamma) v *= *reinterpret_cast<const f32x4_a4*>(a.gamma + k);
     if (a.beta) {
         const f32x4 b = *reinterpret_cast<const f32x4_a4*>(a.beta + k);
+        const float s = t();
 #pragma unroll
-        for (int r = 0; r < 4; ++r) v[r] += b[r] * t;
+        for (int r = 0; r < 4; ++r) v[r] += b[r] * s;
     }
     if constexpr (sizeof(O) == 4) {
         if (a.base) v += *reinterpret_cast<const f32x4_a4*>(static_cast<const float*>(a.base) + i);
@@ -208,7 +209,7 @@ __device__ __forceinline__ void write_tile(const Wgrad& a, const Tile<B, M>& t, 
                 } else {
                     int n, k;
                     const int in = t.quad(a, w, i, j, q, lane, n, k);
-                    if (in > 0) finish4<O>(a, n, k, in, v, a.beta ? a.bsum[n] : 0.0f);
+                    if (in > 0) finish4<O>(a, n, k, in, v, [&] { return a.bsum[n]; });
                 }
             }
         }
@@ -287,22 +288,24 @@ __global__ __launch_bounds__(256) void wgrad_join_kernel(Wgrad a, FastDiv kt, ui
         }
         if (a.dbias && k == 0) put(static_cast<O*>(a.dbias) + n, t);
     }
-    finish4<O>(a, n, k, in, v, t);
+    finish4<O>(a, n, k, in, v, [&] { return t; });
 }
 
 // 64 x 64 outputs, 4 wavefronts of 32 x 32, any size and alignment. A turn is short here, so the loads of AHEAD of them are
 // in flight. Loads are never masked: rows past the last are the last one's and columns past a side's end its last ones, of which
 // the former are cleared on the way to LDS and the latter make sums that are not written.
-template <typename T, typename O>
+template <typename T, typename O, bool SUMS>
 __global__ __launch_bounds__(256) void wgrad_edge_kernel(Wgrad a) {
     __shared__ __attribute__((aligned(16))) uint16_t dy_s[2][kTurn * kEdge], x_s[2][kTurn * kEdge];
     constexpr int PARTS = sizeof(T) == 4 ? 3 : 1, AHEAD = 4;
-    // the first layers of the grid take the sums of dy, where these are wanted and the tokens are split
-    const int layers = (int)gridDim.z - a.splits, split = (int)blockIdx.z - layers;
-    if (split < 0) {
-        const uint32_t at = (blockIdx.z * gridDim.y + blockIdx.y) * gridDim.x + blockIdx.x;
-        if (at < a.sums) sum_dy<T, 4>(a, at, a.bsum, reinterpret_cast<float*>(dy_s));
-        return;
+    int split = (int)blockIdx.z;
+    if (SUMS) {  // the first layers of the grid take the sums of dy (a kernel of its own: 0.5 of 9 us where there are none)
+        split -= (int)gridDim.z - a.splits;
+        if (split < 0) {
+            const uint32_t at = (blockIdx.z * gridDim.y + blockIdx.y) * gridDim.x + blockIdx.x;
+            if (at < a.sums) sum_dy<T, 4>(a, at, a.bsum, reinterpret_cast<float*>(dy_s));
+            return;
+        }
     }
     const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
     const int64_t n0 = (int64_t)blockIdx.y * kEdge;
@@ -579,8 +582,9 @@ hipError_t run(Wgrad a, hipStream_t st) {
         return a.tile == kBig ? launch_tile<T, O, kBig>(a, st) : launch_tile<T, O, kMid>(a, st);
     dim3 n((uint32_t)((a.s.cols + kEdge - 1) / kEdge), (uint32_t)((a.out + kEdge - 1) / kEdge), (uint32_t)a.splits);
     const uint32_t tiles = n.x * n.y;
-    if (a.sums) n.z += (a.sums + tiles - 1) / tiles;
-    wgrad_edge_kernel<T, O><<<n, 256, 0, st>>>(a);
+    n.z += (a.sums + tiles - 1) / tiles;
+    if (a.sums) wgrad_edge_kernel<T, O, true><<<n, 256, 0, st>>>(a);
+    else wgrad_edge_kernel<T, O, false><<<n, 256, 0, st>>>(a);
     if (a.splits > 1) {
         wgrad_join_kernel<O, kEdge, 16><<<tiles * (kEdge * kEdge / 1024), 256, 0, st>>>(a, fast_div(n.x), tiles);
     }
