@@ -76,7 +76,7 @@ def _mat(t, name: str, rows: int, cols: int, dtype):
     ld, inner = t.stride()
     if inner != 1 and cols > 1:
         raise ValueError(f"{name}: rows must be contiguous (strides {t.stride()})")
-    return t.data_ptr(), ld if ld > cols else cols
+    return t.data_ptr(), ld if rows > 1 else cols  # a pitch below cols (rows that overlap, an expanded row) is refused by the library
 
 
 def _vec(t, name: str, n: int, dtype):

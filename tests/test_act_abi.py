@@ -138,3 +138,22 @@ def test_wgrad_sizes_past_the_grids():
     assert need.value <= 11008 * 4 * 257 + 256
     assert _status("al_linear_wgrad_workspace_bytes", 1, 8192, 256, 256, ctypes.byref(need)) == 0
     assert need.value <= 64 << 20
+
+
+@pytest.mark.parametrize("rows,cols,strides,pitch", [
+    (8, 100, (0, 1), 0), (8, 100, (1, 1), 1), (8, 100, (99, 1), 99), (8, 1, (0, 5), 0),  # expanded or overlapping rows keep their pitch
+    (8, 100, (100, 1), 100), (8, 100, (107, 1), 107), (1, 100, (0, 1), 100), (0, 100, (100, 1), 100),
+])
+def test_row_pitch_of_a_tensor(rows, cols, strides, pitch):
+    """An expanded row (the gradient of a sum, say) holds one row: taken for a packed matrix it would be read past its end. Its pitch
+    reaches the library as it is, which refuses it."""
+    from types import SimpleNamespace
+
+    import torch
+
+    from paper_2608_22322_amd import activations as act
+
+    t = SimpleNamespace(dtype=torch.float32, shape=(rows, cols), is_cuda=True, device="cuda", stride=lambda: strides, data_ptr=lambda: A)
+    assert act._mat(t, "x", rows, cols, torch.float32) == (A, pitch)
+    if rows > 1 and pitch < cols:
+        assert _quantize(dtype=0, rows=rows, cols=cols, ld=pitch) == 1

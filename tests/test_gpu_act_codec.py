@@ -110,3 +110,28 @@ def test_refusals():
         act.ActCode(c.codes, c.exps, 9, 100, 64)
     with pytest.raises(ValueError):
         act.ActCode(c.codes.cpu(), c.exps, 8, 100, 64)
+
+
+def test_expanded_rows_are_refused():
+    """Views whose rows overlap hold fewer elements than rows x cols."""
+    import paper_2608_22322_amd as al
+    from paper_2608_22322_amd import activations as act
+
+    c = act.alloc_code(8, 100, 64)
+    wide = torch.randn(1, 100, device="cuda")
+    full = torch.randn(8, 100, device="cuda")
+    for bad in (wide.expand(8, 100), torch.randn(200, device="cuda").as_strided((8, 100), (1, 1))):
+        with pytest.raises(al.ALError):
+            act.quantize(bad, c)
+        with pytest.raises(al.ALError):
+            act.dequantize(c, bad)
+        with pytest.raises(al.ALError):
+            act.norm_forward(act.RMS, bad, torch.empty_like(full))
+        with pytest.raises(al.ALError):
+            act.norm_backward(act.RMS, bad, c, None, torch.ones(8, device="cuda"), torch.empty_like(full))
+        with pytest.raises(al.ALError):
+            act.swiglu_forward(full, bad, torch.empty_like(full))
+        with pytest.raises(al.ALError):
+            act.linear_wgrad(bad, c, torch.empty(100, 100, device="cuda"), al.workspace(1 << 22))
+    c1 = act.alloc_code(1, 100, 64)
+    act.quantize(wide.expand(1, 100), c1)  # a single row has no pitch
