@@ -566,7 +566,8 @@ int32_t norm_backward_parts(int64_t rows, int64_t cols) {
 hipError_t launch_norm_backward(int dtype, bool layer, int grad_dtype, const NormBackward& a, hipStream_t st) {
     hipError_t e = hipSuccess;
     if (a.s.rows > 0) e = dtype == AL_DTYPE_BF16 ? backward<bf16>(layer, a, st) : backward<float>(layer, a, st);
-    if (e == hipSuccess && a.part && (a.parts != 1 || a.s.cols > kRowMax)) {
+    // (without rows there is no workspace either, and the sums are zeros)
+    if (e == hipSuccess && (a.dgamma || a.dbeta) && (a.parts != 1 || a.s.cols > kRowMax)) {
         const FoldOut out[2] = {{a.dgamma, nullptr}, {a.dbeta, nullptr}};
         e = launch_fold(grad_dtype, a.part, a.parts, a.s.cols, out, layer ? 2 : 1, st);
     }

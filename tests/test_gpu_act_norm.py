@@ -304,3 +304,17 @@ def test_in_place_where_a_row_ends_in_another_wavefront(cols, dtype):
         y = d.clone()
         act.norm_forward(act.RMS, y, y, gamma=gd)
         assert torch.equal(y, apart)
+
+
+@pytest.mark.parametrize("kind", ["layer", "rms"])
+@pytest.mark.parametrize("cols", [100, 20000])
+def test_no_rows_give_zero_weight_gradients_without_a_workspace(cols, kind):
+    from paper_2608_22322_amd import activations as act
+
+    k = act.LAYER if kind == "layer" else act.RMS
+    assert act.norm_backward_workspace_bytes(k, 0, cols, torch.float32) == 0
+    none, rows = torch.empty(0, cols, device="cuda"), torch.empty(0, device="cuda")
+    dg = torch.full((cols,), 7.0, device="cuda")
+    db = torch.full((cols,), 7.0, device="cuda") if kind == "layer" else None
+    act.norm_backward(k, none, none, rows if kind == "layer" else None, rows, torch.empty(0, cols, device="cuda"), dgamma=dg, dbeta=db)
+    assert not dg.any() and (db is None or not db.any())
