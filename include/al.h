@@ -420,9 +420,10 @@ al_status al_linear_wgrad_workspace_bytes(int32_t dtype, int64_t tokens, int64_t
  * itself (gradient accumulation). dbias: out_features values of grad_dtype or
  * NULL. The products are exact (both factors are bf16 numbers, an fp32 dy is three
  * of them) and summed in fp32 on the matrix cores. tokens == 0: dw = base, dbias = 0.
- * out_features below 2^22, in_features below 2^29 (AL_EUNSUPPORTED otherwise).
- * One launch where the outputs fill the device; fewer outputs split the tokens,
- * and a second launch adds the parts in order; beta or dbias take two more. */
+ * out_features below 2^22, in_features below 2^29, at most 2^38 weights (AL_EUNSUPPORTED otherwise).
+ * One launch where the outputs fill the device (beta or dbias take two more); fewer
+ * outputs split the tokens, and a second launch adds the parts, and up to 16384
+ * tokens those of dy's sums, in order. */
 al_status al_linear_wgrad(int32_t dtype, const void* dy, int64_t lddy, const void* codes, const void* exps,
                           int32_t block, int64_t tokens, int64_t out_features, int64_t in_features,
                           const float* gamma, const float* beta, int32_t grad_dtype, const void* base, void* dw,

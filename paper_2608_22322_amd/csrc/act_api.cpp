@@ -95,10 +95,11 @@ al_status check_kind(int32_t kind, const char* who) {
     return AL_OK;
 }
 
-// The grids of the products hold these.
+// The grids of the products hold these (2^38 outputs are 2^26 of the smallest tiles, and more than the memory holds).
 al_status check_product(int64_t out, int64_t in, const char* who) {
     if (out >= (int64_t(1) << 22) || in >= (int64_t(1) << 29))
         return fail(AL_EUNSUPPORTED, "%s: %lld out_features (below 2^22) or %lld in_features (below 2^29)", who, (long long)out, (long long)in);
+    if (out * in > (int64_t(1) << 38)) return fail(AL_EUNSUPPORTED, "%s: %lld x %lld weights are too many", who, (long long)out, (long long)in);
     return AL_OK;
 }
 

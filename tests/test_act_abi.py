@@ -157,3 +157,9 @@ def test_row_pitch_of_a_tensor(rows, cols, strides, pitch):
     assert act._mat(t, "x", rows, cols, torch.float32) == (A, pitch)
     if rows > 1 and pitch < cols:
         assert _quantize(dtype=0, rows=rows, cols=cols, ld=pitch) == 1
+
+
+def test_wgrad_refuses_more_weights_than_its_grids_hold():
+    need = ctypes.c_size_t(0)
+    for out, cols, want in (((1 << 22) - 1, 1 << 17, 4), (1 << 21, (1 << 17) + 1, 4), (1 << 21, 1 << 17, 0), ((1 << 22) - 1, (1 << 29) - 1, 4)):
+        assert _status("al_linear_wgrad_workspace_bytes", 1, 64, out, cols, ctypes.byref(need)) == want
