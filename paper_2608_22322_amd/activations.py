@@ -10,7 +10,8 @@ value, one power-of-two step per block of 32, 64 or 128 columns of a row) and th
   also gives the code of its output, for the next linear layer's weight gradient.
 * :func:`linear_wgrad`: a linear layer's weight (and bias) gradient from its input's code.
 
-Matrices are 2-D tensors of float32 or bfloat16, rows contiguous (any row pitch, so slices of wider buffers will do).
+Matrices are 2-D tensors of float32 or bfloat16, rows contiguous (any row pitch, so slices of wider buffers will do; rows that
+overlap, as those of an expanded row do, are refused).
 Every call enqueues on `stream` (default: the current stream) and returns; outputs and workspaces are the caller's.
 """
 from __future__ import annotations
@@ -76,7 +77,7 @@ def _mat(t, name: str, rows: int, cols: int, dtype):
     ld, inner = t.stride()
     if inner != 1 and cols > 1:
         raise ValueError(f"{name}: rows must be contiguous (strides {t.stride()})")
-    return t.data_ptr(), ld if rows > 1 else cols  # a pitch below cols (rows that overlap, an expanded row) is refused by the library
+    return t.data_ptr(), ld if rows > 1 else cols  # the library refuses a pitch below cols
 
 
 def _vec(t, name: str, n: int, dtype):
