@@ -12,6 +12,7 @@ step is al_adamw_step over the block's parameters.
 from __future__ import annotations
 
 import argparse
+import functools
 
 import torch
 
@@ -21,9 +22,20 @@ from . import log2_floor_of, tensor_array, workspace
 NAMES = ("gate", "up", "down", "norm")
 
 
+def _on_its_gpu(method):
+    """Run a method with the block's GPU as the current device, where this package's kernels run."""
+
+    @functools.wraps(method)
+    def run(self, *args):
+        with torch.cuda.device(self.device):
+            return method(self, *args)
+
+    return run
+
+
 class SwigluMLP:
     """The block's parameters (fp32, with bf16 copies for the products), their gradients and states, and its buffers
-    for batches of `tokens` rows."""
+    for batches of `tokens` rows, all on `device`."""
 
     def __init__(self, hidden: int, ffn: int, tokens: int, block: int = 64, eps: float = 1e-5, lr: float = 1e-3, seed: int = 0,
                  device="cuda"):
@@ -48,6 +60,7 @@ class SwigluMLP:
         self.xhat = act.alloc_code(tokens, hidden, block, device)
         self.gate_code, self.up_code = act.alloc_code(tokens, ffn, block, device), act.alloc_code(tokens, ffn, block, device)
         self.rstd = torch.empty(tokens, device=device)
+        self.device = self.rstd.device
         # scratch of either pass
         self.h_code = act.alloc_code(tokens, ffn, block, device)
         self.n = torch.empty(tokens, hidden, **bf16)
@@ -64,6 +77,7 @@ class SwigluMLP:
         """What the same pass keeps in bf16: x, n, gate, up and h."""
         return 2 * self.tokens * (2 * self.hidden + 3 * self.ffn) + 4 * self.tokens
 
+    @_on_its_gpu
     def forward(self, x):
         """y for a [tokens, hidden] bf16 batch."""
         act.norm_forward(act.RMS, x, self.n, rstd=self.rstd, gamma=self.param["norm"].view(-1), eps=self.eps, code=self.xhat)
@@ -72,6 +86,7 @@ class SwigluMLP:
         act.swiglu_forward(self.a, self.b, self.h, self.gate_code, self.up_code)
         return torch.addmm(x, self.h, self.weight["down"].t())
 
+    @_on_its_gpu
     def backward(self, dy):
         """dx from dy, the parameters' gradients into self.grad (what the last forward pass saved is used)."""
         gamma = self.param["norm"].view(-1)
@@ -87,6 +102,7 @@ class SwigluMLP:
                           ws=self.ws)
         return dx
 
+    @_on_its_gpu
     def step(self, t: int) -> None:
         """One AdamW step (8-bit states) and the weights' bf16 copies from the new parameters."""
         adamw_step(self.states, self.cfg, t, self.step_ws, arr=self.arr)
