@@ -26,7 +26,14 @@ from . import DTYPE_BF16, DTYPE_F32, check, lib
 
 LAYER, RMS = 0, 1
 BLOCKS = (32, 64, 128)
-_DTYPES = {torch.float32: DTYPE_F32, torch.bfloat16: DTYPE_BF16}
+
+
+class _Dtypes(dict):
+    def __missing__(self, dtype):
+        raise ValueError(f"dtype {dtype}: float32 or bfloat16 is needed")
+
+
+_DTYPES = _Dtypes({torch.float32: DTYPE_F32, torch.bfloat16: DTYPE_BF16})
 
 
 @dataclass
@@ -52,7 +59,10 @@ class ActCode:
 
 def code_bytes(rows: int, cols: int, block: int = 64) -> int:
     """Bytes of codes and exponents of a rows x cols matrix."""
-    return lib().al_act_code_bytes(rows, cols, block) + lib().al_act_exp_bytes(rows, cols, block)
+    codes, exps = lib().al_act_code_bytes(rows, cols, block), lib().al_act_exp_bytes(rows, cols, block)
+    if codes < 0 or exps < 0:
+        raise ValueError(f"no code of {rows} x {cols} values in blocks of {block}")
+    return codes + exps
 
 
 def alloc_code(rows: int, cols: int, block: int = 64, device="cuda") -> ActCode:
@@ -63,10 +73,7 @@ def alloc_code(rows: int, cols: int, block: int = 64, device="cuda") -> ActCode:
 
 # ---------------------------------------------------------------------------- argument checks
 def _dtype(t) -> int:
-    try:
-        return _DTYPES[t.dtype]
-    except KeyError:
-        raise ValueError(f"dtype {t.dtype}: float32 or bfloat16 is needed") from None
+    return _DTYPES[t.dtype]
 
 
 def _gpu(t, stream=None) -> int:
