@@ -390,7 +390,10 @@ al_status al_norm_backward(int32_t kind, int32_t dtype, const void* dy, int64_t 
                            void* stream);
 
 /* h = silu(gate) * up, silu(g) = g / (1 + e^-g), in fp32, rounded once to
- * dtype; optionally the E8 codes of gate and up (all four pointers or none). */
+ * dtype; optionally the E8 codes of gate and up (all four pointers or none).
+ * Here and in the backward pass 1 / (1 + e^-g) is within 2^-22 of its value
+ * (relative) for fp32, within (|g| + 5) 2^-24 for bf16, and 0 where e^-g
+ * overflows. */
 al_status al_swiglu_forward(int32_t dtype, const void* gate, int64_t ldgate, const void* up, int64_t ldup,
                             int64_t rows, int64_t cols, void* h, int64_t ldh, int32_t block, void* gate_codes,
                             void* gate_exps, void* up_codes, void* up_exps, void* stream);
