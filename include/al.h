@@ -328,8 +328,8 @@ al_status al_apollo_step(const al_apollo_tensor* tensors, int32_t nt, const al_a
  * Matrices. rows x cols, one row per token, element (i, j) at i * ld + j with
  * ld >= cols (ignored for rows <= 1). fp32 or bf16; any alignment of the
  * element type and any ld will do (16-byte aligned rows are fastest). Outputs
- * must not overlap inputs except where an entry point says so. rows and cols
- * up to 2^31 - 1, rows * ld below 2^48.
+ * must not overlap inputs except where an entry point says so. rows up to
+ * 2^31 - 1, cols up to 2^31 - 8193, rows * ld up to 2^48.
  *
  * Activation code E8 (block: 32, 64 or 128 columns; blocks do not cross rows;
  * the last block of a row may be short). For a block with largest magnitude a:
@@ -348,7 +348,7 @@ al_status al_apollo_step(const al_apollo_tensor* tensors, int32_t nt, const al_a
 typedef enum al_norm_kind { AL_NORM_LAYER = 0, AL_NORM_RMS = 1 } al_norm_kind;
 
 /* Bytes of the codes and of the exponents of a rows x cols matrix. -1 for a
- * bad block or a negative size. */
+ * bad block, a negative size or one past the limits above. */
 int64_t al_act_code_bytes(int64_t rows, int64_t cols, int32_t block);
 int64_t al_act_exp_bytes(int64_t rows, int64_t cols, int32_t block);
 

@@ -33,17 +33,17 @@ size_t align256(size_t x) { return (x + 255) & ~size_t(255); }
 
 bool valid_block(int32_t b) { return b == 32 || b == 64 || b == 128; }
 
-constexpr int64_t kMost = (int64_t(1) << 31) - 1;
+// Most rows, most columns (so that column numbers past the last chunk a kernel looks at stay in 32 bits).
+constexpr int64_t kMostRows = (int64_t(1) << 31) - 1, kMostCols = kMostRows - 8192;
 
 al_status check_dtype(int32_t d, const char* who, const char* name) {
     if (d != AL_DTYPE_F32 && d != AL_DTYPE_BF16) return fail(AL_EINVAL, "%s: %s %d", who, name, d);
     return AL_OK;
 }
 
-// cols is held to 2^31 - 1 - 8192 so that column numbers past the last chunk a kernel looks at stay in 32 bits.
 al_status check_shape(int64_t rows, int64_t cols, const char* who) {
     if (rows < 0 || cols < 0) return fail(AL_EINVAL, "%s: negative shape", who);
-    if (rows > kMost || cols > kMost - 8192) return fail(AL_EUNSUPPORTED, "%s: %lld x %lld is too large", who, (long long)rows, (long long)cols);
+    if (rows > kMostRows || cols > kMostCols) return fail(AL_EUNSUPPORTED, "%s: %lld x %lld is too large", who, (long long)rows, (long long)cols);
     return AL_OK;
 }
 
@@ -119,12 +119,12 @@ size_t norm_ws(int32_t kind, int64_t rows, int64_t cols) {
 extern "C" {
 
 int64_t al_act_code_bytes(int64_t rows, int64_t cols, int32_t block) {
-    if (rows < 0 || cols < 0 || rows > kMost || cols > kMost || !valid_block(block)) return -1;
+    if (rows < 0 || cols < 0 || rows > kMostRows || cols > kMostCols || !valid_block(block)) return -1;
     return rows * ((cols + block - 1) / block) * block;
 }
 
 int64_t al_act_exp_bytes(int64_t rows, int64_t cols, int32_t block) {
-    if (rows < 0 || cols < 0 || rows > kMost || cols > kMost || !valid_block(block)) return -1;
+    if (rows < 0 || cols < 0 || rows > kMostRows || cols > kMostCols || !valid_block(block)) return -1;
     return rows * ((cols + block - 1) / block);
 }
 

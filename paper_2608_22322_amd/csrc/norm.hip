@@ -419,12 +419,13 @@ __global__ __launch_bounds__(64) void norm_weights_wide_kernel(NormBackward a) {
     if (LAYER) store_chunk(a.part + ((int64_t)a.parts + blockIdx.y) * cols, c, cols, db);
 }
 
-// Column sums of partial sums: 64 columns a workgroup, wavefront w of 16 takes rows w, w + 16, ..., 8 of them in flight.
+// Column sums of partial sums, from column c0 on: 64 columns a workgroup, wavefront w of 16 takes rows w, w + 16, ..., 8 of them in
+// flight.
 template <typename O>
-__global__ __launch_bounds__(1024) void fold_kernel(const float* part, int32_t parts, int64_t cols, FoldOut o0, FoldOut o1) {
+__global__ __launch_bounds__(1024) void fold_kernel(const float* part, int32_t parts, int64_t cols, int64_t c0, FoldOut o0, FoldOut o1) {
     __shared__ float buf[16][64];
     const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
-    const int64_t c = (int64_t)blockIdx.x * 64 + lane;
+    const int64_t c = c0 + (int64_t)blockIdx.x * 64 + lane;
     const FoldOut o = blockIdx.y ? o1 : o0;
     const float* const p0 = part + (int64_t)blockIdx.y * parts * cols + c;
     float s = 0.0f;
@@ -539,13 +540,18 @@ hipError_t backward(bool layer, const NormBackward& a, hipStream_t st) {
 }  // namespace
 
 hipError_t launch_fold(int grad_dtype, const float* part, int32_t parts, int64_t cols, const FoldOut* out, int count, hipStream_t st) {
-    const dim3 n((uint32_t)((cols + 63) / 64), (uint32_t)count);
+    constexpr int64_t kMost = int64_t(1) << 27;  // columns of one launch (16 threads each; a grid holds fewer than 2^32)
     const FoldOut &a = out[0], &b = out[count - 1];
-    if (grad_dtype == AL_DTYPE_BF16)
-        fold_kernel<bf16><<<n, 1024, 0, st>>>(part, parts, cols, a, b);
-    else
-        fold_kernel<float><<<n, 1024, 0, st>>>(part, parts, cols, a, b);
-    return hipGetLastError();
+    for (int64_t c0 = 0; c0 < cols; c0 += kMost) {
+        const dim3 n((uint32_t)((std::min(kMost, cols - c0) + 63) / 64), (uint32_t)count);
+        if (grad_dtype == AL_DTYPE_BF16)
+            fold_kernel<bf16><<<n, 1024, 0, st>>>(part, parts, cols, c0, a, b);
+        else
+            fold_kernel<float><<<n, 1024, 0, st>>>(part, parts, cols, c0, a, b);
+        const hipError_t e = hipGetLastError();
+        if (e != hipSuccess) return e;
+    }
+    return hipSuccess;
 }
 
 hipError_t launch_norm_forward(int dtype, bool layer, const NormForward& a, hipStream_t st) {

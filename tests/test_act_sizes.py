@@ -1,7 +1,10 @@
 """CPU tests: what the activation operators' size queries answer, and refuse."""
+import ctypes
+
 import pytest
 import torch
 
+import paper_2608_22322_amd as al
 from paper_2608_22322_amd import activations as act
 
 
@@ -19,3 +22,15 @@ def test_sizes_of_no_code_are_refused(rows, cols, block):
 def test_workspaces_of_other_types_are_refused():
     with pytest.raises(ValueError):
         act.norm_backward_workspace_bytes(act.RMS, 4, 100, dtype=torch.float16)
+
+
+def test_size_queries_and_calls_agree_on_the_widest_row():
+    """2^31 - 8193 columns: asked for as a size, then as (empty) work."""
+    L, most = al.lib(), (1 << 31) - 8193
+    assert L.al_act_code_bytes(1, most, 128) == (most + 127) // 128 * 128 and L.al_act_exp_bytes(1, most, 128) == (most + 127) // 128
+    assert L.al_act_code_bytes(1, most + 1, 128) == -1 and L.al_act_exp_bytes(1, most + 1, 128) == -1
+    n = ctypes.c_size_t(0)
+    assert L.al_norm_backward_workspace_bytes(1, 1, 1, most, ctypes.byref(n)) == 0
+    assert L.al_norm_backward_workspace_bytes(1, 1, 1, most + 1, ctypes.byref(n)) == 4
+    assert L.al_act_quantize(1, None, most, 0, most, 64, None, None, None) == 0
+    assert L.al_act_quantize(1, None, most, 0, most + 1, 64, None, None, None) == 4
