@@ -472,9 +472,11 @@ hipError_t forward_slab(bool layer, const NormForward& a, int64_t rows, hipStrea
         return hipGetLastError();
     }
     Shape s = row_shape(a.s.pitch / 8);
-    // bf16 rows of 1025 to 2048 columns: a wavefront each needs no barrier (8192 x 1100: 14.7 -> 9.8 us, 4096 x 2048 10.1 -> 8.7); with
-    // 8 chunks a lane (8192 x 4096) or fp32 there is nothing in it, or less
-    if (sizeof(T) == 2 && s.g == 256 && s.k == 1) s = {64, 4};
+    // bf16 rows of 1025 to 2048 columns: a wavefront each needs no barrier, but walks four chunks a lane one after another, which many rows
+    // hide and few do not (RMS with the code, a wavefront a row and a workgroup a row, us in a graph: 8192 x 1100 11.7 and 16.6, 4096 x 2048 7.9
+    // and 10.2, 2048 x 1032 5.1 and 5.5, 2048 x 1100 6.1 and 5.8, 2048 x 2048 5.8 and 5.9, 1024 x 1536 4.7 and 3.9, 1 x 2048 3.8 and 2.5).
+    // With 8 chunks a lane (8192 x 4096) or fp32 there is nothing in it, or less.
+    if (sizeof(T) == 2 && s.g == 256 && s.k == 1 && a.s.rows >= 2048) s = {64, 4};
     const dim3 n((uint32_t)(s.g == 64 ? (rows + 3) / 4 : rows));
     if (s.g == 64 && s.k == 1)
         norm_forward_kernel<T, 64, 1><<<n, 256, 0, st>>>(a, layer);
