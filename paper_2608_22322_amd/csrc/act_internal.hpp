@@ -13,8 +13,6 @@ namespace al {
 al_status api_fail(al_status s, const char* msg);
 void api_clear();
 
-int device_cu_count();
-
 // A matrix of the caller's dtype, one row per token.
 struct Mat {
     void* p;

@@ -482,8 +482,6 @@ hipError_t forward_slab(bool layer, const NormForward& a, int64_t rows, hipStrea
         norm_forward_kernel<T, 64, 1><<<n, 256, 0, st>>>(a, layer);
     else if (s.g == 64 && s.k == 2)
         norm_forward_kernel<T, 64, 2><<<n, 256, 0, st>>>(a, layer);
-    else if (s.g == 64 && s.k == 4)
-        norm_forward_kernel<T, 64, 4><<<n, 256, 0, st>>>(a, layer);
     else if (s.g == 256 && s.k == 1)
         norm_forward_kernel<T, 256, 1><<<n, 256, 0, st>>>(a, layer);
     else if (s.g == 256 && s.k == 2)
@@ -494,6 +492,8 @@ hipError_t forward_slab(bool layer, const NormForward& a, int64_t rows, hipStrea
         norm_forward_kernel<T, 512, 3><<<n, 512, 0, st>>>(a, layer);
     else if (s.g == 512 && s.k == 4)
         norm_forward_kernel<T, 512, 4><<<n, 512, 0, st>>>(a, layer);
+    if constexpr (sizeof(T) == 2)
+        if (s.g == 64 && s.k == 4) norm_forward_kernel<T, 64, 4><<<n, 256, 0, st>>>(a, layer);
     return hipGetLastError();
 }
 
