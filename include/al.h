@@ -470,6 +470,16 @@ al_status al_diag_levels(int32_t kind, const float* meta, int64_t nblocks, doubl
 #define AL_DIFF_NORMS_OUT 4098
 al_status al_diff_norms(const float* a, const float* b, int64_t n, double* out, void* stream);
 
+/* Diagnostic: how al_linear_wgrad cuts a product, a rule on its sizes alone:
+ * plan[0] = width of the tiles of outputs (64, 128 or 256), plan[1] = splits
+ * of the tokens (1: one launch), plan[2] = slabs that dy's sums are taken in,
+ * plan[3] = 1 where these are taken in the product's own launch, else 0. (Rows of dy
+ * that are 2^25 elements apart, or code rows of 2^26 bytes, are taken in
+ * 64-wide tiles with the same splits.) plan: host memory. No HIP call; the
+ * sizes that al_linear_wgrad refuses are refused. For tests that have to
+ * reach a kernel. */
+al_status al_diag_wgrad_plan(int32_t dtype, int64_t tokens, int64_t out_features, int64_t in_features, int32_t plan[4]);
+
 /* Diagnostic: streaming rates of the fused AdamW byte mix. Reads p (n fp32),
  * g (n bf16), m and v (n bytes each) and writes p, m, v with no optimizer
  * arithmetic. mode selects the access shape:

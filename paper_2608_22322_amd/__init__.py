@@ -86,7 +86,7 @@ EXPORTS = ("al_version", "al_last_error", "al_code_bytes", "al_meta_floats", "al
            "al_diag_levels", "al_diag_stream", "al_diff_norms", "al_synth_normal",
            "al_act_code_bytes", "al_act_exp_bytes", "al_act_quantize", "al_act_dequantize", "al_norm_forward",
            "al_norm_backward_workspace_bytes", "al_norm_backward", "al_swiglu_forward", "al_swiglu_backward",
-           "al_linear_wgrad_workspace_bytes", "al_linear_wgrad")
+           "al_linear_wgrad_workspace_bytes", "al_linear_wgrad", "al_diag_wgrad_plan")
 
 
 def lib():
@@ -137,6 +137,7 @@ def lib():
         L.al_swiglu_backward.argtypes = [i32, vp, i64, i64, i64, i32, vp, vp, vp, vp, vp, i64, vp, i64, vp, vp, vp]
         L.al_linear_wgrad_workspace_bytes.argtypes = [i32, i64, i64, i64, ctypes.POINTER(sz)]
         L.al_linear_wgrad.argtypes = [i32, vp, i64, vp, vp, i32, i64, i64, i64, vp, vp, i32, vp, vp, vp, vp, sz, vp]
+        L.al_diag_wgrad_plan.argtypes = [i32, i64, i64, i64, ctypes.POINTER(i32)]
         for name in ("al_quantize", "al_dequantize", "al_adamw_workspace_bytes", "al_adamw_step", "al_adamw_step_noalloc",
                      "al_adafactor_workspace_bytes",
                      "al_came_workspace_bytes", "al_adafactor_step", "al_came_step", "al_apollo_workspace_bytes",
@@ -144,7 +145,7 @@ def lib():
                      "al_diff_norms", "al_synth_normal",
                      "al_act_quantize", "al_act_dequantize", "al_norm_forward", "al_norm_backward_workspace_bytes",
                      "al_norm_backward", "al_swiglu_forward", "al_swiglu_backward", "al_linear_wgrad_workspace_bytes",
-                     "al_linear_wgrad"):
+                     "al_linear_wgrad", "al_diag_wgrad_plan"):
             getattr(L, name).restype = ctypes.c_int
         _lib = L
     return _lib

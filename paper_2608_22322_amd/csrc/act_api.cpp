@@ -317,6 +317,22 @@ al_status al_linear_wgrad_workspace_bytes(int32_t dtype, int64_t tokens, int64_t
     return AL_OK;
 }
 
+al_status al_diag_wgrad_plan(int32_t dtype, int64_t tokens, int64_t out_features, int64_t in_features, int32_t plan[4]) {
+    const char* const who = "al_diag_wgrad_plan";
+    al::api_clear();
+    if (!plan) return fail(AL_EINVAL, "%s: plan is NULL", who);
+    AL_TRY(check_dtype(dtype, who, "dtype"));
+    AL_TRY(check_shape(tokens, in_features, who));
+    AL_TRY(check_shape(tokens, out_features, who));
+    AL_TRY(check_product(out_features, in_features, who));
+    const al::WgradPlan p = al::wgrad_plan(dtype, tokens, out_features, in_features);
+    plan[0] = p.tile;
+    plan[1] = p.splits;
+    plan[2] = p.bparts;
+    plan[3] = p.beside;
+    return AL_OK;
+}
+
 al_status al_linear_wgrad(int32_t dtype, const void* dy, int64_t lddy, const void* codes, const void* exps,
                           int32_t block, int64_t tokens, int64_t out_features, int64_t in_features,
                           const float* gamma, const float* beta, int32_t grad_dtype, const void* base, void* dw,

@@ -72,3 +72,14 @@ def to_code(codes, exps, cols, block):
 
 def f64(t):
     return t.detach().to("cpu", torch.float64).numpy()
+
+
+def wgrad_plan(dtype, tokens, out, cols):
+    """(tile, splits, slabs, beside) that the library takes for a weight gradient; dtype: 0 fp32, 1 bf16."""
+    import ctypes
+
+    import paper_2608_22322_amd as al
+
+    plan = (ctypes.c_int32 * 4)()
+    al.check(al.lib().al_diag_wgrad_plan(dtype, tokens, out, cols, plan))
+    return plan[0], plan[1], plan[2], bool(plan[3])
