@@ -1,7 +1,7 @@
 """The weight gradient's 128- and 256-wide kernels, unsplit and split, with their joins and bias sums.
 
 Every size is checked against the library's plan, so that a change of the plan's model cannot take a kernel out of the tests. Results are
-exact: small integers, whose sums fp32 holds in any order.
+exact: small integers, whose sums fp32 holds in any order, and 24-bit numbers that meet one token each.
 """
 import numpy as np
 import pytest
@@ -58,6 +58,59 @@ def test_integers_are_exact(dtype, tokens, out, cols, tile, splits, beside):
         assert torch.equal(dw.double(), full) and torch.equal(db.double(), total)
         dw, db = _run(d, code, "bf16", gamma, beta, base.bfloat16(), bias=True)
         assert torch.equal(dw, full.float().bfloat16()) and torch.equal(db, total.float().bfloat16())
+
+
+def _parts(x):
+    """The three bf16 numbers that add up to an fp32 number, each the leading 8 bits of what the ones before it leave."""
+    parts = []
+    for _ in range(3):
+        h = (x.astype(np.float32).view(np.uint32) & 0xFFFF0000).view(np.float32)
+        parts.append(h)
+        x = x - h
+    assert not x.any()
+    return parts
+
+
+def _tokens_met(tokens, out, splits, rng):
+    """A token for each output row: the ends of every split and of the whole turns among them, then all in turn or by chance."""
+    steps = -(-tokens // 32)
+    ends = {0, tokens - 1, tokens // 32 * 32 - 1, tokens // 32 * 32}
+    for s in range(splits + 1):
+        ends |= {steps * s // splits * 32 + i for i in (-33, -32, -1, 0, 31, 32)}
+    ends = [t for t in sorted(ends) if 0 <= t < tokens][:out]
+    rest = rng.permutation(max(tokens, out)) % tokens
+    return rng.permutation(np.concatenate([ends, rest[: out - len(ends)]]).astype(np.int64))
+
+
+@pytest.mark.parametrize("dtype,tokens,out,cols,tile,splits,beside", CASES + [
+    ("f32", 60, 300, 200, 64, 1, False), ("f32", 100, 300, 200, 64, 2, True), ("f32", 2042, 33, 36, 64, 32, True),
+    ("f32", 512, 1024, 1024, 64, 3, True)],
+    ids=NAMES + ["f32-60-300-200", "f32-100-300-200", "f32-2042-33-36", "f32-512-1024-1024"])
+def test_each_output_from_one_token(dtype, tokens, out, cols, tile, splits, beside):
+    """Each column of dy has one number, its product with that token's codes is an output as it is. fp32 numbers have 24 bits, of
+    which each of the three parts holds some: one that is lost, doubled or from another turn shows."""
+    _planned(dtype, tokens, out, cols, tile, splits, beside)
+    rng = np.random.default_rng(tokens + out)
+    bits = rng.integers(1 << 7, 1 << 8, out) << 16  # leading 8 bits
+    if dtype == "f32":
+        bits += (rng.integers(1 << 7, 1 << 8, out) << 8) + rng.integers(0, 1 << 7, out) * 2 + 1
+    v = (np.ldexp(bits.astype(np.float64), rng.integers(-30, -10, out)) * rng.choice([-1, 1], out)).astype(np.float32)
+    if dtype == "f32":
+        assert all(p.all() for p in _parts(v))
+    met = _tokens_met(tokens, out, splits, rng)
+    dy = np.zeros((tokens, out), np.float32)
+    dy[met, np.arange(out)] = v
+    nb = -(-cols // 64)
+    codes = rng.choice([-1, 1], (tokens, nb * 64)).astype(np.int8)
+    codes[:, cols:] = 0
+    exps = rng.integers(118, 137, (tokens, nb)).astype(np.uint8)
+    sign = torch.from_numpy(codes[:, :cols]).cuda()[torch.from_numpy(met).cuda()].double()
+    step = np.ldexp(1.0, exps.astype(int) - 127)
+    scale = torch.from_numpy(step).cuda()[torch.from_numpy(met).cuda()].repeat_interleave(64, 1)[:, :cols]
+    want = torch.from_numpy(v).cuda().double()[:, None] * sign * scale
+    dw, db = _run(gpu(torch.from_numpy(dy).to(DT[dtype]), 3, 1), to_code(codes, exps, cols, 64), "f32", bias=True)
+    assert torch.equal(dw.double(), want)
+    assert torch.equal(db.cpu(), torch.from_numpy(v))
 
 
 @pytest.mark.parametrize("dtype,tokens,out,cols,tile,splits,beside", [
