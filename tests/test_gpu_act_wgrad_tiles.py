@@ -142,3 +142,38 @@ def test_values_that_are_no_numbers_stay_in_their_rows_and_columns(dtype, tokens
         keep[64 * b:64 * b + 64] = False
     sign = torch.from_numpy(np.sign(codes[tokens // 2, :cols]).astype(np.float32)).cuda()
     assert torch.equal(dw[out - 1][keep], (sign * float("inf"))[keep])
+
+
+@pytest.mark.parametrize("dtype,tokens,out,cols,tile,splits,beside", [
+    ("bf16", 97, 4100, 4200, 128, 1, False), ("f32", 277, 196, 4168, 128, 3, True)])
+def test_rows_of_dy_far_apart(dtype, tokens, out, cols, tile, splits, beside):
+    """A row pitch of more than 2^25 elements: a 128-wide plan, unsplit and split, taken by the 64-wide kernel in the plan's workspace."""
+    _planned(dtype, tokens, out, cols, tile, splits, beside)
+    ints, codes, exps, x = _integers(tokens, out, cols, 64, 9)
+    ld = (1 << 25) + 8
+    dy = torch.empty(tokens * ld, dtype=DT[dtype], device="cuda").view(tokens, ld)[:, 16:16 + out]
+    dy.copy_(ints)
+    dw, db = _run(dy, to_code(codes, exps, cols, 64), "f32", bias=True)
+    assert torch.equal(dw.double(), _product(ints, x)) and torch.equal(db.double(), ints.double().sum(0).cuda())
+    beta, base = torch.randint(-2, 3, (cols,)).float().cuda(), torch.randint(-9, 10, (out, cols)).float().cuda()
+    dw, _ = _run(dy, to_code(codes, exps, cols, 64), "f32", beta=beta, base=base)
+    assert torch.equal(dw.double(), _product(ints, x) + ints.double().sum(0).cuda()[:, None] * beta.double() + base.double())
+
+
+def test_code_rows_far_apart():
+    """Code rows of 2^26 bytes, 2^33 outputs: a 128-wide plan taken by the 64-wide kernel."""
+    from paper_2608_22322_amd import activations as act
+
+    tokens, out, cols = 3, 128, 1 << 26
+    _planned("bf16", tokens, out, cols, 128, 1, False)
+    g = torch.Generator(device="cuda").manual_seed(2)
+    codes = torch.randint(-8, 9, (tokens, cols), dtype=torch.int8, device="cuda", generator=g)
+    exps = torch.full((tokens, cols // 64), 127, dtype=torch.uint8, device="cuda")
+    dy = torch.randint(-4, 5, (tokens, out), device="cuda", generator=g).bfloat16()
+    code, dw = act.ActCode(codes, exps, tokens, cols, 64), torch.empty(out, cols, dtype=torch.bfloat16, device="cuda")
+    ws = torch.empty(act.linear_wgrad_workspace_bytes(dy, code, dw), dtype=torch.uint8, device="cuda")
+    act.linear_wgrad(dy, code, dw, ws)
+    step = 1 << 22
+    for c in range(0, cols, step):
+        want = torch.mm(dy.float().t().contiguous(), codes[:, c:c + step].float())  # integers up to 96
+        assert torch.equal(dw[:, c:c + step].float(), want), c
