@@ -422,7 +422,8 @@ al_status al_linear_wgrad_workspace_bytes(int32_t dtype, int64_t tokens, int64_t
  * out_features x in_features of grad_dtype; base NULL = 0, base may be dw
  * itself (gradient accumulation). dbias: out_features values of grad_dtype or
  * NULL. The products are exact (both factors are bf16 numbers, an fp32 dy is three
- * of them) and summed in fp32 on the matrix cores. tokens == 0: dw = base, dbias = 0.
+ * of them but for bits below 2^-133, which are dropped) and summed in fp32 on the
+ * matrix cores. tokens == 0: dw = base, dbias = 0.
  * out_features below 2^22, in_features below 2^29, at most 2^38 weights (AL_EUNSUPPORTED otherwise).
  * One launch where the outputs fill the device (beta or dbias take two more); fewer
  * outputs split the tokens, and a second launch adds the parts, and up to 16384

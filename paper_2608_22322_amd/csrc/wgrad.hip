@@ -2,8 +2,8 @@
 // cores: dw[n][k] = sum over tokens t of dy[t][n] xhat[t][k].
 //
 // Both factors are bf16 numbers (a code is 7 bits and a sign times a power of two; an
-// fp32 dy is the sum of three bf16 numbers, taken in three turns), so every
-// product is exact and the sums are the matrix cores' fp32 ones. A workgroup
+// fp32 dy is the sum of three bf16 numbers, taken in three turns, but for bits below bf16's
+// smallest number, 2^-133), so every product is exact and the sums are the matrix cores' fp32 ones. A workgroup
 // decodes each code once, on its way to LDS (2.5 instructions a value: convert a
 // byte, multiply, pack; the fragments' readers would do it twice or four times).
 #include <algorithm>
@@ -34,7 +34,7 @@ constexpr int64_t kBeside = 16384;  // most tokens at which a split product's la
 
 __device__ __forceinline__ int edge_at(int t, int c) { return t * kEdge + ((((c >> 4) ^ ((t >> 1) & 3)) << 4) | (c & 15)); }
 
-// The bf16 part `which` (0, 1, 2) of fp32 values: x = x0 + x1 + x2 exactly, by truncation; infinities and NaN
+// The bf16 part `which` (0, 1, 2) of fp32 values: x = x0 + x1 + x2 down to bits of 2^-133, by truncation; infinities and NaN
 // are in part 0 alone.
 __device__ __forceinline__ uint32_t split_part(uint32_t x, int which) {
     const bool fin = (x & 0x7f800000u) != 0x7f800000u;
