@@ -73,9 +73,11 @@ class SwigluMLP:
         """Bytes that a batch keeps between its forward and its backward pass."""
         return self.xhat.nbytes() + self.gate_code.nbytes() + self.up_code.nbytes() + 4 * self.tokens
 
-    def bf16_bytes(self) -> int:
-        """What the same pass keeps in bf16: x, n, gate, up and h."""
-        return 2 * self.tokens * (2 * self.hidden + 3 * self.ffn) + 4 * self.tokens
+    def bf16_bytes(self, recompute: bool = False) -> int:
+        """What a pass in bf16 keeps: x, n, gate, up and h; with `recompute` (as here, n and h again in the backward pass) x, gate
+        and up."""
+        kept = self.hidden + 2 * self.ffn + (0 if recompute else self.hidden + self.ffn)
+        return 2 * self.tokens * kept + 4 * self.tokens
 
     @_on_its_gpu
     def forward(self, x):
@@ -131,7 +133,8 @@ def main():
         ap.add_argument("--" + name, type=int, default=value)
     a = ap.parse_args()
     net, losses = train(a.hidden, a.ffn, a.tokens, a.steps, a.block)
-    print("saved for the backward pass: %.1f MiB (%.1f MiB in bf16)" % (net.saved_bytes() / 2**20, net.bf16_bytes() / 2**20))
+    print("saved for the backward pass: %.1f MiB (in bf16 %.1f MiB with the same recomputation, %.1f MiB without)"
+          % tuple(n / 2**20 for n in (net.saved_bytes(), net.bf16_bytes(recompute=True), net.bf16_bytes())))
     print("loss: %.5f -> %.5f in %d steps" % (losses[0], losses[-1], len(losses)))
 
 

@@ -34,3 +34,18 @@ def test_size_queries_and_calls_agree_on_the_widest_row():
     assert L.al_norm_backward_workspace_bytes(1, 1, 1, most + 1, ctypes.byref(n)) == 4
     assert L.al_act_quantize(1, None, most, 0, most, 64, None, None, None) == 0
     assert L.al_act_quantize(1, None, most, 0, most + 1, 64, None, None, None) == 4
+
+
+def test_what_a_block_keeps():
+    """Bytes between the passes of the MLP block, by hand: 2048 tokens at 2048 / 5632."""
+    from types import SimpleNamespace
+
+    from paper_2608_22322_amd.mlp import SwigluMLP
+
+    net = object.__new__(SwigluMLP)
+    net.hidden, net.ffn, net.tokens = 2048, 5632, 2048
+    net.xhat, net.gate_code, net.up_code = (SimpleNamespace(nbytes=lambda c=c: act.code_bytes(2048, c, 64)) for c in (2048, 5632, 5632))
+    assert net.saved_bytes() == 2048 * (2048 + 2 * 5632) * 65 // 64 + 4 * 2048
+    assert net.bf16_bytes(recompute=True) == 2 * 2048 * (2048 + 2 * 5632) + 4 * 2048  # x, gate, up
+    assert net.bf16_bytes() == 2 * 2048 * (2 * 2048 + 3 * 5632) + 4 * 2048  # and n, h
+    assert 0.5 < net.saved_bytes() / net.bf16_bytes(recompute=True) < 0.51
