@@ -41,7 +41,7 @@
  * the caller, except that tensor lists and config structs are host memory
  * read during the call. The library keeps no pointer after a call returns.
  * All device work is enqueued on `stream` (a hipStream_t; NULL = the null
- * stream) in order; calls return without synchronizing. The library never
+ * stream) of the current device, whose memory the pointers are, in order; calls return without synchronizing. The library never
  * allocates device memory: each step takes a caller workspace whose size the
  * matching *_workspace_bytes query returns. Calls on distinct streams with
  * distinct buffers may run concurrently; calls that share a workspace or
@@ -362,7 +362,8 @@ al_status al_act_dequantize(const void* codes, const void* exps, int64_t rows, i
  * biased variance about the mean (AL_NORM_RMS: mean = 0, var = the mean
  * square), y = xhat gamma + beta. gamma, beta: cols floats, NULL = 1 and 0;
  * beta only for AL_NORM_LAYER. x and y have dtype; y may be x itself (same
- * ld). eps >= 0; a row without variance needs eps > 0. mean (AL_NORM_LAYER only, else NULL) and rstd: rows floats, NULL where not
+ * ld). eps >= 0, taken as fp32; a row without variance needs eps > 0, and a row whose squares add up to
+ * more than fp32 holds has rstd = 0. mean (AL_NORM_LAYER only, else NULL) and rstd: rows floats, NULL where not
  * wanted. codes, exps: the E8 code of xhat, both NULL where it is not saved
  * (block is then ignored). xhat is what a backward pass needs of x, and a
  * linear layer that reads y needs nothing else either (al_linear_wgrad). */

@@ -131,7 +131,7 @@ __device__ __forceinline__ void finish4(const Wgrad& a, int64_t n, int k, int in
 
 // The shape of the products, M x M. 16 x 16 x 32 takes more cycles than 32 x 32 x 16 and keeps a higher clock (8192 tokens and
 // features: 1.85M cycles at 2.13 GHz against 1.74M at 1.92 GHz), so bf16 dy takes it; fp32 dy, whose staging needs the
-// registers that fewer fragments in flight leave, takes 32 x 32 x 16 (4096^3: 842 and 400 us).
+// registers that fewer fragments in flight leave, takes 32 x 32 x 16 (4096^3: 842 and 414 us).
 template <int M>
 struct Product;
 template <>
@@ -599,9 +599,9 @@ hipError_t run(Wgrad a, hipStream_t st) {
 //   a turn of a workgroup alone on its compute unit takes `alone`, of as many as fit beside each other `each` per workgroup;
 //   starting and ending take as long as `ends` turns; fp32 dy takes 3 turns for one, each 10% longer; joining takes a launch
 //   and the partial products' way out and back.
-// Measured: 8192 tokens, 11008 x 4096: 256-wide 651, 128-wide 854; 2048 x 2048: 256-wide 4 splits 78, 128-wide 3 splits 93; 1024 x
-// 1024: 128-wide 8 splits 35, 256-wide 12 splits 37; 6001 tokens, 256 x 2048: 64-wide 8 splits 24, 128-wide 12 splits 27; 512 tokens,
-// 1024 x 1024: 64-wide 9, 128-wide 13, 64-wide 2 splits 13.
+// Measured, the choice first: 8192 tokens, 11008 x 4096: 256-wide 651, 128-wide 836; 2048 x 2048: 256-wide 4 splits 78, 128-wide 3 splits 93;
+// 1024 x 1024: 128-wide 8 splits 35, 256-wide 12 splits 38; 6001 tokens, 256 x 2048: 64-wide 6 splits 24.2 (8 splits 23.7), 128-wide 16 splits
+// 25.4; 512 tokens, 1024 x 1024: 64-wide 8.6, 128-wide 13, 64-wide 2 splits 13.
 WgradPlan wgrad_plan(int dtype, int64_t tokens, int64_t out, int64_t in) {
     static constexpr struct {
         int tile, fit, ends;
