@@ -45,6 +45,17 @@ __device__ __forceinline__ float group_sum(float v, float* buf) {
     return v;
 }
 
+// The same sum in the order of a wavefront that holds the row's G / 64 chunks a lane: each lane's chunks first, then the lanes. buf: G floats.
+template <int G>
+__device__ __forceinline__ float group_sum_by_lane(float v, float* buf) {
+    buf[threadIdx.x] = v;
+    __syncthreads();
+    v = 0.0f;
+#pragma unroll
+    for (int w = 0; w < G / 64; ++w) v += buf[w * 64 + (threadIdx.x & 63)];
+    return wave_sum(v);
+}
+
 __device__ __forceinline__ float sum8(const float (&v)[8]) {
     return ((v[0] + v[1]) + (v[2] + v[3])) + ((v[4] + v[5]) + (v[6] + v[7]));
 }
@@ -55,10 +66,16 @@ __device__ __forceinline__ int inside(int c, int cols) { return min(8, max(0, co
 template <typename T, int G, int K>
 __global__ __launch_bounds__(G < 256 ? 256 : G) void norm_forward_kernel(NormForward a, bool layer) {
     constexpr int R = G < 256 ? 256 / G : 1;  // rows per workgroup
-    __shared__ float buf[2][16];
+    // widths of which many rows take a wavefront each and few a workgroup: a row's bits do not depend on their number
+    constexpr bool BY_LANE = sizeof(T) == 2 && G == 256 && K == 1;
+    __shared__ float buf[2][BY_LANE ? G : 16];
     const int lane = threadIdx.x % G, cols = a.s.cols;
     const int64_t row = a.row0 + (int64_t)blockIdx.x * R + threadIdx.x / G;
     if (row >= a.s.rows) return;  // a whole group
+    const auto row_sum = [&](float v, float* b) {
+        if constexpr (BY_LANE) return group_sum_by_lane<G>(v, b);
+        else return group_sum<G>(v, b);
+    };
     const T* const x = static_cast<const T*>(a.x.p) + row * a.x.ld;
     Chunk<T> raw[K];
 #pragma unroll
@@ -71,7 +88,7 @@ __global__ __launch_bounds__(G < 256 ? 256 : G) void norm_forward_kernel(NormFor
     }
     float mean = 0.0f;
     if (layer) {
-        mean = group_sum<G>(sum, buf[0]) / (float)cols;
+        mean = row_sum(sum, buf[0]) / (float)cols;
 #pragma unroll
         for (int k = 0; k < K; ++k) {
             const int n = inside((k * G + lane) * 8, cols);
@@ -87,7 +104,7 @@ __global__ __launch_bounds__(G < 256 ? 256 : G) void norm_forward_kernel(NormFor
         for (int j = 0; j < 8; ++j) t[j] = v[k][j] * v[k][j];
         sq += sum8(t);
     }
-    const float rstd = 1.0f / sqrtf(group_sum<G>(sq, buf[1]) / (float)cols + a.eps);
+    const float rstd = 1.0f / sqrtf(row_sum(sq, buf[1]) / (float)cols + a.eps);
     if (lane == 0) {
         if (a.mean) a.mean[row] = mean;
         if (a.rstd) a.rstd[row] = rstd;

@@ -37,3 +37,21 @@ def test_forward(rows, cols, kind):
     d = x.cuda()
     act.norm_forward(act.LAYER if layer else act.RMS, d, d, gamma=gamma.cuda(), beta=beta.cuda() if layer else None, eps=eps)
     assert torch.equal(d, y)
+
+
+@pytest.mark.parametrize("kind", ["layer", "rms"])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("cols", [64, 1025, 1100, 1536, 2048, 4096])
+def test_a_row_gives_the_same_bits_among_many_rows_and_few(cols, dtype, kind):
+    from paper_2608_22322_amd import activations as act
+
+    rows, few, layer = 2100, 33, kind == "layer"
+    x, gamma, beta = _inputs(rows, cols, dtype, cols)
+    res = []
+    for d in (x.cuda(), x[:few].cuda()):
+        n = d.shape[0]
+        y, mean, rstd, code = torch.empty_like(d), torch.zeros(n, device="cuda"), torch.zeros(n, device="cuda"), act.alloc_code(n, cols)
+        act.norm_forward(act.LAYER if layer else act.RMS, d, y, mean if layer else None, rstd, gamma=gamma.cuda(),
+                         beta=beta.cuda() if layer else None, code=code)
+        res.append((y[:few], mean[:few], rstd[:few], code.codes[:few], code.exps[:few]))
+    assert all(torch.equal(p, q) for p, q in zip(*res))
