@@ -56,8 +56,8 @@
  * are not detected; their codes are unspecified.
  *
  * Alignment. Every device pointer must be 16-byte aligned (AL_EALIGN), except
- * the activation matrices of the al_act_*, al_norm_*, al_swiglu_* and
- * al_linear_wgrad calls (see there).
+ * the matrices of the al_act_*, al_norm_*, al_swiglu_*, al_linear_wgrad and
+ * al_orthogonalize calls (see there).
  */
 #ifndef AL_H
 #define AL_H
@@ -317,6 +317,60 @@ al_status al_apollo_workspace_bytes(const al_apollo_tensor* tensors, int32_t nt,
  * workspace of at least the queried size, 256-byte aligned. */
 al_status al_apollo_step(const al_apollo_tensor* tensors, int32_t nt, const al_apollo_cfg* cfg, int64_t step,
                          void* ws, size_t ws_bytes, void* stream);
+
+/* ------------------------------------------------------------------------
+ * Orthogonalised updates. O(G) replaces the singular values of a matrix by
+ * numbers near 1, by products alone (Newton-Schulz):
+ *   X = G / (|G| + eps), |G| the Frobenius norm, then `steps` times
+ *   X <- a X + (b A + c A A) X, A = X X^T        (rows <= cols)
+ *   X <- a X + X (b A + c A A), A = X^T X        (rows > cols).
+ * A zero matrix gives zeros (also with eps = 0), one that holds an infinity or a NaN gives NaN.
+ * parts: what X, A and b A + c A A are held in between the products, whose
+ * sums are fp32: 1 = one fp16 number each (11 bits: the result is about 1.4e-3 off for normal matrices, 3e-3 where singular values
+ * fall as 1 / k), 2 = the sum of two (22 bits, 3e-7 and 5e-7; three products for one). |G| is a binary64 sum in a fixed order:
+ * every result repeats bit for bit.
+ * a, b, c: for singular values of at most 1 to begin with, those of X must stay within 4 and those of b A + c A A within
+ * 128 (AL_EINVAL; a = 3.4445, b = -4.7750, c = 2.0315 are usual). steps: 1 to 64.
+ * rows, cols up to 2^21, the smaller of them up to 2^16 (AL_EUNSUPPORTED). */
+typedef struct al_ortho_cfg {
+    double a, b, c, eps;
+    int32_t steps, parts;
+} al_ortho_cfg;
+
+/* Workspace bytes of al_orthogonalize. */
+al_status al_orthogonalize_workspace_bytes(int64_t rows, int64_t cols, const al_ortho_cfg* cfg, size_t* bytes);
+
+/* out = O(x), x of dtype and out of out_dtype (al_dtype): rows x cols, element (i, j) at i * ld + j, any alignment of the element
+ * type and any ld >= cols (ignored for rows <= 1). out may be x itself (same type and ld); they must not overlap otherwise. ws: at least
+ * the queried bytes, 256-byte aligned. */
+al_status al_orthogonalize(int32_t dtype, const void* x, int64_t ldx, int64_t rows, int64_t cols, const al_ortho_cfg* cfg, int32_t out_dtype,
+                           void* out, int64_t ldout, void* ws, size_t ws_bytes, void* stream);
+
+/* The step of a matrix by its orthogonalised momentum (the Muon optimizer):
+ *   m = fl32(beta m + (1 - beta) g), u = m or, with nesterov, fl32(beta m + (1 - beta) g),
+ *   param = fl32(param (1 - lr wd) - lr s O(u))
+ * in binary64 but for O (ortho), whose result is fp32; m is coded as m (UF8, block 256) or kept as FP32, and u is formed from m before it
+ * is coded. s by `scale`: 0 = 1, 1 = sqrt(max(1, rows / cols)), 2 = 0.2 sqrt(max(rows, cols)) (the RMS of an AdamW update). */
+typedef enum al_muon_scale { AL_MUON_SCALE_NONE = 0, AL_MUON_SCALE_SPECTRAL = 1, AL_MUON_SCALE_RMS = 2 } al_muon_scale;
+typedef struct al_muon_cfg {
+    double lr, beta, weight_decay;
+    al_ortho_cfg ortho;
+    int32_t nesterov, scale;
+    int32_t grad_dtype;
+    int32_t reserved;
+    al_state_spec m;
+} al_muon_cfg;
+
+/* Workspace size (bytes) that al_muon_step needs for this tensor list and config. A part of a list never needs more than the list.
+ * Tensors of one shape are stepped together, up to 64 of them and 2^26 elements at a time (one at least): an fp32 update of each, X twice and A and
+ * b A + c A A, 2 or 4 bytes an element, sides padded to multiples of 64. */
+al_status al_muon_workspace_bytes(const al_tensor* tensors, int32_t nt, const al_muon_cfg* cfg, size_t* bytes);
+
+/* One step over nt matrices (rows, cols >= 1; a list's 1-D tensors, embedding and head take al_adamw_step). Uses per tensor: param, grad, m, m_meta;
+ * the other slots must be NULL, and no two tensors may share memory. step: the 1-based step count, which the update does not depend on. Per shape: the momentum pass (which also sums the squares of u),
+ * the norm, u into 16-bit parts, and three products a step of O, the last of which ends in the parameters. ws: device workspace
+ * of at least the queried size, 256-byte aligned. */
+al_status al_muon_step(const al_tensor* tensors, int32_t nt, const al_muon_cfg* cfg, int64_t step, void* ws, size_t ws_bytes, void* stream);
 
 /* ------------------------------------------------------------------------
  * Activations in 8 bits, and the operators that save and use them: the code
