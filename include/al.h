@@ -488,6 +488,55 @@ al_status al_linear_wgrad(int32_t dtype, const void* dy, int64_t lddy, const voi
                           const float* gamma, const float* beta, int32_t grad_dtype, const void* base, void* dw,
                           void* dbias, void* ws, size_t ws_bytes, void* stream);
 
+/* ------------------------------------------------------------------------
+ * The two ends of a token model: the lookup of embeddings and its gradient,
+ * and softmax cross entropy of a linear head with its gradients. Matrices as
+ * for the activations above, except that a matrix of the products (w) has 16-byte
+ * aligned rows of bf16; weight gradients are packed, in the types the optimizer steps read.
+ *
+ * Token ids and targets: tokens values of index_dtype, one behind the other. An
+ * id or a target below 0 or from vocab on stands for no token: its embedding is zero, and it takes part in no loss and no
+ * gradient, whatever its row holds.
+ *
+ * Sums are fp32 and independent of scheduling: every result repeats bit for
+ * bit. tokens up to 2^31 - 1, vocab up to 2^31 - 1. */
+typedef enum al_index { AL_INDEX_I32 = 0, AL_INDEX_I64 = 1 } al_index;
+
+/* out[t] = scale table[ids[t]], in fp32, rounded once to out_dtype. table:
+ * vocab x cols of table_dtype, out: tokens x cols. */
+al_status al_embed_forward(int32_t table_dtype, const void* table, int64_t ldtable, int64_t vocab, int64_t cols, int32_t index_dtype,
+                           const void* ids, int64_t tokens, double scale, int32_t out_dtype, void* out, int64_t ldout, void* stream);
+
+/* Workspace bytes of al_embed_backward: the sorted tokens, and sums of every 128 of them. */
+al_status al_embed_backward_workspace_bytes(int64_t tokens, int64_t vocab, int64_t cols, size_t* bytes);
+
+/* Gradient of the table: dw[v] = base[v] + scale * sum of dy[t] over the tokens t with ids[t] = v, in the order of the tokens.
+ * dy: tokens x cols of dtype. base, dw: packed vocab x cols of grad_dtype, 16-byte aligned; base NULL = 0, base may be dw itself
+ * (gradient accumulation, or a head's gradient where the table is tied: then rows without a token are not touched). ws: at least the
+ * queried bytes, 256-byte aligned. The tokens are sorted by id (runs of 4096, then merged: one launch for every doubling), sums over
+ * 128 sorted tokens of one id are taken apart from the rows, and each row is written once. */
+al_status al_embed_backward(int32_t dtype, const void* dy, int64_t lddy, int32_t index_dtype, const void* ids, int64_t tokens, int64_t vocab,
+                            int64_t cols, double scale, int32_t grad_dtype, const void* base, void* dw, void* ws, size_t ws_bytes, void* stream);
+
+/* Workspace bytes of al_linear_xent; dh, dw: whether these gradients are wanted. */
+al_status al_linear_xent_workspace_bytes(int64_t tokens, int64_t hidden, int64_t vocab, int64_t ldw, int32_t want_dh, int32_t dh_dtype,
+                                         int32_t want_dw, int32_t grad_dtype, size_t* bytes);
+
+/* Softmax cross entropy of logits = h w^T (h: tokens x hidden, w: vocab x hidden, both bf16) against target, with its gradients, without
+ * a tokens x vocab matrix:
+ *   lse[t] = log sum over v of exp(logit[t][v]),  loss[t] = lse[t] - logit[t][target[t]]
+ *   d[t][v] = scale weight[t] (exp(logit[t][v] - lse[t]) - [v = target[t]])
+ *   dh = d w,  dw = d^T h + base                  (of scale * sum over t of weight[t] loss[t])
+ * loss, lse: tokens floats, 0 for a token without a target, NULL where not wanted. weight: tokens floats, NULL = 1. dh: tokens x hidden of
+ * dh_dtype; base, dw: packed vocab x hidden of grad_dtype, 16-byte aligned, base NULL = 0, base may be dw itself (dw NULL: base too); NULL where not wanted.
+ * Products of bf16 numbers with fp32 sums; d is rounded to bf16 for a bf16 gradient and to the sum of two bf16 numbers (16 bits) for an fp32
+ * one. Logits are taken once for the losses and, where a gradient is wanted, again, a piece of the vocabulary at a time: the workspace holds 2^26
+ * elements of d (256 columns at least) and, with several pieces, dh in fp32. w: 16-byte aligned; ldw or hidden that is no multiple of 8 costs a copy of w in the
+ * workspace. tokens * vocab up to 2^38, tokens * hidden and vocab * hidden up to 2^34, each of them up to 2^24 (AL_EUNSUPPORTED). */
+al_status al_linear_xent(const void* h, int64_t ldh, const void* w, int64_t ldw, int64_t tokens, int64_t hidden, int64_t vocab,
+                         int32_t index_dtype, const void* target, const float* weight, double scale, float* loss, float* lse, int32_t dh_dtype, void* dh,
+                         int64_t lddh, int32_t grad_dtype, const void* base, void* dw, void* ws, size_t ws_bytes, void* stream);
+
 /* Diagnostic: evaluate, elementwise on the device, a math primitive the
  * codes rely on, so tests can bound it against the host: fn 0 = hardware
  * fp32 log2 of (float)x (the fast code position uses it on mantissas in

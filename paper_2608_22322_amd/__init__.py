@@ -98,7 +98,8 @@ EXPORTS = ("al_version", "al_last_error", "al_code_bytes", "al_meta_floats", "al
            "al_act_code_bytes", "al_act_exp_bytes", "al_act_quantize", "al_act_dequantize", "al_norm_forward",
            "al_norm_backward_workspace_bytes", "al_norm_backward", "al_swiglu_forward", "al_swiglu_backward",
            "al_linear_wgrad_workspace_bytes", "al_linear_wgrad", "al_diag_wgrad_plan",
-           "al_orthogonalize_workspace_bytes", "al_orthogonalize", "al_muon_workspace_bytes", "al_muon_step")
+           "al_orthogonalize_workspace_bytes", "al_orthogonalize", "al_muon_workspace_bytes", "al_muon_step",
+           "al_embed_forward", "al_embed_backward_workspace_bytes", "al_embed_backward", "al_linear_xent_workspace_bytes", "al_linear_xent")
 
 
 def lib():
@@ -154,6 +155,12 @@ def lib():
         L.al_orthogonalize.argtypes = [i32, vp, i64, i64, i64, ctypes.POINTER(OrthoCfg), i32, vp, i64, vp, sz, vp]
         L.al_muon_workspace_bytes.argtypes = [ctypes.POINTER(Tensor), i32, ctypes.POINTER(MuonCfg), ctypes.POINTER(sz)]
         L.al_muon_step.argtypes = [ctypes.POINTER(Tensor), i32, ctypes.POINTER(MuonCfg), i64, vp, sz, vp]
+        d = ctypes.c_double
+        L.al_embed_forward.argtypes = [i32, vp, i64, i64, i64, i32, vp, i64, d, i32, vp, i64, vp]
+        L.al_embed_backward_workspace_bytes.argtypes = [i64, i64, i64, ctypes.POINTER(sz)]
+        L.al_embed_backward.argtypes = [i32, vp, i64, i32, vp, i64, i64, i64, d, i32, vp, vp, vp, sz, vp]
+        L.al_linear_xent_workspace_bytes.argtypes = [i64, i64, i64, i64, i32, i32, i32, i32, ctypes.POINTER(sz)]
+        L.al_linear_xent.argtypes = [vp, i64, vp, i64, i64, i64, i64, i32, vp, vp, d, vp, vp, i32, vp, i64, i32, vp, vp, vp, sz, vp]
         for name in ("al_quantize", "al_dequantize", "al_adamw_workspace_bytes", "al_adamw_step", "al_adamw_step_noalloc",
                      "al_adafactor_workspace_bytes",
                      "al_came_workspace_bytes", "al_adafactor_step", "al_came_step", "al_apollo_workspace_bytes",
@@ -162,7 +169,9 @@ def lib():
                      "al_act_quantize", "al_act_dequantize", "al_norm_forward", "al_norm_backward_workspace_bytes",
                      "al_norm_backward", "al_swiglu_forward", "al_swiglu_backward", "al_linear_wgrad_workspace_bytes",
                      "al_linear_wgrad", "al_diag_wgrad_plan",
-                     "al_orthogonalize_workspace_bytes", "al_orthogonalize", "al_muon_workspace_bytes", "al_muon_step"):
+                     "al_orthogonalize_workspace_bytes", "al_orthogonalize", "al_muon_workspace_bytes", "al_muon_step",
+                     "al_embed_forward", "al_embed_backward_workspace_bytes", "al_embed_backward", "al_linear_xent_workspace_bytes",
+                     "al_linear_xent"):
             getattr(L, name).restype = ctypes.c_int
         _lib = L
     return _lib

@@ -183,7 +183,7 @@ struct MmCore {
             bn.renew();
             multiply(as, bs);
         };
-        load(t0, as0, bs0);
+        if (t0 < t1) load(t0, as0, bs0);
         int t = t0;
         for (; t + 1 < t1; t += 2) {
             turn(t, as0, bs0, as1, bs1);
@@ -218,7 +218,12 @@ __device__ __forceinline__ MmId mm_id(const Mm& p) {
     return t;
 }
 
-// E: end(batch, row, first column, 4 sums, mirror) writes 4 neighbouring outputs (and, where mirror, those across the diagonal).
+// E: end(batch, row, first column, 4 sums, mirror) takes 4 neighbouring outputs (mirror: for those across the diagonal too). One with E::kRows takes a wavefront's
+// row instead, end.row<FN>(row, first column of its part, lane, sums), and no splits.
+template <class E, class = void>
+struct MmRows : std::false_type {};
+template <class E>
+struct MmRows<E, std::enable_if_t<E::kRows>> : std::true_type {};
 template <class T, int B, bool AK, bool BK, bool ENDS, class E>
 __global__ __launch_bounds__(MmTile<B>::kThreads, B == 64 ? 4 : 2) void mm_kernel(Mm p, E end) {
     typedef MmTile<B> G;
@@ -241,8 +246,14 @@ __global__ __launch_bounds__(MmTile<B>::kThreads, B == 64 ? 4 : 2) void mm_kerne
 #pragma unroll
     for (int i = 0; i < G::FM; ++i) {
         __builtin_amdgcn_sched_barrier(0);
+        if constexpr (MmRows<E>::value) {
+            end.template row<G::FN>(m + 16 * i, n, lane, acc[i]);
+            continue;
+        }
 #pragma unroll
-        for (int j = 0; j < G::FN; ++j) end(id.batch, m + 16 * i, n + 16 * j, acc[i][j], p.sym && id.m != id.n);
+        for (int j = 0; j < G::FN; ++j) {
+            if constexpr (!MmRows<E>::value) end(id.batch, m + 16 * i, n + 16 * j, acc[i][j], p.sym && id.m != id.n);
+        }
     }
 }
 
@@ -286,7 +297,8 @@ hipError_t mm_launch(const Mm& p, const E& end, hipStream_t st) {
     const uint32_t tiles = MmTile<B>::tiles(p);
     if (tiles == 0) return hipSuccess;
     mm_kernel<T, B, AK, BK, ENDS, E><<<tiles * (uint32_t)(p.batches * p.splits), MmTile<B>::kThreads, 0, st>>>(p, end);
-    if (p.splits > 1) mm_join_kernel<B, E><<<tiles * (uint32_t)p.batches * (B * B / 1024), 256, 0, st>>>(p, end, tiles);
+    if constexpr (!MmRows<E>::value)
+        if (p.splits > 1) mm_join_kernel<B, E><<<tiles * (uint32_t)p.batches * (B * B / 1024), 256, 0, st>>>(p, end, tiles);
     return hipGetLastError();
 }
 
