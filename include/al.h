@@ -507,14 +507,14 @@ typedef enum al_index { AL_INDEX_I32 = 0, AL_INDEX_I64 = 1 } al_index;
 al_status al_embed_forward(int32_t table_dtype, const void* table, int64_t ldtable, int64_t vocab, int64_t cols, int32_t index_dtype,
                            const void* ids, int64_t tokens, double scale, int32_t out_dtype, void* out, int64_t ldout, void* stream);
 
-/* Workspace bytes of al_embed_backward: the sorted tokens, and sums of every 128 of them. */
+/* Workspace bytes of al_embed_backward: the sorted tokens, and sums of every 32 of them. */
 al_status al_embed_backward_workspace_bytes(int64_t tokens, int64_t vocab, int64_t cols, size_t* bytes);
 
 /* Gradient of the table: dw[v] = base[v] + scale * sum of dy[t] over the tokens t with ids[t] = v, in the order of the tokens.
  * dy: tokens x cols of dtype. base, dw: packed vocab x cols of grad_dtype, 16-byte aligned; base NULL = 0, base may be dw itself
  * (gradient accumulation, or a head's gradient where the table is tied: then rows without a token are not touched). ws: at least the
- * queried bytes, 256-byte aligned. The tokens are sorted by id (runs of 4096, then merged: one launch for every doubling), sums over
- * 128 sorted tokens of one id are taken apart from the rows, and each row is written once. */
+ * queried bytes, 256-byte aligned. The tokens are sorted by id (runs of 1024, then up to 64 of them merged in a launch), sums over
+ * 32 sorted tokens of one id are taken apart from the rows, and each row is written once. */
 al_status al_embed_backward(int32_t dtype, const void* dy, int64_t lddy, int32_t index_dtype, const void* ids, int64_t tokens, int64_t vocab,
                             int64_t cols, double scale, int32_t grad_dtype, const void* base, void* dw, void* ws, size_t ws_bytes, void* stream);
 

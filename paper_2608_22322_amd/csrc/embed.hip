@@ -36,142 +36,257 @@ __global__ __launch_bounds__(256) void lookup_kernel(Mat table, Ids ids, int64_t
 
 constexpr uint64_t kNoToken = ~uint64_t(0);
 
-// Runs of kSortRun keys (id, token), each sorted by a workgroup in LDS (a bitonic network; keys differ, so their order is one). Ids outside the table come last.
-__global__ __launch_bounds__(1024) void sort_kernel(Ids ids, int64_t tokens, int64_t vocab, uint64_t* keys) {
-    __shared__ uint64_t s[kSortRun];
+// Runs of kSortRun keys (id, token), each sorted by a workgroup with a bitonic network. Ids outside the table come last. A lane holds 4 neighbouring keys, a
+// wavefront 256: of the 55 steps 52 exchange within a wavefront, without a barrier. Up to 2^22 - 1 ids a key is 32 bits (the id, the place in the run).
+// The steps are a loop: unrolled, one workgroup's time is the fetching of its instructions (8192 tokens 13.8 us, exchanged by DPP moves 24.9).
+__device__ __forceinline__ uint32_t either(uint32_t x, uint32_t y, bool least) { return least ? std::min(x, y) : std::max(x, y); }
+__device__ __forceinline__ uint64_t either(uint64_t x, uint64_t y, bool least) { return (x < y) == least ? x : y; }
+__device__ __forceinline__ uint32_t from_lane(uint32_t x, int mask) { return (uint32_t)__shfl_xor((int)x, mask); }
+__device__ __forceinline__ uint64_t from_lane(uint64_t x, int mask) { return (uint64_t)__shfl_xor((unsigned long long)x, mask); }
+
+template <typename K>
+__global__ __launch_bounds__(256) void sort_kernel(Ids ids, int64_t tokens, int64_t vocab, uint64_t* keys) {
+    constexpr bool kNarrow = sizeof(K) == 4;
+    __shared__ K s[kSortRun];
     const int64_t first = (int64_t)blockIdx.x * kSortRun;
-    for (int i = threadIdx.x; i < kSortRun; i += 1024) {
-        const int64_t t = first + i;
-        const int64_t id = t < tokens ? id_at(ids, t) : -1;
-        s[i] = id >= 0 && id < vocab ? (uint64_t)id << 32 | (uint64_t)t : kNoToken - (uint64_t)(kSortRun - 1 - i);
+    const int p0 = threadIdx.x * 4;
+    K k[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        const int64_t t = first + p0 + j, id = t < tokens ? id_at(ids, t) : -1;
+        const uint64_t at = kNarrow ? (uint64_t)id * kSortRun + (uint64_t)(p0 + j) : (uint64_t)id << 32 | (uint64_t)t;
+        k[j] = id >= 0 && id < vocab ? (K)at : ~K(0);
     }
-    __syncthreads();
-    for (int size = 2; size <= kSortRun; size *= 2) {
-        for (int gap = size / 2; gap > 0; gap /= 2) {
-            for (int i = threadIdx.x; i < kSortRun / 2; i += 1024) {
-                const int a = (i & ~(gap - 1)) * 2 + (i & (gap - 1)), b = a + gap;
-                const uint64_t x = s[a], y = s[b];
-                if ((x > y) == ((a & size) == 0)) s[a] = y, s[b] = x;
+    const int64_t left = std::min<int64_t>(kSortRun, tokens - first);  // few tokens: the rest of the run is in order
+#pragma unroll 1
+    for (int size = 2; size / 2 < left; size *= 2) {
+#pragma unroll 1
+        for (int gap = size / 2; gap >= 4; gap /= 2) {
+            K y[4];
+            if (gap >= 256) {
+                __syncthreads();
+#pragma unroll
+                for (int j = 0; j < 4; ++j) s[p0 + j] = k[j];
+                __syncthreads();
+#pragma unroll
+                for (int j = 0; j < 4; ++j) y[j] = s[(p0 ^ gap) + j];
+            } else {
+#pragma unroll
+                for (int j = 0; j < 4; ++j) y[j] = from_lane(k[j], gap / 4);
             }
-            __syncthreads();
+            const bool least = ((p0 & gap) == 0) == ((p0 & size) == 0);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) k[j] = either(k[j], y[j], least);
         }
+        const auto step = [&](int i, int j) __attribute__((always_inline)) {
+            const bool up = ((p0 + i) & size) == 0;
+            const K x = k[i], y = k[j];
+            k[i] = either(x, y, up);
+            k[j] = either(x, y, !up);
+        };
+        if (size > 2) step(0, 2), step(1, 3);
+        step(0, 1), step(2, 3);
     }
-    for (int i = threadIdx.x; i < kSortRun; i += 1024)
-        if (first + i < tokens) keys[first + i] = s[i];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        if (p0 + j >= left) continue;
+        uint64_t out = k[j];
+        if (kNarrow) out = k[j] == ~K(0) ? kNoToken : (uint64_t)(k[j] / kSortRun) << 32 | (uint64_t)(first + k[j] % kSortRun);
+        keys[first + p0 + j] = out;
+    }
 }
 
-// Pairs of sorted runs of `run` keys into one: a key's place is its own plus the number of the other run's keys before it.
-__global__ __launch_bounds__(256) void merge_kernel(const uint64_t* from, uint64_t* to, int64_t tokens, int64_t run) {
-    const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
+// Up to kMergeRuns sorted runs of `run` keys into one: a key's place is its own plus the numbers of the other runs' keys before it (keys without a
+// token may be equal: those of an earlier run go first). The searches of 8 runs go on together, each halving its run.
+constexpr int kMergeRuns = 64;
+__global__ __launch_bounds__(256) void merge_kernel(const uint64_t* from, uint64_t* to, uint32_t tokens, uint32_t run, int steps) {
+    const uint32_t i = blockIdx.x * 256 + threadIdx.x;
     if (i >= tokens) return;
-    const int64_t mine = i / run, pair = mine & ~int64_t(1), other = mine ^ 1, o0 = std::min(other * run, tokens), o1 = std::min(o0 + run, tokens);
+    const uint32_t mine = i / run, group = mine / kMergeRuns * kMergeRuns;
     const uint64_t k = from[i];
-    // (keys without a token may be equal: those of the first run go first)
-    int64_t lo = o0, hi = o1;
-    while (lo < hi) {
-        const int64_t mid = (lo + hi) >> 1;
-        const uint64_t x = from[mid];
-        if (x < k || (x == k && (mine & 1)))
-            lo = mid + 1;
+    uint64_t place = (uint64_t)group * run + (i - mine * run);
+    for (uint32_t o = group; o < group + kMergeRuns; o += 8) {
+        if ((uint64_t)o * run >= tokens) break;
+        uint32_t lo[8], n[8];  // n keys from lo on are still in question
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            const uint64_t at = (uint64_t)(o + j) * run;
+            n[j] = at < tokens && o + j != mine ? std::min(run, (uint32_t)(tokens - at)) : 0u;
+            lo[j] = at < tokens ? (uint32_t)at : 0u;
+            place -= lo[j];
+        }
+        for (int s = 0; s < steps; ++s) {
+            uint64_t x[8];
+#pragma unroll
+            for (int j = 0; j < 8; ++j) x[j] = from[std::min(lo[j] + n[j] / 2, tokens - 1)];
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                const bool below = n[j] > 0 && (x[j] < k || (x[j] == k && o + j < mine));
+                const uint32_t half = n[j] / 2;
+                lo[j] += below ? half + 1 : 0u;
+                n[j] = below ? n[j] - half - 1 : half;
+            }
+        }
+#pragma unroll
+        for (int j = 0; j < 8; ++j) place += lo[j];
+    }
+    to[place] = k;
+}
+
+// A lane holds 4 columns in the sums, so that a wavefront's fp32 accesses are whole lines (8 would be two accesses of every other 16 bytes:
+// 8192 tokens, 32000 x 4096 in fp32 251 us).
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef float f32x4_a4 __attribute__((ext_vector_type(4), aligned(4)));
+typedef uint32_t u32x2_a2 __attribute__((ext_vector_type(2), aligned(2)));
+constexpr int kSlab = 1024;  // columns of a workgroup
+
+// the 4 columns from c on of a row of `cols`, those past it 0
+template <typename T>
+struct Quad;
+template <>
+struct Quad<float> {
+    f32x4 q;
+    __device__ __forceinline__ void load(const float* row, int c, int cols) {
+        if (c + 4 <= cols) {
+            q = *reinterpret_cast<const f32x4_a4*>(row + c);
+        } else {
+            q = 0.0f;
+#pragma unroll
+            for (int j = 0; j < 3; ++j)
+                if (c + j < cols) q[j] = row[c + j];
+        }
+    }
+    __device__ __forceinline__ f32x4 get() const { return q; }
+};
+template <>
+struct Quad<bf16> {
+    u32x2 q;
+    __device__ __forceinline__ void load(const bf16* row, int c, int cols) {
+        if (c + 4 <= cols) {
+            q = *reinterpret_cast<const u32x2_a2*>(row + c);
+        } else {
+            uint32_t h[3];
+#pragma unroll
+            for (int j = 0; j < 3; ++j) h[j] = c + j < cols ? row[c + j].b : 0u;
+            q = u32x2{h[0] | h[1] << 16, h[2]};
+        }
+    }
+    __device__ __forceinline__ f32x4 get() const {
+        return f32x4{bits_f(q[0] << 16), bits_f(q[0] & 0xffff0000u), bits_f(q[1] << 16), bits_f(q[1] & 0xffff0000u)};
+    }
+};
+// NT: past the caches (the rows' kernel, 8192 tokens, 32000 x 4096: 135 us, past the caches 109).
+template <bool NT = false>
+__device__ __forceinline__ void store4(float* row, int c, int cols, f32x4 v) {
+    if (c + 4 <= cols) {
+        if (NT)
+            __builtin_nontemporal_store(v, reinterpret_cast<f32x4_a4*>(row + c));
         else
-            hi = mid;
+            *reinterpret_cast<f32x4_a4*>(row + c) = v;
+        return;
     }
-    to[pair * run + (i - mine * run) + (lo - o0)] = k;
+#pragma unroll
+    for (int j = 0; j < 3; ++j)
+        if (c + j < cols) row[c + j] = v[j];
+}
+template <bool NT = false>
+__device__ __forceinline__ void store4(bf16* row, int c, int cols, f32x4 v) {
+    if (c + 4 <= cols) {
+        const u32x2 q = {pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3])};
+        if (NT)
+            __builtin_nontemporal_store(q, reinterpret_cast<u32x2_a2*>(row + c));
+        else
+            *reinterpret_cast<u32x2_a2*>(row + c) = q;
+        return;
+    }
+#pragma unroll
+    for (int j = 0; j < 3; ++j)
+        if (c + j < cols) put(row + c + j, v[j]);
 }
 
-// 8 columns of the sum over sorted tokens i0 .. i1, in order.
+// 4 columns of the sum over sorted tokens i0 .. i1, in order, the loads of 8 in flight.
 template <typename T>
-__device__ __forceinline__ void add_tokens(const EmbedBackward& a, int64_t i0, int64_t i1, int c, float (&s)[8]) {
-    for (int64_t i = i0; i < i1; i += 4) {
-        Chunk<T> k[4];
+__device__ __forceinline__ void add_tokens(const EmbedBackward& a, int64_t i0, int64_t i1, int c, f32x4& s) {
+    for (int64_t i = i0; i < i1; i += 8) {
+        Quad<T> k[8];
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            k[j].zero();
-            if (i + j < i1) load_chunk(k[j], static_cast<const T*>(a.dy.p) + (int64_t)(uint32_t)a.key0[i + j] * a.dy.ld, c, a.cols);
-        }
+        for (int j = 0; j < 8; ++j)
+            if (i + j < i1) k[j].load(static_cast<const T*>(a.dy.p) + (int64_t)(uint32_t)a.key0[i + j] * a.dy.ld, c, a.cols);
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            float v[8];
-            k[j].get(v);
-#pragma unroll
-            for (int e = 0; e < 8; ++e) s[e] += v[e];
-        }
+        for (int j = 0; j < 8; ++j)
+            if (i + j < i1) s += k[j].get();
     }
 }
 
-// Sums over pieces of kPiece sorted tokens of one id, so that a frequent id is not one workgroup's work.
+// Two things that the sorted tokens give, side by side: sums over pieces of kPiece tokens of one id, so that a frequent id is not one workgroup's work, and
+// for each row of the table where its tokens begin (a search by every lane; in the rows' own kernel it would hold up their stores: 8192 tokens, 32000 x 4096 in fp32 225 us).
 template <typename T>
-__global__ __launch_bounds__(256) void piece_kernel(EmbedBackward a) {
-    const int64_t i0 = (int64_t)blockIdx.x * kPiece;
+__global__ __launch_bounds__(256) void piece_kernel(EmbedBackward a, uint32_t pieces, uint32_t slabs) {
+    if (blockIdx.x >= pieces * slabs) {
+        const int64_t v = (int64_t)(blockIdx.x - pieces * slabs) * 256 + threadIdx.x;
+        if (v > a.vocab) return;
+        uint32_t lo = 0, n = (uint32_t)a.tokens;
+        while (n > 0) {
+            const uint32_t half = n / 2;
+            if ((int64_t)(a.key0[lo + half] >> 32) < v)
+                lo += half + 1, n -= half + 1;
+            else
+                n = half;
+        }
+        a.begin[v] = lo;
+        return;
+    }
+    const uint32_t piece = blockIdx.x / slabs;
+    const int64_t i0 = (int64_t)piece * kPiece;
     const uint32_t id = (uint32_t)(a.key0[i0] >> 32);
     if ((uint32_t)(a.key0[i0 + kPiece - 1] >> 32) != id || id >= (uint64_t)a.vocab) return;
-    const int c = ((int)blockIdx.y * 256 + threadIdx.x) * 8;
+    const int c = (int)(blockIdx.x % slabs) * kSlab + threadIdx.x * 4;
     if (c >= a.cols) return;
-    float s[8] = {};
+    f32x4 s = {};
     add_tokens<T>(a, i0, i0 + kPiece, c, s);
-    store_chunk(a.part + (int64_t)blockIdx.x * a.cols, c, a.cols, s);
+    store4(a.part + (int64_t)piece * a.cols, c, a.cols, s);
 }
 
-// Number of sorted keys below `key`: 64 places are looked at at once.
-__device__ __forceinline__ int64_t count_below(const uint64_t* keys, int64_t n, uint64_t key, int lane) {
-    int64_t lo = 0, hi = n;  // the answer lies in lo .. hi
-    while (lo < hi) {
-        const int64_t step = (hi - lo + 63) / 64, at = lo + (lane + 1) * step - 1;
-        const int below = __popcll(__ballot(at < hi && keys[std::min(at, hi - 1)] < key));
-        hi = std::min(hi, lo + (below + 1) * step - 1);
-        lo += below * step;
-    }
-    return lo;
-}
-
-// kRows rows of the table's gradient, 2048 columns: sums of their tokens, scaled, added to the base and rounded once.
+// kRows rows of the table's gradient, kSlab columns: sums of their tokens, scaled, added to the base and rounded once.
 constexpr int kRows = 8;
 template <typename T, typename O>
 __global__ __launch_bounds__(256) void rows_kernel(EmbedBackward a) {
-    const int lane = threadIdx.x & 63;
     const int64_t v0 = (int64_t)blockIdx.x * kRows;
-    const int c = ((int)blockIdx.y * 256 + threadIdx.x) * 8;
-    int64_t i = count_below(a.key0, a.tokens, (uint64_t)v0 << 32, lane);
-    for (int64_t v = v0; v < std::min(v0 + kRows, a.vocab); ++v) {
-        int64_t end = i;  // (ids of the next 64 tokens at a time)
-        for (;;) {
-            const bool same = end + lane < a.tokens && (int64_t)(a.key0[end + lane] >> 32) == v;
-            const int n = __popcll(__ballot(same));
-            end += n;
-            if (n < 64) break;
-        }
-        const int64_t i0 = i;
-        i = end;
-        if (c >= a.cols) continue;
-        O* const row = static_cast<O*>(a.dw) + v * a.cols;
-        if (i0 == end && a.base == a.dw) continue;
-        float s[8] = {};
-        const int64_t p0 = (i0 + kPiece - 1) / kPiece, p1 = end / kPiece;
-        if (p0 < p1) {
-            add_tokens<T>(a, i0, p0 * kPiece, c, s);
-            for (int64_t p = p0; p < p1; ++p) {
-                Chunk<float> k;
-                load_chunk(k, a.part + p * a.cols, c, a.cols);
-                float v8[8];
-                k.get(v8);
+    const int c = (int)blockIdx.y * kSlab + threadIdx.x * 4;
+    if (c >= a.cols) return;
+    const int rows = (int)std::min<int64_t>(kRows, a.vocab - v0);
+    uint32_t begin[kRows + 1];
 #pragma unroll
-                for (int e = 0; e < 8; ++e) s[e] += v8[e];
+    for (int r = 0; r <= kRows; ++r) begin[r] = a.tokens > 0 ? a.begin[v0 + std::min(r, rows)] : 0u;
+    for (int r = 0; r < rows; ++r) {
+        const int64_t v = v0 + r;
+        uint32_t i0 = begin[0], i1 = begin[1];
+#pragma unroll
+        for (int j = 0; j < kRows; ++j) begin[j] = begin[j + 1];
+        if (i0 == i1 && a.base == a.dw) continue;
+        f32x4 s = {};
+        if (i0 < i1) {
+            const int64_t p0 = ((int64_t)i0 + kPiece - 1) / kPiece, p1 = i1 / kPiece;
+            const bool split = p0 < p1;
+            add_tokens<T>(a, i0, split ? p0 * kPiece : i1, c, s);
+            for (int64_t p = p0; p < p1; p += 8) {
+                Quad<float> k[8];
+#pragma unroll
+                for (int j = 0; j < 8; ++j)
+                    if (p + j < p1) k[j].load(a.part + (p + j) * a.cols, c, a.cols);
+#pragma unroll
+                for (int j = 0; j < 8; ++j)
+                    if (p + j < p1) s += k[j].get();
             }
-            add_tokens<T>(a, p1 * kPiece, end, c, s);
-        } else {
-            add_tokens<T>(a, i0, end, c, s);
+            if (split) add_tokens<T>(a, p1 * kPiece, i1, c, s);
+            s *= a.scale;
         }
-#pragma unroll
-        for (int e = 0; e < 8; ++e) s[e] *= a.scale;
         if (a.base) {
-            Chunk<O> k;
-            load_chunk(k, static_cast<const O*>(a.base) + v * a.cols, c, a.cols);
-            float b[8];
-            k.get(b);
-#pragma unroll
-            for (int e = 0; e < 8; ++e) s[e] += b[e];
+            Quad<O> k;
+            k.load(static_cast<const O*>(a.base) + v * a.cols, c, a.cols);
+            s += k.get();
         }
-        store_chunk(row, c, a.cols, s);
+        store4<true>(static_cast<O*>(a.dw) + v * a.cols, c, a.cols, s);
     }
 }
 
@@ -185,14 +300,21 @@ hipError_t run_lookup(Mat table, Ids ids, int64_t tokens, int64_t vocab, int32_t
 
 template <typename T, typename O>
 hipError_t run_backward(EmbedBackward a, hipStream_t st) {
-    const uint32_t slabs = (uint32_t)((a.cols + 2047) / 2048);
+    const uint32_t slabs = (uint32_t)((a.cols + kSlab - 1) / kSlab);
     if (a.tokens > 0) {
-        sort_kernel<<<(uint32_t)((a.tokens + kSortRun - 1) / kSortRun), 1024, 0, st>>>(a.ids, a.tokens, a.vocab, a.key0);
-        for (int64_t run = kSortRun; run < a.tokens; run *= 2) {
-            merge_kernel<<<(uint32_t)((a.tokens + 255) / 256), 256, 0, st>>>(a.key0, a.key1, a.tokens, run);
+        const uint32_t runs = (uint32_t)((a.tokens + kSortRun - 1) / kSortRun);
+        if (a.vocab < (1 << 22))
+            sort_kernel<uint32_t><<<runs, 256, 0, st>>>(a.ids, a.tokens, a.vocab, a.key0);
+        else
+            sort_kernel<uint64_t><<<runs, 256, 0, st>>>(a.ids, a.tokens, a.vocab, a.key0);
+        for (int64_t run = kSortRun; run < a.tokens; run *= kMergeRuns) {
+            int steps = 1;  // a search among n keys takes floor(log2 n) + 1 steps
+            while ((run >> steps) > 0) ++steps;
+            merge_kernel<<<(uint32_t)((a.tokens + 255) / 256), 256, 0, st>>>(a.key0, a.key1, (uint32_t)a.tokens, (uint32_t)run, steps);
             std::swap(a.key0, a.key1);
         }
-        if (a.tokens >= kPiece) piece_kernel<T><<<dim3((uint32_t)(a.tokens / kPiece), slabs), 256, 0, st>>>(a);
+        const uint32_t pieces = (uint32_t)(a.tokens / kPiece);
+        piece_kernel<T><<<pieces * slabs + (uint32_t)(a.vocab / 256 + 1), 256, 0, st>>>(a, pieces, slabs);
     }
     rows_kernel<T, O><<<dim3((uint32_t)((a.vocab + kRows - 1) / kRows), slabs), 256, 0, st>>>(a);
     return hipGetLastError();
@@ -209,11 +331,12 @@ hipError_t launch_embed_forward(int table_dtype, int out_dtype, Mat table, Ids i
                                       : run_lookup<float, float>(table, ids, tokens, vocab, cols, scale, out, st);
 }
 
-EmbedPlan embed_plan(int64_t tokens, int64_t cols) {
+EmbedPlan embed_plan(int64_t tokens, int64_t vocab, int64_t cols) {
     const auto up = [](size_t x) { return (x + 255) & ~size_t(255); };
     EmbedPlan p = {};
     p.key1_off = up((size_t)tokens * 8);
-    p.part_off = p.key1_off + (tokens > kSortRun ? up((size_t)tokens * 8) : 0);
+    p.begin_off = p.key1_off + (tokens > kSortRun ? up((size_t)tokens * 8) : 0);
+    p.part_off = p.begin_off + (tokens > 0 ? up((size_t)(vocab + 1) * 4) : 0);
     p.bytes = p.part_off + up((size_t)(tokens / kPiece) * cols * 4);
     return p;
 }

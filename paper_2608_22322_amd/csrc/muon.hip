@@ -67,7 +67,9 @@ __global__ __launch_bounds__(256) void momentum_kernel(MuonList l, MuonArgs a, i
 #pragma unroll
             for (int m = 1; m < 64; m <<= 1) top = umax(top, (uint32_t)__shfl_xor((int)top, m));
             const float am = u2f(top);
-            const double r = am > 0.0f ? rdiv127((double)am) : 0.0;
+            // A position is x times 127 (1 / absmax), each rounded: within 2 ulps of 127 x / absmax, so that a code differs from one decided by the
+            // quotient only where |x| is half of absmax (position 63.5).
+            const double r = am > 0.0f ? 127.0 * (1.0 / (double)am) : 0.0;
             uint32_t q[4];
 #pragma unroll
             for (int j = 0; j < 4; ++j) q[j] = rint_low_bits((double)mn[j] * r);

@@ -37,9 +37,9 @@ al_status check_packed(const void* dw, const void* base, int64_t rows, int64_t c
     return AL_OK;
 }
 
-// What the rows of the table's gradient take: a grid of rows by 2048 columns.
+// What the rows of the table's gradient take: a grid of rows by 1024 columns.
 al_status check_rows(int64_t vocab, int64_t cols, const char* who) {
-    if ((cols + 2047) / 2048 > 65535) return fail(AL_EUNSUPPORTED, "%s: %lld columns are too many", who, (long long)cols);
+    if ((cols + 1023) / 1024 > 65535) return fail(AL_EUNSUPPORTED, "%s: %lld columns are too many", who, (long long)cols);
     (void)vocab;
     return AL_OK;
 }
@@ -83,7 +83,7 @@ al_status al_embed_backward_workspace_bytes(int64_t tokens, int64_t vocab, int64
     *bytes = 0;
     AL_TRY(check_sizes(tokens, vocab, cols, who));
     AL_TRY(check_rows(vocab, cols, who));
-    *bytes = al::embed_plan(tokens, cols).bytes;
+    *bytes = al::embed_plan(tokens, vocab, cols).bytes;
     return AL_OK;
 }
 
@@ -103,7 +103,7 @@ al_status al_embed_backward(int32_t dtype, const void* dy, int64_t lddy, int32_t
         AL_TRY(check_ids(ids, index_dtype, who, "ids"));
         AL_TRY(check_mat(dy, &lddy, tokens, cols, dtype, true, who, "dy"));
     }
-    const al::EmbedPlan p = al::embed_plan(tokens, cols);
+    const al::EmbedPlan p = al::embed_plan(tokens, vocab, cols);
     AL_TRY(check_ws(ws, ws_bytes, p.bytes, who));
     char* const w = static_cast<char*>(ws);
     al::EmbedBackward a;
@@ -118,6 +118,7 @@ al_status al_embed_backward(int32_t dtype, const void* dy, int64_t lddy, int32_t
     a.dw = dw;
     a.key0 = reinterpret_cast<uint64_t*>(w);
     a.key1 = reinterpret_cast<uint64_t*>(w + p.key1_off);
+    a.begin = reinterpret_cast<uint32_t*>(w + p.begin_off);
     a.part = reinterpret_cast<float*>(w + p.part_off);
     return launched(al::launch_embed_backward(dtype, grad_dtype, a, as_stream(stream)), who);
 }

@@ -20,8 +20,8 @@ struct Ids {
 hipError_t launch_embed_forward(int table_dtype, int out_dtype, Mat table, Ids ids, int64_t tokens, int64_t vocab, int32_t cols, float scale, Mat out,
                                 hipStream_t st);
 
-// Sorted (id, token) keys in two buffers, and sums of dy over whole pieces of equal ids.
-constexpr int kSortRun = 4096, kPiece = 128;
+// Sorted (id, token) keys in two buffers, where each row's tokens begin among them, and sums of dy over whole pieces of equal ids.
+constexpr int kSortRun = 1024, kPiece = 32;
 struct EmbedBackward {
     Mat dy;
     Ids ids;
@@ -31,12 +31,13 @@ struct EmbedBackward {
     const void* base;
     void* dw;
     uint64_t *key0, *key1;
+    uint32_t* begin;
     float* part;
 };
 struct EmbedPlan {
-    size_t key0_off, key1_off, part_off, bytes;
+    size_t key1_off, begin_off, part_off, bytes;
 };
-EmbedPlan embed_plan(int64_t tokens, int64_t cols);
+EmbedPlan embed_plan(int64_t tokens, int64_t vocab, int64_t cols);
 hipError_t launch_embed_backward(int dtype, int grad_dtype, const EmbedBackward& a, hipStream_t st);
 
 // Cross entropy: how a call is cut, by its sizes alone.
