@@ -44,6 +44,7 @@ struct Mm {
 template <int B>
 struct MmTile {
     static constexpr int kThreads = B == 256 ? 512 : 256, kWaves = kThreads / 64, WM = B / 2, WN = B == 64 ? 32 : 64, FM = WM / 16, FN = WN / 16;
+    static constexpr int kStages = B == 64 ? 4 : 2;  // turns in LDS: 64 (64-wide tiles), 64 and 128 KB
     static constexpr int kChunks = B * kMmTurn / 8 / kThreads;  // 16-byte pieces of an operand that a thread stages in a turn
     static __device__ __forceinline__ int wave_m(int w) { return w / (B / WN) * WM; }
     static __device__ __forceinline__ int wave_n(int w) { return w % (B / WN) * WN; }
@@ -143,8 +144,11 @@ struct MmCore {
         }
     };
 
-    static __device__ __forceinline__ void run(const Mm& p, int batch, int m0, int n0, int t0, int t1, uint16_t* as0, uint16_t* as1, uint16_t* bs0,
-                                               uint16_t* bs1, MmAcc (&acc)[G::FM][G::FN]) {
+    // Turns t0 .. t1 of a tile. `lds`: kStages places for a turn of either operand (arrays of their own, so that the compiler knows that a
+    // read of one does not wait for the loads into the others). The loads of kStages - 1 turns are in flight.
+    static __device__ __forceinline__ void run(const Mm& p, int batch, int m0, int n0, int t0, int t1, uint16_t* const (&as)[G::kStages],
+                                               uint16_t* const (&bs)[G::kStages], MmAcc (&acc)[G::FM][G::FN]) {
+        constexpr int S = G::kStages;
         const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6);
         uint32_t oa[G::kChunks], ob[G::kChunks];
 #pragma unroll
@@ -153,43 +157,51 @@ struct MmCore {
             ob[i] = offset<BK, false>(p.b, n0, i, tid, 0);
         }
         const uint16_t *const pa = p.a.p + batch * p.a.batch, *const pb = p.b.p + batch * p.b.batch;
-        const auto load = [&](int t, uint16_t* as, uint16_t* bs) __attribute__((always_inline)) {
-            const int seg = t / p.turns, k0 = (t - seg * p.turns) * kMmTurn;
-            issue<AK, false>(p.a, (p.amask >> seg) & 1 ? pa + p.a.lo : pa, m0, k0, oa, as, (w << 6) | lane);
-            issue<BK, ENDS>(p.b, (p.bmask >> seg) & 1 ? pb + p.b.lo : pb, n0, k0, ob, bs, (w << 6) | lane);
+        int seg = t0 / p.turns, k0 = (t0 - seg * p.turns) * kMmTurn;  // of the next turn to load
+        const auto load = [&](int s) __attribute__((always_inline)) {
+            issue<AK, false>(p.a, (p.amask >> seg) & 1 ? pa + p.a.lo : pa, m0, k0, oa, as[s], (w << 6) | lane);
+            issue<BK, ENDS>(p.b, (p.bmask >> seg) & 1 ? pb + p.b.lo : pb, n0, k0, ob, bs[s], (w << 6) | lane);
+            k0 += kMmTurn;
+            if (k0 == p.turns * kMmTurn) k0 = 0, ++seg;
         };
         Places<AK> am(G::wave_m(w), lane);
         Places<BK> bn(G::wave_n(w), lane);
-        const auto multiply = [&](const uint16_t* as, const uint16_t* bs) __attribute__((always_inline)) {
+        const auto multiply = [&](int s) __attribute__((always_inline)) {
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
                 MmFragment fb[G::FN];
 #pragma unroll
-                for (int j = 0; j < G::FN; ++j) fb[j] = bn.read(bs, j, h);
+                for (int j = 0; j < G::FN; ++j) fb[j] = bn.read(bs[s], j, h);
 #pragma unroll
                 for (int i = 0; i < G::FM; ++i) {
-                    const MmFragment fa = am.read(as, i, h);
+                    const MmFragment fa = am.read(as[s], i, h);
 #pragma unroll
                     for (int j = 0; j < G::FN; ++j) acc[i][j] = mm_mul<T>(fb[j], fa, acc[i][j]);
                 }
             }
         };
-        // the loads of a turn are in flight while the turn before it is multiplied
-        const auto turn = [&](int t, const uint16_t* as, const uint16_t* bs, uint16_t* an, uint16_t* bn_) __attribute__((always_inline)) {
-            __builtin_amdgcn_s_waitcnt(0x0f70);  // vmcnt(0)
-            __syncthreads();
-            if (t + 1 < t1) load(t + 1, an, bn_);
-            am.renew();
-            bn.renew();
-            multiply(as, bs);
-        };
-        if (t0 < t1) load(t0, as0, bs0);
-        int t = t0;
-        for (; t + 1 < t1; t += 2) {
-            turn(t, as0, bs0, as1, bs1);
-            turn(t + 1, as1, bs1, as0, bs0);
+#pragma unroll
+        for (int s = 0; s < S - 1; ++s)
+            if (t0 + s < t1) load(s);
+        for (int t = t0; t < t1; t += S) {
+#pragma unroll
+            for (int s = 0; s < S; ++s) {
+                if (t + s >= t1) break;
+                // This wavefront's pieces of the turn have arrived (all its loads but those of the S - 2 turns behind it: vmcnt), and it has read what the next
+                // loads will overwrite (lgkmcnt); behind the barrier that holds for all. (__syncthreads would wait for every load.)
+                if (S > 2 && t + s + S - 2 < t1)
+                    __builtin_amdgcn_s_waitcnt(0x0070 | (S - 2) * 2 * G::kChunks);
+                else
+                    __builtin_amdgcn_s_waitcnt(0x0070);
+                asm volatile("" ::: "memory");
+                __builtin_amdgcn_s_barrier();
+                asm volatile("" ::: "memory");
+                if (t + s + S - 1 < t1) load((s + S - 1) % S);
+                am.renew();
+                bn.renew();
+                multiply(s);
+            }
         }
-        if (t < t1) turn(t, as0, bs0, as1, bs1);
     }
 };
 
@@ -225,13 +237,19 @@ struct MmRows : std::false_type {};
 template <class E>
 struct MmRows<E, std::enable_if_t<E::kRows>> : std::true_type {};
 template <class T, int B, bool AK, bool BK, bool ENDS, class E>
-__global__ __launch_bounds__(MmTile<B>::kThreads, B == 64 ? 4 : 2) void mm_kernel(Mm p, E end) {
+__global__ __launch_bounds__(MmTile<B>::kThreads, 2) void mm_kernel(Mm p, E end) {
     typedef MmTile<B> G;
     __shared__ __attribute__((aligned(16))) uint16_t as0[B * kMmTurn], as1[B * kMmTurn], bs0[B * kMmTurn], bs1[B * kMmTurn];
+    __shared__ __attribute__((aligned(16))) uint16_t as2[G::kStages > 2 ? B * kMmTurn : 8], as3[G::kStages > 2 ? B * kMmTurn : 8],
+        bs2[G::kStages > 2 ? B * kMmTurn : 8], bs3[G::kStages > 2 ? B * kMmTurn : 8];
+    uint16_t* as[G::kStages];
+    uint16_t* bs[G::kStages];
+    as[0] = as0, as[1] = as1, bs[0] = bs0, bs[1] = bs1;
+    if constexpr (G::kStages > 2) as[2] = as2, as[3] = as3, bs[2] = bs2, bs[3] = bs3;
     const MmId id = mm_id<B>(p);
     const int total = p.turns * p.segs, t0 = (int)((int64_t)total * id.split / p.splits), t1 = (int)((int64_t)total * (id.split + 1) / p.splits);
     MmAcc acc[G::FM][G::FN] = {};
-    MmCore<T, B, AK, BK, ENDS>::run(p, id.batch, id.m * B, id.n * B, t0, t1, as0, as1, bs0, bs1, acc);
+    MmCore<T, B, AK, BK, ENDS>::run(p, id.batch, id.m * B, id.n * B, t0, t1, as, bs, acc);
     const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
     const int m = id.m * B + G::wave_m(w) + (lane & 15), n = id.n * B + G::wave_n(w) + 4 * (lane >> 4);
     if (p.splits > 1) {
