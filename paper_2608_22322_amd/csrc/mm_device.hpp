@@ -25,20 +25,19 @@ constexpr int kMmTurn = 64;
 // 8, ld too, and p is 16-byte aligned), for outputs that are not written or against zeros of the other operand.
 struct MmOperand {
     const uint16_t* p;
-    int64_t batch;  // elements from one batch's matrix to the next
-    int64_t lo;     // elements from a matrix to its low part
+    int64_t lo;  // elements from a matrix to its low part
     int32_t ld, rows, cols;
 };
 
-// A product, or a batch of them. An operand may be the sum of a high and a low part: `segs` segments of `turns` turns each, segment
+// A product. An operand may be the sum of a high and a low part: `segs` segments of `turns` turns each, segment
 // i with the low part of A (B) where bit i of amask (bmask) is set.
 struct Mm {
     MmOperand a, b;
     int32_t m, n, turns, segs;
     uint32_t amask, bmask;
-    int32_t batches, splits;  // splits over the turns
-    int32_t sym;              // A A^T: the tiles on and below the diagonal alone
-    float* part;              // splits > 1: partial sums, [batch][split][tile][lanes' order]
+    int32_t splits;  // over the turns
+    int32_t sym;     // A A^T: the tiles on and below the diagonal alone
+    float* part;     // splits > 1: partial sums, [split][tile][lanes' order]
 };
 
 template <int B>
@@ -49,7 +48,7 @@ struct MmTile {
     static __device__ __forceinline__ int wave_m(int w) { return w / (B / WN) * WM; }
     static __device__ __forceinline__ int wave_n(int w) { return w % (B / WN) * WN; }
     static uint32_t side(int n) { return (uint32_t)((n + B - 1) / B); }
-    static uint32_t tiles(const Mm& p) { return p.sym ? side(p.m) * (side(p.m) + 1) / 2 : side(p.m) * side(p.n); }
+    static uint32_t tiles(const Mm& p) { return side(p.m) * side(p.n); }
 };
 
 typedef f32x4 MmAcc;
@@ -144,9 +143,9 @@ struct MmCore {
         }
     };
 
-    // Turns t0 .. t1 of a tile. `lds`: kStages places for a turn of either operand (arrays of their own, so that the compiler knows that a
-    // read of one does not wait for the loads into the others). The loads of kStages - 1 turns are in flight.
-    static __device__ __forceinline__ void run(const Mm& p, int batch, int m0, int n0, int t0, int t1, uint16_t* const (&as)[G::kStages],
+    // Turns t0 .. t1 of a tile. as, bs: kStages places for a turn of either operand (arrays of their own, so that the compiler knows that a
+    // read of one does not wait for the loads into the others).
+    static __device__ __forceinline__ void run(const Mm& p, int m0, int n0, int t0, int t1, uint16_t* const (&as)[G::kStages],
                                                uint16_t* const (&bs)[G::kStages], MmAcc (&acc)[G::FM][G::FN]) {
         constexpr int S = G::kStages;
         const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -156,7 +155,7 @@ struct MmCore {
             oa[i] = offset<AK, false>(p.a, m0, i, tid, 0);
             ob[i] = offset<BK, false>(p.b, n0, i, tid, 0);
         }
-        const uint16_t *const pa = p.a.p + batch * p.a.batch, *const pb = p.b.p + batch * p.b.batch;
+        const uint16_t *const pa = p.a.p, *const pb = p.b.p;
         int seg = t0 / p.turns, k0 = (t0 - seg * p.turns) * kMmTurn;  // of the next turn to load
         const auto load = [&](int s) __attribute__((always_inline)) {
             issue<AK, false>(p.a, (p.amask >> seg) & 1 ? pa + p.a.lo : pa, m0, k0, oa, as[s], (w << 6) | lane);
@@ -166,71 +165,133 @@ struct MmCore {
         };
         Places<AK> am(G::wave_m(w), lane);
         Places<BK> bn(G::wave_n(w), lane);
-        const auto multiply = [&](int s) __attribute__((always_inline)) {
-#pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                MmFragment fb[G::FN];
-#pragma unroll
-                for (int j = 0; j < G::FN; ++j) fb[j] = bn.read(bs[s], j, h);
-#pragma unroll
-                for (int i = 0; i < G::FM; ++i) {
-                    const MmFragment fa = am.read(as[s], i, h);
-#pragma unroll
-                    for (int j = 0; j < G::FN; ++j) acc[i][j] = mm_mul<T>(fb[j], fa, acc[i][j]);
-                }
-            }
+        // This wavefront's pieces of a turn have arrived (`behind`: those of the S - 2 turns after it may be in flight: vmcnt), and what it read of an earlier one is
+        // in its registers (lgkmcnt); behind the barrier that holds for all, and the loads into the earlier turn's place may begin. (__syncthreads would wait for every load.)
+        const auto meet = [&](bool behind) __attribute__((always_inline)) {
+            if (S > 2 && behind)
+                __builtin_amdgcn_s_waitcnt(0x0070 | (S - 2) * 2 * G::kChunks);
+            else
+                __builtin_amdgcn_s_waitcnt(0x0070);
+            asm volatile("" ::: "memory");
+            __builtin_amdgcn_s_barrier();
+            asm volatile("" ::: "memory");
         };
-#pragma unroll
-        for (int s = 0; s < S - 1; ++s)
-            if (t0 + s < t1) load(s);
-        for (int t = t0; t < t1; t += S) {
-#pragma unroll
-            for (int s = 0; s < S; ++s) {
-                if (t + s >= t1) break;
-                // This wavefront's pieces of the turn have arrived (all its loads but those of the S - 2 turns behind it: vmcnt), and it has read what the next
-                // loads will overwrite (lgkmcnt); behind the barrier that holds for all. (__syncthreads would wait for every load.)
-                if (S > 2 && t + s + S - 2 < t1)
-                    __builtin_amdgcn_s_waitcnt(0x0070 | (S - 2) * 2 * G::kChunks);
-                else
-                    __builtin_amdgcn_s_waitcnt(0x0070);
-                asm volatile("" ::: "memory");
-                __builtin_amdgcn_s_barrier();
-                asm volatile("" ::: "memory");
-                if (t + s + S - 1 < t1) load((s + S - 1) % S);
+        if (t0 >= t1) return;
+        if constexpr (B == 256) {
+            // The barrier lies between the halves of a turn: the products of the second half, whose fragments are in registers, cover the next turn's first
+            // reads and the issuing of loads (8 wavefronts, 2 a SIMD; 4096^3: 240 us with the barrier between the turns, 220 so. The smaller tiles have fewer products to
+            // cover them with, and take longer so.)
+            struct Half {
+                MmFragment a[G::FM], b[G::FN];
+            } f0, f1;
+            const auto read = [&](Half& f, int s, int h) __attribute__((always_inline)) {
                 am.renew();
                 bn.renew();
-                multiply(s);
+#pragma unroll
+                for (int j = 0; j < G::FN; ++j) f.b[j] = bn.read(bs[s], j, h);
+#pragma unroll
+                for (int i = 0; i < G::FM; ++i) f.a[i] = am.read(as[s], i, h);
+            };
+            const auto multiply = [&](const Half& f) __attribute__((always_inline)) {
+#pragma unroll
+                for (int i = 0; i < G::FM; ++i)
+#pragma unroll
+                    for (int j = 0; j < G::FN; ++j) acc[i][j] = mm_mul<T>(f.b[j], f.a[i], acc[i][j]);
+            };
+#pragma unroll
+            for (int s = 0; s < S; ++s)
+                if (t0 + s < t1) load(s);
+            meet(false);
+            read(f0, 0, 0);
+            for (int t = t0; t < t1; t += S) {
+#pragma unroll
+                for (int s = 0; s < S; ++s) {
+                    if (t + s >= t1) break;
+                    read(f1, s, 1);
+                    __builtin_amdgcn_sched_barrier(0);
+                    multiply(f0);
+                    __builtin_amdgcn_sched_barrier(0);
+                    if (t + s + 1 < t1) {
+                        meet(t + s + S - 1 < t1);
+                        read(f0, (s + 1) % S, 0);
+                        if (t + s + S < t1) load(s);
+                    }
+                    __builtin_amdgcn_sched_barrier(0);
+                    multiply(f1);
+                    __builtin_amdgcn_sched_barrier(0);
+                }
+            }
+        } else {
+#pragma unroll
+            for (int s = 0; s < S - 1; ++s)
+                if (t0 + s < t1) load(s);
+            for (int t = t0; t < t1; t += S) {
+#pragma unroll
+                for (int s = 0; s < S; ++s) {
+                    if (t + s >= t1) break;
+                    meet(t + s + S - 2 < t1);
+                    if (t + s + S - 1 < t1) load((s + S - 1) % S);
+                    am.renew();
+                    bn.renew();
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) {
+                        MmFragment fb[G::FN];
+#pragma unroll
+                        for (int j = 0; j < G::FN; ++j) fb[j] = bn.read(bs[s], j, h);
+#pragma unroll
+                        for (int i = 0; i < G::FM; ++i) {
+                            const MmFragment fa = am.read(as[s], i, h);
+#pragma unroll
+                            for (int j = 0; j < G::FN; ++j) acc[i][j] = mm_mul<T>(fb[j], fa, acc[i][j]);
+                        }
+                    }
+                }
             }
         }
     }
 };
 
-// Workgroup -> batch, split and tile; an XCD takes a contiguous share, in bands of 8 tiles along m.
-struct MmId {
-    int batch, split, m, n, tile;
+// The places of a tile's turns in LDS: arrays of their own.
+#define MM_PLACES(B, as, bs)                                                                                                                        \
+    __shared__ __attribute__((aligned(16))) uint16_t as##0_[B * kMmTurn], as##1_[B * kMmTurn], bs##0_[B * kMmTurn], bs##1_[B * kMmTurn];            \
+    __shared__ __attribute__((aligned(16))) uint16_t as##2_[MmTile<B>::kStages > 2 ? B * kMmTurn : 8], as##3_[MmTile<B>::kStages > 2 ? B * kMmTurn : 8], \
+        bs##2_[MmTile<B>::kStages > 2 ? B * kMmTurn : 8], bs##3_[MmTile<B>::kStages > 2 ? B * kMmTurn : 8];                                         \
+    uint16_t *as[MmTile<B>::kStages], *bs[MmTile<B>::kStages];                                                                                      \
+    as[0] = as##0_, as[1] = as##1_, bs[0] = bs##0_, bs[1] = bs##1_;                                                                                 \
+    if constexpr (MmTile<B>::kStages > 2) as[2] = as##2_, as[3] = as##3_, bs[2] = bs##2_, bs[3] = bs##3_
+
+// Tile number (the same in all lanes) -> its rows and columns of tiles: the triangle on and below the diagonal row by row, others in bands of 8 along m.
+struct MmAt {
+    int m, n;
+};
+template <int B>
+__device__ __forceinline__ MmAt mm_at(const Mm& p, uint32_t tile) {
+    if (p.sym) {
+        uint32_t i = (uint32_t)((sqrtf(8.0f * (float)tile + 1.0f) - 1.0f) * 0.5f);
+        while (i * (i + 1) / 2 > tile) --i;
+        while ((i + 1) * (i + 2) / 2 <= tile) ++i;
+        return {__builtin_amdgcn_readfirstlane((int)i), __builtin_amdgcn_readfirstlane((int)(tile - i * (i + 1) / 2))};
+    }
+    const uint32_t mt = (uint32_t)((p.m + B - 1) / B), nt = (uint32_t)((p.n + B - 1) / B);
+    const uint32_t band = tile / (8 * nt), rows = min(8u, mt - band * 8), q = tile - band * 8 * nt, n = q / rows;
+    return {__builtin_amdgcn_readfirstlane((int)(band * 8 + q - n * rows)), __builtin_amdgcn_readfirstlane((int)n)};
+}
+
+// Workgroup -> split and tile; an XCD takes a contiguous share.
+struct MmId : MmAt {
+    int split, tile;
 };
 template <int B>
 __device__ __forceinline__ MmId mm_id(const Mm& p) {
-    const uint32_t mt = (uint32_t)((p.m + B - 1) / B), nt = p.sym ? mt : (uint32_t)((p.n + B - 1) / B);
-    const uint32_t per = p.sym ? mt * (mt + 1) / 2 : mt * nt, id = xcd_block(blockIdx.x, gridDim.x);
-    const uint32_t b = id / per, r = id - b * per;
+    const uint32_t per = gridDim.x / (uint32_t)p.splits, id = xcd_block(blockIdx.x, gridDim.x), s = id / per;
     MmId t;
-    t.batch = (int)(b / (uint32_t)p.splits);
-    t.split = (int)(b - t.batch * (uint32_t)p.splits);
-    t.tile = (int)r;
-    if (p.sym) {
-        uint32_t i = (uint32_t)((sqrtf(8.0f * (float)r + 1.0f) - 1.0f) * 0.5f);
-        while (i * (i + 1) / 2 > r) --i;
-        while ((i + 1) * (i + 2) / 2 <= r) ++i;
-        t.m = (int)i, t.n = (int)(r - i * (i + 1) / 2);
-    } else {
-        const uint32_t band = r / (8 * nt), rows = min(8u, mt - band * 8), q = r - band * 8 * nt, n = q / rows;
-        t.m = (int)(band * 8 + q - n * rows), t.n = (int)n;
-    }
+    t.split = (int)s;
+    t.tile = (int)(id - s * per);
+    static_cast<MmAt&>(t) = mm_at<B>(p, (uint32_t)t.tile);
     return t;
 }
 
-// E: end(batch, row, first column, 4 sums, mirror) takes 4 neighbouring outputs (mirror: for those across the diagonal too). One with E::kRows takes a wavefront's
+// E: end(row, first column, 4 sums) takes 4 neighbouring outputs. One with E::kRows takes a wavefront's
 // row instead, end.row<FN>(row, first column of its part, lane, sums), and no splits.
 template <class E, class = void>
 struct MmRows : std::false_type {};
@@ -239,22 +300,15 @@ struct MmRows<E, std::enable_if_t<E::kRows>> : std::true_type {};
 template <class T, int B, bool AK, bool BK, bool ENDS, class E>
 __global__ __launch_bounds__(MmTile<B>::kThreads, 2) void mm_kernel(Mm p, E end) {
     typedef MmTile<B> G;
-    __shared__ __attribute__((aligned(16))) uint16_t as0[B * kMmTurn], as1[B * kMmTurn], bs0[B * kMmTurn], bs1[B * kMmTurn];
-    __shared__ __attribute__((aligned(16))) uint16_t as2[G::kStages > 2 ? B * kMmTurn : 8], as3[G::kStages > 2 ? B * kMmTurn : 8],
-        bs2[G::kStages > 2 ? B * kMmTurn : 8], bs3[G::kStages > 2 ? B * kMmTurn : 8];
-    uint16_t* as[G::kStages];
-    uint16_t* bs[G::kStages];
-    as[0] = as0, as[1] = as1, bs[0] = bs0, bs[1] = bs1;
-    if constexpr (G::kStages > 2) as[2] = as2, as[3] = as3, bs[2] = bs2, bs[3] = bs3;
+    MM_PLACES(B, as, bs);
     const MmId id = mm_id<B>(p);
     const int total = p.turns * p.segs, t0 = (int)((int64_t)total * id.split / p.splits), t1 = (int)((int64_t)total * (id.split + 1) / p.splits);
     MmAcc acc[G::FM][G::FN] = {};
-    MmCore<T, B, AK, BK, ENDS>::run(p, id.batch, id.m * B, id.n * B, t0, t1, as, bs, acc);
+    MmCore<T, B, AK, BK, ENDS>::run(p, id.m * B, id.n * B, t0, t1, as, bs, acc);
     const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
     const int m = id.m * B + G::wave_m(w) + (lane & 15), n = id.n * B + G::wave_n(w) + 4 * (lane >> 4);
     if (p.splits > 1) {
-        f32x4* const part = reinterpret_cast<f32x4*>(p.part) +
-                            (((int64_t)(id.batch * p.splits + id.split) * (gridDim.x / (uint32_t)(p.batches * p.splits)) + id.tile) * G::kWaves + w) * (G::FM * G::FN * 64) + lane;
+        f32x4* const part = reinterpret_cast<f32x4*>(p.part) + (((int64_t)id.split * (gridDim.x / (uint32_t)p.splits) + id.tile) * G::kWaves + w) * (G::FM * G::FN * 64) + lane;
 #pragma unroll
         for (int i = 0; i < G::FM; ++i)
 #pragma unroll
@@ -270,7 +324,7 @@ __global__ __launch_bounds__(MmTile<B>::kThreads, 2) void mm_kernel(Mm p, E end)
         }
 #pragma unroll
         for (int j = 0; j < G::FN; ++j) {
-            if constexpr (!MmRows<E>::value) end(id.batch, m + 16 * i, n + 16 * j, acc[i][j], p.sym && id.m != id.n);
+            if constexpr (!MmRows<E>::value) end(m + 16 * i, n + 16 * j, acc[i][j]);
         }
     }
 }
@@ -280,10 +334,9 @@ template <int B, class E>
 __global__ __launch_bounds__(256) void mm_join_kernel(Mm p, E end, uint32_t tiles) {
     typedef MmTile<B> G;
     constexpr uint32_t kBlocks = B * B / 1024;
-    const uint32_t id = blockIdx.x / kBlocks, at = blockIdx.x % kBlocks * 256 + threadIdx.x, lane = at & 63, slot = at >> 6;
-    const uint32_t batch = id / tiles, tile = id - batch * tiles;
+    const uint32_t tile = blockIdx.x / kBlocks, at = blockIdx.x % kBlocks * 256 + threadIdx.x, lane = at & 63, slot = at >> 6;
     const int64_t size = (int64_t)tiles * (B * B / 4);
-    const f32x4* q = reinterpret_cast<const f32x4*>(p.part) + batch * (int64_t)p.splits * size + (int64_t)tile * (B * B / 4) + at;
+    const f32x4* q = reinterpret_cast<const f32x4*>(p.part) + (int64_t)tile * (B * B / 4) + at;
     f32x4 v = {};
     int s = 0;
     for (; s + 4 <= p.splits; s += 4, q += 4 * size) {
@@ -295,28 +348,17 @@ __global__ __launch_bounds__(256) void mm_join_kernel(Mm p, E end, uint32_t tile
     }
     for (; s < p.splits; ++s, q += size) v += *q;
     const uint32_t w = slot / (G::FM * G::FN), e = slot % (G::FM * G::FN);
-    uint32_t tm, tn;
-    const uint32_t mt = (uint32_t)((p.m + B - 1) / B), nt = (uint32_t)((p.n + B - 1) / B);
-    if (p.sym) {
-        uint32_t i = (uint32_t)((sqrtf(8.0f * (float)tile + 1.0f) - 1.0f) * 0.5f);
-        while (i * (i + 1) / 2 > tile) --i;
-        while ((i + 1) * (i + 2) / 2 <= tile) ++i;
-        tm = i, tn = tile - i * (i + 1) / 2;
-    } else {
-        const uint32_t band = tile / (8 * nt), rows = min(8u, mt - band * 8), r = tile - band * 8 * nt;
-        tn = r / rows, tm = band * 8 + r - tn * rows;
-    }
-    end((int)batch, (int)tm * B + G::wave_m((int)w) + (int)(lane & 15) + 16 * (int)(e / G::FN),
-        (int)tn * B + G::wave_n((int)w) + 4 * (int)(lane >> 4) + 16 * (int)(e % G::FN), v, p.sym && tm != tn);
+    const MmAt id = mm_at<B>(p, tile);
+    end(id.m * B + G::wave_m((int)w) + (int)(lane & 15) + 16 * (int)(e / G::FN), id.n * B + G::wave_n((int)w) + 4 * (int)(lane >> 4) + 16 * (int)(e % G::FN), v);
 }
 
 template <class T, int B, bool AK, bool BK, bool ENDS, class E>
 hipError_t mm_launch(const Mm& p, const E& end, hipStream_t st) {
     const uint32_t tiles = MmTile<B>::tiles(p);
     if (tiles == 0) return hipSuccess;
-    mm_kernel<T, B, AK, BK, ENDS, E><<<tiles * (uint32_t)(p.batches * p.splits), MmTile<B>::kThreads, 0, st>>>(p, end);
+    mm_kernel<T, B, AK, BK, ENDS, E><<<tiles * (uint32_t)p.splits, MmTile<B>::kThreads, 0, st>>>(p, end);
     if constexpr (!MmRows<E>::value)
-        if (p.splits > 1) mm_join_kernel<B, E><<<tiles * (uint32_t)p.batches * (B * B / 1024), 256, 0, st>>>(p, end, tiles);
+        if (p.splits > 1) mm_join_kernel<B, E><<<tiles * (B * B / 1024), 256, 0, st>>>(p, end, tiles);
     return hipGetLastError();
 }
 

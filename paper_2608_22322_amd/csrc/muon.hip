@@ -20,14 +20,17 @@ __device__ __forceinline__ double block_sum(double v) {
 }
 
 // m <- beta m + (1 - beta) g (binary64, rounded once), its code, and the update u = m or beta m + (1 - beta) g as fp32 with its sum of squares. A
-// wavefront takes blocks of 256 elements, four a lane; a workgroup kMomentum of them.
+// wavefront takes blocks of 256 elements, four a lane; a workgroup kSquareUnit elements.
 template <int G, bool UF>
-__global__ __launch_bounds__(256) void momentum_kernel(MuonList l, MuonArgs a, int64_t n, int64_t pitch, float* u, double* sums) {
-    const MuonItem& t = l.t[blockIdx.y];
+__global__ __launch_bounds__(256) void momentum_kernel(MomentumList l, MuonArgs a, double* sums) {
+    int item = 0;
+    while (item + 1 < l.count && blockIdx.x >= l.begin[item + 1]) ++item;
+    const MomentumItem& t = l.t[item];
+    const int64_t n = t.n, unit = blockIdx.x - l.begin[item];
     const gp<const void> g = to_g(t.g);
-    float* const out = u + blockIdx.y * pitch;
+    float* const out = t.u;
     const int lane = threadIdx.x & 63;
-    const int64_t begin = (int64_t)blockIdx.x * kMomentum + (threadIdx.x >> 6) * 256, end = min(n, (int64_t)(blockIdx.x + 1) * kMomentum);
+    const int64_t begin = unit * kSquareUnit + (threadIdx.x >> 6) * 256, end = min(n, (unit + 1) * kSquareUnit);
     double s = 0;
     for (int64_t b = begin; b < end; b += 1024) {
         const int64_t e = b + 4 * lane;
@@ -89,19 +92,19 @@ __global__ __launch_bounds__(256) void momentum_kernel(MuonList l, MuonArgs a, i
         }
     }
     s = block_sum(s);
-    if (threadIdx.x == 0) sums[(int64_t)blockIdx.y * gridDim.x + blockIdx.x] = s;
+    if (threadIdx.x == 0) sums[blockIdx.x] = s;
 }
 
 }  // namespace
 
-hipError_t launch_momentum(const MuonArgs& a, const MuonList& l, int64_t n, int64_t pitch, int32_t parts, int32_t batches, float* u, double* sums, hipStream_t s) {
-    const dim3 grid((uint32_t)parts, (uint32_t)batches);
+hipError_t launch_momentum(const MuonArgs& a, const MomentumList& l, double* sums, hipStream_t s) {
+    const uint32_t grid = l.begin[l.count];
     if (a.grad_bf16) {
-        if (a.uf8) momentum_kernel<G_BF16, true><<<grid, 256, 0, s>>>(l, a, n, pitch, u, sums);
-        else momentum_kernel<G_BF16, false><<<grid, 256, 0, s>>>(l, a, n, pitch, u, sums);
+        if (a.uf8) momentum_kernel<G_BF16, true><<<grid, 256, 0, s>>>(l, a, sums);
+        else momentum_kernel<G_BF16, false><<<grid, 256, 0, s>>>(l, a, sums);
     } else {
-        if (a.uf8) momentum_kernel<G_F32, true><<<grid, 256, 0, s>>>(l, a, n, pitch, u, sums);
-        else momentum_kernel<G_F32, false><<<grid, 256, 0, s>>>(l, a, n, pitch, u, sums);
+        if (a.uf8) momentum_kernel<G_F32, true><<<grid, 256, 0, s>>>(l, a, sums);
+        else momentum_kernel<G_F32, false><<<grid, 256, 0, s>>>(l, a, sums);
     }
     return hipGetLastError();
 }

@@ -1,15 +1,21 @@
-// Orthogonalised updates: Newton-Schulz products of 16-bit parts on the matrix cores, and the momentum step around them.
+// Orthogonalised updates: Newton-Schulz products of 16-bit parts on the matrix cores.
 //
 // X0 = G / (|G| + eps) in the Frobenius norm, then X <- a X + (b A + c A A) X with A = X X^T, or for more rows than columns
-// X <- a X + X (b A + c A A) with A = X^T X. A and A A are symmetric: the tiles below the diagonal are computed and written twice.
+// X <- a X + X (b A + c A A) with A = X^T X. A and A A are symmetric: the tiles on and below the diagonal are computed and written twice.
 //
 // Held between the products as fp16, scaled by powers of two, either one number (11 bits) or the sum of two (22 bits; the
 // products hi hi + hi lo + lo hi). bf16 at the same speed has 8 bits: the products amplify what is lost in X by up to a^steps in
 // directions of small singular values, and the result is 1e-2 off instead of 1.4e-3 (normal matrices). X0 is scaled by a power of two alone, so a bf16 G
 // is held exactly; 1 / |G| goes into the sums of the first step.
+//
+// A step is three launches for all the matrices of a group. Where whole tiles would leave compute units idle (136 tiles for 256 of them, or matrices of
+// different sizes), the group's turns are dealt out evenly instead: a workgroup takes a stretch of them, across tiles, and tiles
+// that two or more worked on are joined in a second launch, in order.
 #include <algorithm>
 #include <cmath>
+#include <cstring>
 
+#include "mm_cut.hpp"
 #include "mm_device.hpp"
 #include "ortho_internal.hpp"
 
@@ -25,11 +31,11 @@ typedef f16 f16x4 __attribute__((ext_vector_type(4)));
 constexpr float kXScale = 1024.0f, kAScale = 1024.0f, kBScale = 256.0f;
 
 struct Norm {
-    double scale;  // 2^k with |G| + eps = nu 2^-k, nu in [1/2, 1)
+    double scale;     // 2^k with |G| + eps = nu 2^-k, nu in [1/2, 1)
     float inv, inv2;  // 1 / nu, 1 / nu^2
 };
 
-// Sum of squares of a matrix's slab, binary64 and in a fixed order.
+// The workgroup's sum, in a fixed order.
 __device__ __forceinline__ double block_sum(double v) {
     __shared__ double part[4];
     for (int m = 1; m < 64; m <<= 1) v += __shfl_xor(v, m);
@@ -38,6 +44,7 @@ __device__ __forceinline__ double block_sum(double v) {
     return (part[0] + part[1]) + (part[2] + part[3]);
 }
 
+// Sums of squares of a matrix's slabs.
 template <typename T>
 __global__ __launch_bounds__(256) void square_kernel(const T* x, int64_t ld, int64_t rows, int cols, double* sums) {
     const int chunks = (cols + 7) / 8;
@@ -57,14 +64,11 @@ __global__ __launch_bounds__(256) void square_kernel(const T* x, int64_t ld, int
     if (threadIdx.x == 0) sums[blockIdx.x] = s;
 }
 
-// The norm of each matrix from its partial sums. A zero matrix gives zeros, one with an infinity or a NaN gives NaN.
-__global__ __launch_bounds__(64) void norm_kernel(const double* sums, int count, double eps, Norm* norm) {
-    const double* const p = sums + (int64_t)blockIdx.x * count;
+// The norm of a matrix from its partial sums, by a workgroup. A zero matrix gives zeros, one with an infinity or a NaN gives NaN.
+__device__ __forceinline__ Norm norm_of(const double* sums, uint32_t count, double eps) {
     double s = 0;
-    for (int i = threadIdx.x; i < count; i += 64) s += p[i];
-    for (int m = 1; m < 64; m <<= 1) s += __shfl_xor(s, m);
-    if (threadIdx.x) return;
-    const double n = sqrt(s) + eps;
+    for (uint32_t i = threadIdx.x; i < count; i += 256) s += sums[i];
+    const double n = sqrt(block_sum(s)) + eps;
     Norm r;
     if (!(n < __builtin_inf())) {
         r.scale = 1.0;
@@ -79,337 +83,680 @@ __global__ __launch_bounds__(64) void norm_kernel(const double* sums, int count,
         r.inv = (float)(1.0 / f);
         r.inv2 = (float)(1.0 / (f * f));
     }
-    norm[blockIdx.x] = r;
+    return r;
 }
 
 __device__ __forceinline__ uint32_t pair(f16 a, f16 b) {
     return (uint32_t)__builtin_bit_cast(uint16_t, a) | (uint32_t)__builtin_bit_cast(uint16_t, b) << 16;
 }
 
-// x (fp32 or bf16) -> X0 2^10 as one or two fp16 parts, padded with zeros. 8 columns a lane.
+struct PackList {
+    struct {
+        const void* x;
+        int64_t ld;
+        uint16_t* out;
+        int32_t rows, cols, rp, cp;
+    } t[kOrthoGroup];
+    uint32_t begin[kOrthoGroup + 1];  // workgroups (2048 elements each)
+    uint32_t sums[kOrthoGroup + 1];   // partial sums of squares
+    int32_t count;
+};
+
+// x (fp32 or bf16) -> X0 2^10 as one or two fp16 parts, padded with zeros: 8 columns a lane. Each workgroup takes the norm from its partial sums by itself (a launch
+// less); the first of a matrix writes it for the first step's sums.
 template <typename T>
-__global__ __launch_bounds__(256) void pack_kernel(const T* x, int64_t ld, int64_t batch, int rows, int cols, int rp, int cp, int parts, const Norm* norm,
-                                                   uint16_t* out) {
-    const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
-    const int chunks = cp / 8;
-    if (i >= (int64_t)rp * chunks) return;
-    const int r = (int)(i / chunks), c = (int)(i - (int64_t)r * chunks) * 8, b = blockIdx.y;
+__global__ __launch_bounds__(256) void pack_kernel(PackList l, int parts, double eps, const double* sums, Norm* norms) {
+    int b = 0;
+    while (b + 1 < l.count && blockIdx.x >= l.begin[b + 1]) ++b;
+    const auto& t = l.t[b];
+    const Norm norm = norm_of(sums + l.sums[b], l.sums[b + 1] - l.sums[b], eps);
+    if (threadIdx.x == 0 && blockIdx.x == l.begin[b]) norms[b] = norm;
+    const int64_t i = (int64_t)(blockIdx.x - l.begin[b]) * 256 + threadIdx.x;
+    const int chunks = t.cp / 8, r = (int)(i / chunks), c = (int)(i - (int64_t)r * chunks) * 8;
     float v[8] = {};
-    if (r < rows) {
+    if (r < t.rows) {
         Chunk<T> k;
-        load_chunk(k, x + b * batch + r * ld, c, cols);
+        load_chunk(k, static_cast<const T*>(t.x) + r * t.ld, c, t.cols);
         k.get(v);
     }
-    const double s = norm[b].scale * (double)kXScale;
+    const double s = norm.scale * (double)kXScale;
     u32x4 hi, lo;
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
-        f16 h[2], l[2];
+        f16 h[2], w[2];
 #pragma unroll
         for (int e = 0; e < 2; ++e) {
             const float y = (float)((double)v[2 * j + e] * s);
             h[e] = (f16)y;
-            l[e] = (f16)(y - (float)h[e]);
+            w[e] = (f16)(y - (float)h[e]);
         }
         hi[j] = pair(h[0], h[1]);
-        lo[j] = pair(l[0], l[1]);
+        lo[j] = pair(w[0], w[1]);
     }
-    const int64_t size = (int64_t)rp * cp;
-    uint16_t* const o = out + b * parts * size + (int64_t)r * cp + c;
+    uint16_t* const o = t.out + (int64_t)r * t.cp + c;
     *reinterpret_cast<u32x4*>(o) = hi;
-    if (parts > 1) *reinterpret_cast<u32x4*>(o + size) = lo;
+    if (parts > 1) *reinterpret_cast<u32x4*>(o + (int64_t)t.rp * t.cp) = lo;
 }
 
-// A matrix of the workspace: size = side times side, the low part behind the high one.
+// A matrix of the workspace, the low part behind the high one.
 struct Held {
     uint16_t* p;
     int64_t size;
     int32_t ld, parts;
-    __device__ __forceinline__ f32x4 get(int b, int m, int n) const {
-        const uint16_t* const q = p + b * parts * size + (int64_t)m * ld + n;
+    __device__ __forceinline__ f32x4 get(int m, int n) const {
+        const uint16_t* const q = p + (int64_t)m * ld + n;
         f32x4 v = __builtin_convertvector(*reinterpret_cast<const f16x4*>(q), f32x4);
         if (parts > 1) v += __builtin_convertvector(*reinterpret_cast<const f16x4*>(q + size), f32x4);
         return v;
     }
-    __device__ __forceinline__ void put(int b, int m, int n, f32x4 v, bool mirror) const {
+    __device__ __forceinline__ void put(int m, int n, f32x4 v, bool mirror) const {
         const f16x4 h = __builtin_convertvector(v, f16x4), l = __builtin_convertvector(v - __builtin_convertvector(h, f32x4), f16x4);
-        uint16_t* const q = p + b * parts * size;
-        *reinterpret_cast<f16x4*>(q + (int64_t)m * ld + n) = h;
-        if (parts > 1) *reinterpret_cast<f16x4*>(q + size + (int64_t)m * ld + n) = l;
+        *reinterpret_cast<f16x4*>(p + (int64_t)m * ld + n) = h;
+        if (parts > 1) *reinterpret_cast<f16x4*>(p + size + (int64_t)m * ld + n) = l;
         if (mirror) {
 #pragma unroll
             for (int r = 0; r < 4; ++r) {
-                *reinterpret_cast<f16*>(q + (int64_t)(n + r) * ld + m) = h[r];
-                if (parts > 1) *reinterpret_cast<f16*>(q + size + (int64_t)(n + r) * ld + m) = l[r];
+                *reinterpret_cast<f16*>(p + (int64_t)(n + r) * ld + m) = h[r];
+                if (parts > 1) *reinterpret_cast<f16*>(p + size + (int64_t)(n + r) * ld + m) = l[r];
             }
         }
     }
+    __device__ __forceinline__ MmOperand operand(int rows) const { return {p, size, ld, rows, ld}; }
 };
 
-// A = X X^T.
-struct EndGram {
-    Held a;
-    const Norm* norm;  // first step: A = X0 X0^T / nu^2
-    __device__ __forceinline__ void operator()(int b, int m, int n, f32x4 v, bool mirror) const {
-        if (m >= a.ld || n >= a.ld) return;
-        float s = kAScale / (kXScale * kXScale);
-        if (norm) s *= norm[b].inv2;
-        a.put(b, m, n, v * s, mirror);
-    }
-};
+// The products of a step: A = X X^T, B = b A + c A A, and a X + B X as the next X, the result, or a step of the parameters.
+enum Kind : int { kGram, kPoly, kNext, kOut, kStep };
+__host__ __device__ constexpr bool square_kind(int kind) { return kind == kGram || kind == kPoly; }
 
-// B = b A + c A A.
-struct EndPoly {
-    Held a, o;
-    float cb, cc;
-    __device__ __forceinline__ void operator()(int b, int m, int n, f32x4 v, bool mirror) const {
-        if (m >= a.ld || n >= a.ld) return;
-        o.put(b, m, n, a.get(b, m, n) * (cb * (kBScale / kAScale)) + v * (cc * (kBScale / (kAScale * kAScale))), mirror);
-    }
-};
-
-// X <- a X + B X: the next X, the result, or a step of the parameters.
-struct EndBase {
-    Held x;
-    const Norm* norm;
-    float ca;
-    int32_t rows, cols;  // of the output
-    __device__ __forceinline__ f32x4 next(int b, int m, int n, f32x4 v) const {
-        v = x.get(b, m, n) * ca + v * (1.0f / kBScale);
-        if (norm) v *= norm[b].inv;
-        return v;
-    }
-};
-struct EndNext : EndBase {
-    Held o;
-    __device__ __forceinline__ void operator()(int b, int m, int n, f32x4 v, bool) const {
-        if (m < rows && n < cols) o.put(b, m, n, next(b, m, n, v), false);
-    }
-};
-struct EndOut : EndBase {
+struct OrthoLaunch {
+    OrthoItem it[kOrthoGroup];
+    int64_t begin[kOrthoGroup + 1];  // first tile of each item, or, with slots, first turn
+    int64_t slots;                   // workgroups that the turns are dealt out to; 0: a tile a workgroup
+    int32_t count, parts, from, first;  // from: which place X is in; first: the first step
+    float ca, cb, cc;
+    const Norm* norms;
+    float* part;  // [2 slots][a tile in the lanes' order]
+    double decay;
     void* out;
-    int64_t ld;
+    int64_t ldout;
     int32_t out_bf16;
-    __device__ __forceinline__ void operator()(int b, int m, int n, f32x4 v, bool) const {
-        if (m >= rows || n >= cols) return;
-        v = next(b, m, n, v) * (1.0f / kXScale);
-        const int64_t i = m * ld + n;
-        const int in = min(4, cols - n);
-        if (out_bf16) {
-            bf16* const p = static_cast<bf16*>(out) + i;
-            typedef uint32_t u32x2_a2 __attribute__((ext_vector_type(2), aligned(2)));
-            if (in == 4) {
-                *reinterpret_cast<u32x2_a2*>(p) = u32x2{pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3])};
-                return;
-            }
-#pragma unroll
-            for (int r = 0; r < 3; ++r)
-                if (r < in) al::put(p + r, v[r]);
-        } else {
-            float* const p = static_cast<float*>(out) + i;
-            typedef float f32x4_a4 __attribute__((ext_vector_type(4), aligned(4)));
-            if (in == 4) {
-                *reinterpret_cast<f32x4_a4*>(p) = v;
-                return;
-            }
-#pragma unroll
-            for (int r = 0; r < 3; ++r)
-                if (r < in) p[r] = v[r];
-        }
-    }
 };
-struct EndStep : EndBase {
-    float* p[kMuonBatch];
-    double decay, step;
-    __device__ __forceinline__ void operator()(int b, int m, int n, f32x4 v, bool) const {
-        if (m >= rows || n >= cols) return;
-        v = next(b, m, n, v) * (1.0f / kXScale);
-        float* const q = p[b] + (int64_t)m * cols + n;
-        const int in = min(4, cols - n);
+
+__host__ __device__ inline int64_t item_tiles(const OrthoItem& t, int kind, int tile) {
+    if (!square_kind(kind)) return (int64_t)((t.rp + tile - 1) / tile) * ((t.cp + tile - 1) / tile);
+    const int64_t s = ((t.rp < t.cp ? t.rp : t.cp) + tile - 1) / tile;
+    return s * (s + 1) / 2;
+}
+__host__ __device__ inline int32_t item_turns(const OrthoItem& t, int kind, int parts) {
+    const int32_t k = kind == kGram ? (t.rp > t.cp ? t.rp : t.cp) : t.rp < t.cp ? t.rp : t.cp;
+    return k / kMmTurn * (parts > 1 ? 3 : 1);
+}
+
+// One item's product.
+template <int KIND>
+struct Task {
+    const OrthoLaunch& a;
+    const OrthoItem t;
+    int item;
+    bool tall;
+    int32_t dp;
+    Held x, g, b;
+    __device__ __forceinline__ Task(const OrthoLaunch& l, int i) : a(l), t(l.it[i]), item(i) {
+        tall = t.rp > t.cp || (t.rp == t.cp && t.rows > t.cols);
+        dp = min(t.rp, t.cp);
+        x = {a.from ? t.x[1] : t.x[0], (int64_t)t.rp * t.cp, t.cp, a.parts};
+        g = {t.a, (int64_t)dp * dp, dp, a.parts};
+        b = {t.a + a.parts * g.size, g.size, dp, a.parts};
+    }
+    __device__ __forceinline__ Mm product() const {
+        Mm p;
+        p.segs = a.parts > 1 ? 3 : 1;
+        p.amask = a.parts > 1 ? 4u : 0u;
+        p.bmask = a.parts > 1 ? 2u : 0u;
+        p.splits = 1;
+        p.part = nullptr;
+        p.sym = square_kind(KIND);
+        p.m = square_kind(KIND) ? dp : t.rp;
+        p.n = square_kind(KIND) ? dp : t.cp;
+        p.turns = item_turns(t, KIND, 1);
+        const MmOperand ox = x.operand(t.rp);
+        p.a = KIND == kGram ? ox : KIND == kPoly ? g.operand(dp) : tall ? ox : b.operand(dp);
+        p.b = KIND == kGram ? ox : KIND == kPoly ? g.operand(dp) : tall ? b.operand(dp) : ox;
+        return p;
+    }
+    // What the product is combined with: sum * factor() + from() * other(), and that times after().
+    __device__ __forceinline__ const Held& from() const { return KIND == kPoly ? g : x; }
+    __device__ __forceinline__ float factor() const {
+        return KIND == kGram ? kAScale / (kXScale * kXScale) * (a.first ? a.norms[item].inv2 : 1.0f)
+                             : KIND == kPoly ? a.cc * (kBScale / (kAScale * kAScale)) : 1.0f / kBScale;
+    }
+    __device__ __forceinline__ float other() const { return KIND == kPoly ? a.cb * (kBScale / kAScale) : a.ca; }
+    __device__ __forceinline__ float after() const { return !square_kind(KIND) && a.first ? a.norms[item].inv : 1.0f; }
+    // where it goes, for what stays in the workspace
+    __device__ __forceinline__ Held to() const {
+        if (KIND == kGram) return g;
+        if (KIND == kPoly) return b;
+        return {a.from ? t.x[0] : t.x[1], x.size, x.ld, a.parts};
+    }
+    __device__ __forceinline__ int32_t rows() const { return square_kind(KIND) ? dp : t.rp; }
+    __device__ __forceinline__ int32_t cols() const { return square_kind(KIND) ? dp : t.cp; }
+
+    // 4 neighbouring values of the result or of the parameters
+    __device__ __forceinline__ void write(int m, int n, f32x4 v) const {
+        if (m >= t.rows || n >= t.cols) return;
+        v *= 1.0f / kXScale;
+        const int in = min(4, t.cols - n);
         typedef float f32x4_a4 __attribute__((ext_vector_type(4), aligned(4)));
-        if (in == 4) {
-            f32x4 o = *reinterpret_cast<const f32x4_a4*>(q);
+        typedef uint32_t u32x2_a2 __attribute__((ext_vector_type(2), aligned(2)));
+        if constexpr (KIND == kStep) {
+            float* const q = t.p + (int64_t)m * t.cols + n;
+            if (in == 4) {
+                f32x4 o = *reinterpret_cast<const f32x4_a4*>(q);
 #pragma unroll
-            for (int r = 0; r < 4; ++r) o[r] = (float)((double)o[r] * decay - step * (double)v[r]);
-            *reinterpret_cast<f32x4_a4*>(q) = o;
-            return;
+                for (int r = 0; r < 4; ++r) o[r] = (float)((double)o[r] * a.decay - t.step * (double)v[r]);
+                *reinterpret_cast<f32x4_a4*>(q) = o;
+            } else {
+#pragma unroll
+                for (int r = 0; r < 3; ++r)
+                    if (r < in) q[r] = (float)((double)q[r] * a.decay - t.step * (double)v[r]);
+            }
+        } else if (a.out_bf16) {
+            bf16* const q = static_cast<bf16*>(a.out) + m * a.ldout + n;
+            if (in == 4) {
+                *reinterpret_cast<u32x2_a2*>(q) = u32x2{pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3])};
+            } else {
+#pragma unroll
+                for (int r = 0; r < 3; ++r)
+                    if (r < in) al::put(q + r, v[r]);
+            }
+        } else {
+            float* const q = static_cast<float*>(a.out) + m * a.ldout + n;
+            if (in == 4) {
+                *reinterpret_cast<f32x4_a4*>(q) = v;
+            } else {
+#pragma unroll
+                for (int r = 0; r < 3; ++r)
+                    if (r < in) q[r] = v[r];
+            }
         }
-#pragma unroll
-        for (int r = 0; r < 3; ++r)
-            if (r < in) q[r] = (float)((double)q[r] * decay - step * (double)v[r]);
+    }
+    // 4 neighbouring outputs from their sums
+    __device__ __forceinline__ void end(int m, int n, f32x4 v, bool mirror) const {
+        if (m >= rows() || n >= cols()) return;
+        v *= factor();
+        if constexpr (KIND != kGram) v += from().get(m, n) * other();
+        v *= after();
+        if constexpr (KIND == kOut || KIND == kStep)
+            write(m, n, v);
+        else
+            to().put(m, n, v, mirror);
     }
 };
 
-template <bool AK, bool BK, class E>
-hipError_t product(const MmCut& cut, Mm p, const E& end, hipStream_t st) {
-    p.splits = cut.splits;
-    if (cut.tile == 256) return mm_launch<f16, 256, AK, BK, false>(p, end, st);
-    if (cut.tile == 128) return mm_launch<f16, 128, AK, BK, false>(p, end, st);
-    return mm_launch<f16, 64, AK, BK, false>(p, end, st);
-}
-
-// The products of a batch whose X0 lies at x1; the last step's outputs go to `last`.
-template <class E>
-hipError_t iterate(const OrthoPlan& p, const OrthoCoefs& k, E last, char* ws, hipStream_t st) {
-    const int64_t xs = (int64_t)p.rp * p.cp, ds = (int64_t)p.dp * p.dp;
-    const Norm* const norm = reinterpret_cast<const Norm*>(ws + p.norm_off);
-    Held x[2] = {{reinterpret_cast<uint16_t*>(ws + p.x1_off), xs, p.cp, p.parts}, {reinterpret_cast<uint16_t*>(ws + p.x0_off), xs, p.cp, p.parts}};
-    const Held a = {reinterpret_cast<uint16_t*>(ws + p.a_off), ds, p.dp, p.parts}, b = {reinterpret_cast<uint16_t*>(ws + p.b_off), ds, p.dp, p.parts};
-    const auto operand = [&](const Held& h, int rows) { return MmOperand{h.p, h.parts * h.size, h.size, h.ld, rows, h.ld}; };
-    Mm q = {};
-    q.segs = p.parts == 1 ? 1 : 3;
-    q.amask = p.parts == 1 ? 0u : 4u;
-    q.bmask = p.parts == 1 ? 0u : 2u;
-    q.batches = p.batches;
-    q.part = reinterpret_cast<float*>(ws + p.part_off);
-    for (int i = 0; i < k.steps; ++i) {
-        const Held &from = x[i & 1], &to = x[(i & 1) ^ 1];
-        const Norm* const first = i == 0 ? norm : nullptr;
-        const MmOperand ox = operand(from, p.rp), oa = operand(a, p.dp), ob = operand(b, p.dp);
-        hipError_t e;
-        Mm g = q;
-        g.a = g.b = ox;
-        g.m = g.n = p.dp;
-        g.turns = (p.tall ? p.rp : p.cp) / kMmTurn;
-        g.sym = 1;
-        const EndGram gram = {a, first};
-        if ((e = p.tall ? product<false, false>(p.g1, g, gram, st) : product<true, true>(p.g1, g, gram, st)) != hipSuccess) return e;
-        g.a = g.b = oa;
-        g.turns = p.dp / kMmTurn;
-        const EndPoly poly = {a, b, k.b, k.c};
-        if ((e = product<true, true>(p.g2, g, poly, st)) != hipSuccess) return e;
-        g.sym = 0;
-        g.m = p.rp;
-        g.n = p.cp;
-        g.a = p.tall ? ox : ob;
-        g.b = p.tall ? ob : ox;
-        const auto third = [&](auto end) {
-            end.x = from;
-            end.norm = first;
-            end.ca = k.a;
-            return p.tall ? product<true, true>(p.g3, g, end, st) : product<true, false>(p.g3, g, end, st);
-        };
-        if (i + 1 < k.steps) {
-            EndNext next;
-            next.rows = p.rp;
-            next.cols = p.cp;
-            next.o = to;
-            e = third(next);
-        } else {
-            last.rows = (int32_t)p.rows;
-            last.cols = (int32_t)p.cols;
-            e = third(last);
-        }
-        if (e != hipSuccess) return e;
+// A tile of one part in LDS, in the places of the turns (64 rows in each): rows of B values whose 16-byte pieces are exchanged by the row, so that the lanes' quads
+// (16 rows at once) and whole rows both meet all banks. The tile's ends go through it: the lanes' own 8-byte pieces of 16 rows at
+// a time take 25 us of memory accesses for a 256 x 256 tile.
+template <int B>
+struct Image {
+    typedef MmTile<B> G;
+    static constexpr int kMask = B == 64 ? 7 : 15;
+    typedef __attribute__((address_space(3))) uint16_t* lds_u16;
+    typedef __attribute__((address_space(3))) u32x4* lds_u32x4;
+    typedef __attribute__((address_space(3))) f16x4* lds_f16x4;
+    typedef __attribute__((address_space(3))) f16* lds_f16;
+    uint32_t a0, a1, b0, b1;  // LDS addresses (a choice among pointers would be a generic one)
+    __device__ __forceinline__ Image(uint16_t* const (&as)[G::kStages], uint16_t* const (&bs)[G::kStages])
+        : a0((uint32_t)(uintptr_t)(lds_u16)as[0]), a1((uint32_t)(uintptr_t)(lds_u16)as[1]), b0((uint32_t)(uintptr_t)(lds_u16)bs[0]),
+          b1((uint32_t)(uintptr_t)(lds_u16)bs[1]) {}
+    // rows 64 q .. 64 q + 63
+    __device__ __forceinline__ uint32_t rows(int q) const { return B == 64 ? a0 : B == 128 ? (q & 1 ? a1 : a0) : q & 2 ? (q & 1 ? b1 : b0) : (q & 1 ? a1 : a0); }
+    // bytes from those on
+    static __device__ __forceinline__ uint32_t offset(int row, int col) {
+        return (uint32_t)((row & 63) * B + ((((col >> 3) ^ row) & kMask) << 3) + (B > 128 ? col & 128 : 0) + (col & 7)) * 2u;
     }
-    return hipSuccess;
+    __device__ __forceinline__ lds_u32x4 piece(int k) const {
+        const int row = k / (B / 8), col = k % (B / 8) * 8;
+        return (lds_u32x4)(uintptr_t)(rows(row >> 6) + offset(row, col));
+    }
+    // f(sums, their quad) for the lane's quads: row r + 16 i, columns c + 16 j ..
+    template <class F>
+    __device__ __forceinline__ void quads(int r, int c, MmAcc (&acc)[G::FM][G::FN], const F& f) const {
+        uint32_t off = offset(r, c);
+        asm volatile("" : "+v"(off));  // (32 addresses a pass would not stay in registers)
+#pragma unroll
+        for (int i = 0; i < G::FM; ++i) {
+            __builtin_amdgcn_sched_barrier(0);
+            const uint32_t q = rows(__builtin_amdgcn_readfirstlane(r >> 6) + i / 4) + i % 4 * 32 * B;
+#pragma unroll
+            for (int j = 0; j < G::FN; ++j) f(acc[i][j], (lds_f16x4)(uintptr_t)(q + (off ^ (uint32_t)(j << 5))));
+        }
+        __builtin_amdgcn_sched_barrier(0);
+    }
+    // the lane's quads across the diagonal: element e of a quad at row c + 16 j + e, column r + 16 i
+    __device__ __forceinline__ void across(int r, int c, const MmAcc (&acc)[G::FM][G::FN]) const {
+        uint32_t off[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            off[e] = offset(c + e, r);
+            asm volatile("" : "+v"(off[e]));
+        }
+        const uint32_t q = rows(__builtin_amdgcn_readfirstlane(c >> 6));
+#pragma unroll
+        for (int i = 0; i < G::FM; ++i) {
+            __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+            for (int j = 0; j < G::FN; ++j) {
+                const f16x4 h = __builtin_convertvector(acc[i][j], f16x4);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) *(lds_f16)(uintptr_t)(q + j * 32 * B + (off[e] ^ (uint32_t)(i << 5))) = h[e];
+            }
+        }
+        __builtin_amdgcn_sched_barrier(0);
+    }
+    // Rows and columns m0, n0 .. of a matrix of m x n (multiples of 64): a thread takes one column of pieces, 4 rows of them at a time.
+    static constexpr int kPer = B * B / 8 / G::kThreads, kStep = G::kThreads / (B / 8);
+    __device__ __forceinline__ void load(int tid, const uint16_t* p, int ld, int m0, int n0, int m, int n) const {
+        const int row = tid / (B / 8), col = tid % (B / 8) * 8;
+        const bool in = n0 + col < n;
+        const uint16_t* q = p + (int64_t)(m0 + row) * ld + n0 + col;
+#pragma unroll 1
+        for (int i = 0; i < kPer; i += 4) {
+            u32x4 v[4];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                v[j] = 0u;
+                if (i + j < kPer && in && m0 + row + (i + j) * kStep < m) v[j] = *reinterpret_cast<const u32x4*>(q);
+                q += (int64_t)kStep * ld;
+            }
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+                if (i + j < kPer) *piece((i + j) * G::kThreads + tid) = v[j];
+        }
+    }
+    __device__ __forceinline__ void store(int tid, uint16_t* p, int ld, int m0, int n0, int m, int n) const {
+        const int row = tid / (B / 8), col = tid % (B / 8) * 8;
+        if (n0 + col >= n) return;
+        uint16_t* q = p + (int64_t)(m0 + row) * ld + n0 + col;
+#pragma unroll 1
+        for (int i = 0; i < kPer; ++i, q += (int64_t)kStep * ld)
+            if (m0 + row + i * kStep < m) *reinterpret_cast<u32x4*>(q) = *piece(i * G::kThreads + tid);
+    }
+};
+
+// The end of a tile (m0, n0: its first row and column).
+template <int B, int KIND>
+__device__ __forceinline__ void finish(const Task<KIND>& task, int m0, int n0, const Image<B>& image, MmAcc (&acc)[MmTile<B>::FM][MmTile<B>::FN]) {
+    typedef MmTile<B> G;
+    int tid = threadIdx.x;
+    asm volatile("" : "+v"(tid));  // (what follows from it is formed here, not carried through the products in registers that they need)
+    const int lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int r = G::wave_m(w) + (lane & 15), c = G::wave_n(w) + 4 * (lane >> 4);  // the lane's first row and columns
+    const auto each = [&](auto f) __attribute__((always_inline)) {
+#pragma unroll
+        for (int i = 0; i < G::FM; ++i)
+#pragma unroll
+            for (int j = 0; j < G::FN; ++j) f(acc[i][j]);
+    };
+    // (keeps the compiler from holding on to one pass's conversions for the next)
+    const auto renew = [&]() __attribute__((always_inline)) { each([&](f32x4& v) { asm volatile("" : "+v"(v)); }); };
+    const float factor = task.factor(), other = task.other(), after = task.after();
+    const int parts = task.a.parts, m = task.rows(), n = task.cols();
+    each([&](f32x4& v) { v *= factor; });
+    if constexpr (KIND != kGram) {
+        const Held& f = task.from();
+#pragma unroll 1
+        for (int p = 0; p < parts; ++p) {
+            image.load(tid, f.p + p * f.size, f.ld, m0, n0, m, n);
+            __syncthreads();
+            image.quads(r, c, acc, [&](f32x4& v, auto q) { v += __builtin_convertvector((f16x4)*q, f32x4) * other; });
+            __syncthreads();
+        }
+        each([&](f32x4& v) { v *= after; });
+    }
+    if constexpr (KIND == kOut || KIND == kStep) {
+#pragma unroll
+        for (int i = 0; i < G::FM; ++i) {
+            __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+            for (int j = 0; j < G::FN; ++j) task.write(m0 + r + 16 * i, n0 + c + 16 * j, acc[i][j]);
+        }
+    } else {
+        const Held o = task.to();
+#pragma unroll 1
+        for (int p = 0; p < parts; ++p) {
+            uint16_t* const q = o.p + p * o.size;
+            image.quads(r, c, acc, [&](f32x4& v, auto q) { *q = __builtin_convertvector(v, f16x4); });
+            __syncthreads();
+            image.store(tid, q, o.ld, m0, n0, m, n);
+            if (square_kind(KIND) && m0 != n0) {
+                __syncthreads();
+                renew();
+                image.across(r, c, acc);
+                __syncthreads();
+                image.store(tid, q, o.ld, n0, m0, n, m);
+            }
+            if (p + 1 < parts) {
+                __syncthreads();
+                renew();
+                each([&](f32x4& v) { v -= __builtin_convertvector(__builtin_convertvector(v, f16x4), f32x4); });
+            }
+        }
+    }
 }
 
-template <typename T>
-void pack(const OrthoPlan& p, const T* x, int64_t ld, int64_t batch, char* ws, hipStream_t st) {
-    const dim3 grid((uint32_t)(((int64_t)p.rp * p.cp / 8 + 255) / 256), (uint32_t)p.batches);
-    pack_kernel<T><<<grid, 256, 0, st>>>(x, ld, batch, (int)p.rows, (int)p.cols, p.rp, p.cp, p.parts, reinterpret_cast<const Norm*>(ws + p.norm_off),
-                                         reinterpret_cast<uint16_t*>(ws + p.x1_off));
+// First turn of slot g of a launch whose turns are dealt out.
+__device__ __forceinline__ int64_t slot_begin(const OrthoLaunch& a, int64_t g) { return g * a.begin[a.count] / a.slots; }
+__device__ __forceinline__ int item_at(const OrthoLaunch& a, int64_t pos) {
+    int i = 0;
+    while (i + 1 < a.count && pos >= a.begin[i + 1]) ++i;
+    return i;
 }
 
-}  // namespace
+// Turns t0 .. t1 of a tile, and its end or, where that is not all of it, its partial sums.
+template <int B, int KIND, bool TALL>
+__device__ __forceinline__ void segment(const Task<KIND>& task, int tile, int t0, int t1, int64_t place, uint16_t* const (&as)[MmTile<B>::kStages],
+                                        uint16_t* const (&bs)[MmTile<B>::kStages]) {
+    typedef MmTile<B> G;
+    const Mm p = task.product();
+    const MmAt id = mm_at<B>(p, (uint32_t)tile);
+    MmAcc acc[G::FM][G::FN] = {};
+    constexpr bool kRows = KIND == kPoly || (KIND == kGram ? !TALL : true), kCols = KIND == kPoly || (KIND == kGram ? !TALL : TALL);  // k along the rows
+    MmCore<f16, B, kRows, kCols, false>::run(p, id.m * B, id.n * B, t0, t1, as, bs, acc);
+    if (t1 - t0 < p.turns * p.segs) {
+        const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
+        f32x4* const part = reinterpret_cast<f32x4*>(task.a.part) + (place * G::kWaves + w) * (G::FM * G::FN * 64) + lane;
+#pragma unroll
+        for (int r = 0; r < G::FM; ++r)
+#pragma unroll
+            for (int j = 0; j < G::FN; ++j) part[(r * G::FN + j) * 64] = acc[r][j];
+    } else {
+        __syncthreads();  // every wavefront has read its last turn
+        finish<B, KIND>(task, id.m * B, id.n * B, Image<B>(as, bs), acc);
+    }
+}
+template <int B, int KIND>
+__device__ __forceinline__ void segment(const Task<KIND>& task, int tile, int t0, int t1, int64_t place, uint16_t* const (&as)[MmTile<B>::kStages],
+                                        uint16_t* const (&bs)[MmTile<B>::kStages]) {
+    if (KIND != kPoly && task.tall)
+        segment<B, KIND, true>(task, tile, t0, t1, place, as, bs);
+    else
+        segment<B, KIND, false>(task, tile, t0, t1, place, as, bs);
+}
 
-MmCut mm_cut(int64_t m, int64_t n, int64_t turns, int64_t batches, bool sym) {
-    static constexpr struct {
-        int tile, fit;
-        double ends, alone, each;
-    } kinds[] = {{64, 4, 2, 0.45, 0.16}, {128, 2, 2, 0.8, 0.55}, {256, 1, 3, 2.0, 2.0}};
-    static constexpr int counts[] = {1, 2, 3, 4, 6, 8, 12, 16, 24, 32};
-    MmCut best = {64, 1};
-    double least = 0;
-    for (const auto& k : kinds) {
-        const int64_t s = (m + k.tile - 1) / k.tile, tiles = (sym ? s * (s + 1) / 2 : s * ((n + k.tile - 1) / k.tile)) * batches;
-        for (const int c : counts) {
-            if (c > 1 && (4 * c > turns || tiles * c > 1024)) break;
-            const double load = (double)(tiles * c) / 256, whole = std::ceil(load), turn = k.fit == 1 ? k.each * whole : load > k.fit ? k.each * load : std::max(k.alone, k.each * whole),
-                         t = ((double)((turns + c - 1) / c) + k.ends) * turn + (c > 1 ? 3 + 8e-7 * (double)(c * tiles) * k.tile * k.tile : 0);
-            if (least == 0 || t < least) least = t, best = {k.tile, c};
+template <int B, int KIND>
+__global__ __launch_bounds__(MmTile<B>::kThreads, 2) void ortho_kernel(OrthoLaunch a) {
+    MM_PLACES(B, as, bs);
+    // An XCD takes a contiguous eighth of each item's tiles, the items one after the other (longest first): contiguous eighths of all the tiles would leave the long ones
+    // to some of the XCDs. Items with few tiles begin at different XCDs.
+    uint32_t k = blockIdx.x >> 3, tile = 0;
+    int i = 0;
+    for (; i < a.count; ++i) {
+        const uint32_t n = (uint32_t)(a.begin[i + 1] - a.begin[i]), x = (blockIdx.x + (uint32_t)i) & 7u, per = n >> 3, rest = n & 7u, mine = per + (x < rest ? 1u : 0u);
+        tile = x * per + min(x, rest) + k;
+        if (k < mine) break;
+        k -= mine;
+    }
+    if (i == a.count) return;
+    segment<B, KIND>(Task<KIND>(a, i), (int32_t)tile, 0, item_turns(a.it[i], KIND, a.parts), 0, as, bs);
+}
+
+// The turns dealt out to slots. (Kernels of their own: the loop over a slot's tiles takes registers that 256-wide tiles do not have.)
+template <int B, int KIND>
+__global__ __launch_bounds__(MmTile<B>::kThreads, 2) void ortho_slots_kernel(OrthoLaunch a) {
+    MM_PLACES(B, as, bs);
+    const int64_t g = xcd_block(blockIdx.x, gridDim.x), stop = slot_begin(a, g + 1);
+    int64_t at = slot_begin(a, g), place = 2 * g;
+    while (at < stop) {
+        const int i = item_at(a, at);
+        const Task<KIND> task(a, i);
+        const int32_t turns = item_turns(a.it[i], KIND, a.parts);
+        const int64_t local = at - a.begin[i];
+        const int32_t tile = __builtin_amdgcn_readfirstlane((int32_t)(local / turns)), t0 = __builtin_amdgcn_readfirstlane((int32_t)(local - (int64_t)tile * turns)), t1 = (int32_t)min((int64_t)turns, t0 + (stop - at));
+        segment<B, KIND>(task, tile, t0, t1, place, as, bs);
+        at += t1 - t0;
+        place = 2 * g + 1;
+        __syncthreads();  // every wavefront has read its last turn, or the tile's last image
+    }
+}
+
+// The tiles that slots share, each joined by the workgroups of the first slot that begins inside it.
+template <int B, int KIND>
+__global__ __launch_bounds__(256) void ortho_join_kernel(OrthoLaunch a) {
+    typedef MmTile<B> G;
+    constexpr uint32_t kBlocks = B * B / 1024;
+    const int64_t g = blockIdx.x / kBlocks + 1, pos = slot_begin(a, g);
+    const int i = item_at(a, pos);
+    const Task<KIND> task(a, i);
+    const Mm p = task.product();
+    const int32_t turns = p.turns * p.segs, tile = (int32_t)((pos - a.begin[i]) / turns);
+    const int64_t s = a.begin[i] + (int64_t)tile * turns, e = s + turns, before = slot_begin(a, g - 1);
+    if (pos == s || before > s) return;
+    const uint32_t at = blockIdx.x % kBlocks * 256 + threadIdx.x, lane = at & 63, slot = at >> 6;
+    const f32x4* const part = reinterpret_cast<const f32x4*>(a.part) + at;
+    constexpr int64_t kTile = B * B / 4;
+    const int64_t last = (e * a.slots - 1) / a.begin[a.count];  // the last slot that begins before e
+    f32x4 v = part[(2 * (g - 1) + (before < s ? 1 : 0)) * kTile];
+    for (int64_t h = g; h <= last; h += 8) {
+        f32x4 q[8];
+#pragma unroll
+        for (int r = 0; r < 8; ++r)
+            if (h + r <= last) q[r] = part[2 * (h + r) * kTile];
+#pragma unroll
+        for (int r = 0; r < 8; ++r)
+            if (h + r <= last) v += q[r];
+    }
+    const MmAt id = mm_at<B>(p, (uint32_t)tile);
+    const uint32_t w = slot / (G::FM * G::FN), q = slot % (G::FM * G::FN);
+    task.end(id.m * B + G::wave_m((int)w) + (int)(lane & 15) + 16 * (int)(q / G::FN), id.n * B + G::wave_n((int)w) + 4 * (int)(lane >> 4) + 16 * (int)(q % G::FN), v,
+             p.sym && id.m != id.n);
+}
+
+template <int B, int KIND>
+hipError_t launch(const OrthoLaunch& a, hipStream_t st) {
+    if constexpr (B < 256) {
+        if (a.slots) {
+            ortho_slots_kernel<B, KIND><<<(uint32_t)a.slots, MmTile<B>::kThreads, 0, st>>>(a);
+            ortho_join_kernel<B, KIND><<<(uint32_t)((a.slots - 1) * (B * B / 1024)), 256, 0, st>>>(a);
+            return hipGetLastError();
+        }
+    }
+    uint32_t most = 0;  // of an XCD
+    for (int i = 0; i < a.count; ++i) most += (uint32_t)((a.begin[i + 1] - a.begin[i] + 7) / 8);
+    ortho_kernel<B, KIND><<<8 * most, MmTile<B>::kThreads, 0, st>>>(a);
+    return hipGetLastError();
+}
+
+// How a group's product is cut: the tile and, where that is faster by the measured times, the slots that its turns are dealt out to. Slots that work at different places of k
+// share little of what they load: whole tiles run in step and find their neighbours' loads in the L2 (FIGURES). What dealing out is for is few tiles and a long sum.
+struct Cut {
+    int32_t tile;
+    int64_t slots;
+};
+Cut group_cut(const OrthoLaunch& a, int kind) {
+    Cut best = {64, 0};
+    double least = -1, bytes = 0;  // bytes: of the operands
+    for (int i = 0; i < a.count; ++i) {
+        const double x = (double)a.it[i].rp * a.it[i].cp, d = (double)std::min(a.it[i].rp, a.it[i].cp);
+        bytes += 2.0 * a.parts * (kind == kGram ? x : kind == kPoly ? d * d : x + d * d);
+    }
+    const double rate = bytes < 8e6 ? 17e6 : bytes < 100e6 ? 7e6 : 4.4e6;  // bytes a us, from the L2s, the last-level cache and memory
+    for (const int tile : {64, 128, 256}) {
+        int64_t tiles = 0, turns = 0;
+        int32_t most = 0, same = 1;
+        for (int i = 0; i < a.count; ++i) {
+            const int64_t n = item_tiles(a.it[i], kind, tile);
+            const int32_t t = item_turns(a.it[i], kind, a.parts);
+            if (i > 0 && t != most) same = 0;
+            tiles += n;
+            turns += n * t;
+            most = std::max(most, t);
+        }
+        const double mean = (double)turns / (double)tiles;
+        // tiles of different lengths: the longest begin first, and one that begins alone ends last
+        const double lone = 2 + (tile == 256 ? 10.5 + 1.29 * most : tile == 128 ? 4 + 0.6 * most : 1 + 0.36 * most);
+        const double whole = same ? mm_time(tile, tiles, most) : std::max(lone, mm_time(tile, tiles, (int64_t)std::ceil(mean)));
+        if (least < 0 || whole < least) least = whole, best = {tile, 0};
+        for (const int64_t slots : {16, 32, 64, 128, 256, 512}) {
+            if (tile == 256 || turns < 4 * slots) break;
+            const bool two = slots > 256;
+            const double turn = std::max(tile == 128 ? (two ? 1.05 : 0.6) : (two ? 0.42 : 0.36), (double)(slots * tile * 256) / rate),
+                         end = tile == 128 ? (two ? 6 : 4) : (two ? 2 : 1), w = (double)turns / (double)slots,
+                         pieces = std::min((double)(2 * slots), (double)(slots + tiles)), t = 2 + w * turn + (w / mean + 1) * end + 5 + pieces * tile * tile * 4 / 4e6;
+            if (t < least) least = t, best = {tile, slots};
         }
     }
     return best;
 }
 
-size_t mm_part_bytes(const MmCut& c, int64_t m, int64_t n, int64_t batches, bool sym) {
-    if (c.splits == 1) return 0;
-    const int64_t s = (m + c.tile - 1) / c.tile, tiles = sym ? s * (s + 1) / 2 : s * ((n + c.tile - 1) / c.tile);
-    return (size_t)(tiles * batches * c.splits) * c.tile * c.tile * 4;
+template <int KIND>
+hipError_t product(OrthoLaunch& a, hipStream_t st) {
+    const Cut c = group_cut(a, KIND);
+    a.slots = c.slots;
+    a.begin[0] = 0;
+    for (int i = 0; i < a.count; ++i)
+        a.begin[i + 1] = a.begin[i] + item_tiles(a.it[i], KIND, c.tile) * (c.slots ? item_turns(a.it[i], KIND, a.parts) : 1);
+    return c.tile == 256 ? launch<256, KIND>(a, st) : c.tile == 128 ? launch<128, KIND>(a, st) : launch<64, KIND>(a, st);
 }
 
-OrthoPlan ortho_plan(int64_t rows, int64_t cols, int32_t parts, int32_t batches, bool update) {
-    OrthoPlan p = {};
-    p.rows = rows;
-    p.cols = cols;
-    p.parts = parts;
-    p.batches = batches;
-    p.tall = rows > cols;
-    p.rp = (int32_t)((rows + 63) / 64 * 64);
-    p.cp = (int32_t)((cols + 63) / 64 * 64);
-    p.dp = std::min(p.rp, p.cp);
-    const int segs = parts == 1 ? 1 : 3;
-    const int64_t kd = (int64_t)p.dp / kMmTurn * segs, kx = (int64_t)(p.tall ? p.rp : p.cp) / kMmTurn * segs;
-    p.g1 = mm_cut(p.dp, p.dp, kx, batches, true);
-    p.g2 = mm_cut(p.dp, p.dp, kd, batches, true);
-    p.g3 = mm_cut(p.rp, p.cp, kd, batches, false);
-    p.sums = (int32_t)(update ? (rows * cols + kMomentum - 1) / kMomentum : std::min<int64_t>(1024, (rows * cols + 4095) / 4096));
-    const auto up = [](size_t x) { return (x + 255) & ~size_t(255); };
-    const size_t xs = (size_t)p.rp * p.cp, ds = (size_t)p.dp * p.dp;
-    size_t off = 0;
-    const auto take = [&](size_t bytes) {
-        const size_t at = off;
-        off += up(bytes);
-        return at;
-    };
-    p.norm_off = take((size_t)batches * sizeof(Norm));
-    p.sum_off = take((size_t)batches * p.sums * 8);
-    p.x0_off = take(batches * xs * std::max(update ? 4 : 2, 2 * parts));
-    p.x1_off = take(batches * xs * 2 * parts);
-    p.a_off = take(batches * ds * 2 * parts);
-    p.b_off = take(batches * ds * 2 * parts);
-    p.part_off = take(std::max({mm_part_bytes(p.g1, p.dp, p.dp, batches, true), mm_part_bytes(p.g2, p.dp, p.dp, batches, true),
-                                mm_part_bytes(p.g3, p.rp, p.cp, batches, false)}));
-    p.bytes = off;
-    return p;
+// The steps of a group whose X0 lies in place 1; the last one's outputs go where LAST says.
+template <int LAST>
+hipError_t iterate(OrthoLaunch& a, const OrthoCoefs& k, hipStream_t st) {
+    a.parts = k.parts;
+    a.ca = k.a;
+    a.cb = k.b;
+    a.cc = k.c;
+    for (int i = 0; i < k.steps; ++i) {
+        a.from = (i & 1) ^ 1;
+        a.first = i == 0;
+        hipError_t e = product<kGram>(a, st);
+        if (e == hipSuccess) e = product<kPoly>(a, st);
+        if (e == hipSuccess) e = i + 1 < k.steps ? product<kNext>(a, st) : product<LAST>(a, st);
+        if (e != hipSuccess) return e;
+    }
+    return hipSuccess;
 }
 
-hipError_t launch_orthogonalize(const OrthoPlan& p, const OrthoCoefs& k, int dtype, const void* x, int64_t ldx, int out_dtype, void* out, int64_t ldout,
+size_t up(size_t x) { return (x + 255) & ~size_t(255); }
+int32_t padded(int64_t n) { return (int32_t)((n + 63) / 64 * 64); }
+
+size_t first_bytes(const OrthoItem& t, int32_t parts, bool update) { return up((size_t)t.rp * t.cp * std::max(update ? 4 : 2, 2 * parts)); }
+
+// Places of an item in the workspace from `at` on; returns the first byte behind.
+char* place(OrthoItem& t, int64_t rows, int64_t cols, int32_t parts, bool update, char* at) {
+    t.rows = (int32_t)rows;
+    t.cols = (int32_t)cols;
+    t.rp = padded(rows);
+    t.cp = padded(cols);
+    t.x[0] = reinterpret_cast<uint16_t*>(at);
+    at += first_bytes(t, parts, update);
+    t.x[1] = reinterpret_cast<uint16_t*>(at);
+    at += up((size_t)t.rp * t.cp * 2 * parts);
+    t.a = reinterpret_cast<uint16_t*>(at);
+    const size_t d = (size_t)std::min(t.rp, t.cp);
+    return at + up(d * d * 2 * parts * 2);
+}
+
+}  // namespace
+
+size_t ortho_item_bytes(int64_t rows, int64_t cols, int32_t parts, bool update) {
+    OrthoItem t = {};
+    return (size_t)(place(t, rows, cols, parts, update, nullptr) - static_cast<char*>(nullptr));
+}
+
+int64_t ortho_sums(int64_t rows, int64_t cols) { return (rows * cols + kSquareUnit - 1) / kSquareUnit; }
+
+int64_t ortho_turns(int64_t rows, int64_t cols, int32_t parts) {
+    const int64_t r = padded(rows) / 64, c = padded(cols) / 64, d = std::min(r, c);
+    return std::max(d * (d + 1) / 2 * std::max(r, c), r * c * d) * (parts > 1 ? 3 : 1);
+}
+
+// A slot has at least 4 turns and leaves at most two tiles of sums; 512 slots of 128 x 128 outputs leave the most.
+size_t ortho_part_bytes(int64_t turns) { return (size_t)std::min<int64_t>(512, turns / 4) * 2 * 128 * 128 * 4; }
+
+size_t ortho_part_bytes(int64_t rows, int64_t cols, int32_t parts) {
+    OrthoLaunch a;
+    std::memset(&a, 0, sizeof(a));
+    a.count = 1;
+    a.parts = parts;
+    place(a.it[0], rows, cols, parts, false, nullptr);
+    size_t most = 0;
+    for (const int kind : {kGram, kPoly, kNext}) {
+        const Cut c = group_cut(a, kind);
+        most = std::max(most, (size_t)c.slots * 2 * c.tile * c.tile * 4);
+    }
+    return most;
+}
+
+size_t ortho_head_bytes(int64_t sums) { return up(kOrthoGroup * sizeof(Norm)) + up((size_t)sums * 8); }
+
+hipError_t launch_orthogonalize(int64_t rows, int64_t cols, const OrthoCoefs& k, int dtype, const void* x, int64_t ldx, int out_dtype, void* out, int64_t ldout,
                                 void* ws, hipStream_t st) {
     char* const w = static_cast<char*>(ws);
-    double* const sums = reinterpret_cast<double*>(w + p.sum_off);
-    if (dtype == AL_DTYPE_BF16)
-        square_kernel<bf16><<<p.sums, 256, 0, st>>>(static_cast<const bf16*>(x), ldx, p.rows, (int)p.cols, sums);
-    else
-        square_kernel<float><<<p.sums, 256, 0, st>>>(static_cast<const float*>(x), ldx, p.rows, (int)p.cols, sums);
-    norm_kernel<<<1, 64, 0, st>>>(sums, p.sums, k.eps, reinterpret_cast<Norm*>(w + p.norm_off));
-    if (dtype == AL_DTYPE_BF16)
-        pack(p, static_cast<const bf16*>(x), ldx, 0, w, st);
-    else
-        pack(p, static_cast<const float*>(x), ldx, 0, w, st);
-    EndOut last;
-    last.out = out;
-    last.ld = ldout;
-    last.out_bf16 = out_dtype == AL_DTYPE_BF16;
-    return iterate(p, k, last, w, st);
+    const int64_t units = ortho_sums(rows, cols);
+    Norm* const norms = reinterpret_cast<Norm*>(w);
+    double* const sums = reinterpret_cast<double*>(w + up(kOrthoGroup * sizeof(Norm)));
+    char* at = w + ortho_head_bytes(units);
+    OrthoLaunch a;
+    std::memset(&a, 0, sizeof(a));
+    a.count = 1;
+    a.norms = norms;
+    a.part = reinterpret_cast<float*>(at);
+    place(a.it[0], rows, cols, k.parts, false, at + ortho_part_bytes(rows, cols, k.parts));
+    a.out = out;
+    a.ldout = ldout;
+    a.out_bf16 = out_dtype == AL_DTYPE_BF16;
+    const uint32_t slabs = (uint32_t)std::min<int64_t>(units, 1024);
+    PackList l;
+    std::memset(&l, 0, sizeof(l));
+    l.count = 1;
+    l.t[0] = {x, ldx, a.it[0].x[1], a.it[0].rows, a.it[0].cols, a.it[0].rp, a.it[0].cp};
+    l.begin[1] = (uint32_t)((int64_t)a.it[0].rp * a.it[0].cp / 2048);
+    l.sums[1] = slabs;
+    if (dtype == AL_DTYPE_BF16) {
+        square_kernel<bf16><<<slabs, 256, 0, st>>>(static_cast<const bf16*>(x), ldx, rows, (int)cols, sums);
+        pack_kernel<bf16><<<l.begin[1], 256, 0, st>>>(l, k.parts, k.eps, sums, norms);
+    } else {
+        square_kernel<float><<<slabs, 256, 0, st>>>(static_cast<const float*>(x), ldx, rows, (int)cols, sums);
+        pack_kernel<float><<<l.begin[1], 256, 0, st>>>(l, k.parts, k.eps, sums, norms);
+    }
+    return iterate<kOut>(a, k, st);
 }
 
-hipError_t launch_muon(const OrthoPlan& p, const OrthoCoefs& k, const MuonArgs& a, const MuonList& l, void* ws, hipStream_t st) {
+hipError_t launch_muon(const MuonItem* items, int count, const OrthoCoefs& k, const MuonArgs& m, void* ws, hipStream_t st) {
     char* const w = static_cast<char*>(ws);
-    double* const sums = reinterpret_cast<double*>(w + p.sum_off);
-    float* const u = reinterpret_cast<float*>(w + p.x0_off);
-    const int64_t n = p.rows * p.cols, pitch = (int64_t)p.rp * p.cp;
-    const hipError_t e = launch_momentum(a, l, n, pitch, p.sums, p.batches, u, sums, st);
+    int64_t units = 0, turns = 0;
+    for (int i = 0; i < count; ++i) units += ortho_sums(items[i].rows, items[i].cols), turns += ortho_turns(items[i].rows, items[i].cols, k.parts);
+    Norm* const norms = reinterpret_cast<Norm*>(w);
+    double* const sums = reinterpret_cast<double*>(w + up(kOrthoGroup * sizeof(Norm)));
+    char* at = w + ortho_head_bytes(units);
+    OrthoLaunch a;
+    MomentumList l;
+    PackList q;
+    std::memset(&a, 0, sizeof(a));
+    std::memset(&l, 0, sizeof(l));
+    std::memset(&q, 0, sizeof(q));
+    a.count = l.count = q.count = count;
+    a.norms = norms;
+    a.part = reinterpret_cast<float*>(at);
+    a.decay = m.decay;
+    at += ortho_part_bytes(turns);
+    for (int i = 0; i < count; ++i) {
+        const MuonItem& s = items[i];
+        OrthoItem& t = a.it[i];
+        at = place(t, s.rows, s.cols, k.parts, true, at);
+        t.p = s.p;
+        t.step = s.step;
+        float* const u = reinterpret_cast<float*>(t.x[0]);
+        l.t[i] = {s.g, s.m, s.meta, u, s.rows * s.cols};
+        l.begin[i + 1] = l.begin[i] + (uint32_t)ortho_sums(s.rows, s.cols);
+        q.t[i] = {u, s.cols, t.x[1], t.rows, t.cols, t.rp, t.cp};
+        q.begin[i + 1] = q.begin[i] + (uint32_t)((int64_t)t.rp * t.cp / 2048);
+        q.sums[i + 1] = l.begin[i + 1];
+    }
+    const hipError_t e = launch_momentum(m, l, sums, st);
     if (e != hipSuccess) return e;
-    norm_kernel<<<p.batches, 64, 0, st>>>(sums, p.sums, k.eps, reinterpret_cast<Norm*>(w + p.norm_off));
-    pack(p, static_cast<const float*>(u), p.cols, pitch, w, st);
-    EndStep last;
-    for (int i = 0; i < kMuonBatch; ++i) last.p[i] = l.t[i].p;
-    last.decay = a.decay;
-    last.step = a.step;
-    return iterate(p, k, last, w, st);
+    pack_kernel<float><<<q.begin[count], 256, 0, st>>>(q, k.parts, k.eps, sums, norms);
+    return iterate<kStep>(a, k, st);
 }
 
 }  // namespace al

@@ -56,15 +56,9 @@ al_status check_sides(int64_t rows, int64_t cols, const char* who) {
     return AL_OK;
 }
 
-al::OrthoCoefs coefs(const al_ortho_cfg& k) { return {(float)k.a, (float)k.b, (float)k.c, k.eps, k.steps}; }
+al::OrthoCoefs coefs(const al_ortho_cfg& k) { return {(float)k.a, (float)k.b, (float)k.c, k.eps, k.steps, k.parts}; }
 
 bool aligned16(const void* p) { return (at(p) & 15u) == 0; }
-
-// Matrices of a shape that are stepped together.
-int64_t batch_of(int64_t rows, int64_t cols) {
-    const int64_t n = (rows + 63) / 64 * 64 * ((cols + 63) / 64 * 64);
-    return std::max<int64_t>(1, std::min<int64_t>(al::kMuonBatch, (int64_t(1) << 26) / n));
-}
 
 al_status check_muon(const al_tensor* ts, int32_t nt, const al_muon_cfg* cfg, const char* who) {
     if (!cfg) return fail(AL_EINVAL, "%s: cfg is NULL", who);
@@ -92,33 +86,43 @@ al_status check_muon(const al_tensor* ts, int32_t nt, const al_muon_cfg* cfg, co
     return AL_OK;
 }
 
-// The non-empty tensors by shape, in list order within each.
-std::vector<int> by_shape(const al_tensor* ts, int32_t nt) {
+// The non-empty tensors, longest products first: neighbours share launches.
+std::vector<int> by_size(const al_tensor* ts, int32_t nt) {
     std::vector<int> order;
     for (int i = 0; i < nt; ++i)
         if (ts[i].rows > 0 && ts[i].cols > 0) order.push_back(i);
-    std::stable_sort(order.begin(), order.end(), [&](int x, int y) {
-        return ts[x].rows != ts[y].rows ? ts[x].rows < ts[y].rows : ts[x].cols < ts[y].cols;
-    });
+    std::stable_sort(order.begin(), order.end(), [&](int x, int y) { return std::max(ts[x].rows, ts[x].cols) > std::max(ts[y].rows, ts[y].cols); });
     return order;
 }
 
-size_t shape_end(const al_tensor* ts, const std::vector<int>& order, size_t i) {
-    size_t j = i;
-    while (j < order.size() && ts[order[j]].rows == ts[order[i]].rows && ts[order[j]].cols == ts[order[i]].cols) ++j;
+// One past the last tensor of the group that begins with order[i].
+size_t group_end(const al_tensor* ts, const std::vector<int>& order, size_t i, int32_t parts) {
+    size_t bytes = 0, j = i;
+    for (; j < order.size() && j < i + al::kOrthoGroup; ++j) {
+        bytes += al::ortho_item_bytes(ts[order[j]].rows, ts[order[j]].cols, parts, true);
+        if (j > i && bytes > al::kOrthoBytes) break;
+    }
     return j;
 }
 
-size_t muon_bytes(const al_tensor* ts, const std::vector<int>& order, int32_t parts) {
-    size_t most = 0;
-    for (size_t i = 0, j; i < order.size(); i = j) {
-        j = shape_end(ts, order, i);
-        const al_tensor& t = ts[order[i]];
-        // every smaller batch too: it may be cut into more splits
-        for (int64_t b = std::min<int64_t>(batch_of(t.rows, t.cols), (int64_t)(j - i)); b > 0; --b)
-            most = std::max(most, al::ortho_plan(t.rows, t.cols, parts, (int32_t)b, true).bytes);
+// What any group of these tensors, or of some of them, takes: each term grows with the list.
+size_t muon_bytes(const al_tensor* ts, int32_t nt, int32_t parts) {
+    size_t all = 0, most = 0;
+    int64_t sums = 0, turns = 0;
+    for (int i = 0; i < nt; ++i) {
+        if (ts[i].rows == 0 || ts[i].cols == 0) continue;
+        const size_t b = al::ortho_item_bytes(ts[i].rows, ts[i].cols, parts, true);
+        all += b;
+        most = std::max(most, b);
+        sums += al::ortho_sums(ts[i].rows, ts[i].cols);
+        turns += al::ortho_turns(ts[i].rows, ts[i].cols, parts);
     }
-    return most;
+    if (all == 0) return 0;
+    return al::ortho_head_bytes(sums) + al::ortho_part_bytes(turns) + std::min(all, std::max(most, al::kOrthoBytes));
+}
+
+size_t ortho_bytes(int64_t rows, int64_t cols, int32_t parts) {
+    return al::ortho_head_bytes(al::ortho_sums(rows, cols)) + al::ortho_part_bytes(rows, cols, parts) + al::ortho_item_bytes(rows, cols, parts, false);
 }
 
 }  // namespace
@@ -133,7 +137,7 @@ al_status al_orthogonalize_workspace_bytes(int64_t rows, int64_t cols, const al_
     if (!cfg) return fail(AL_EINVAL, "%s: cfg is NULL", who);
     AL_TRY(check_ortho(*cfg, who));
     AL_TRY(check_sides(rows, cols, who));
-    if (rows > 0 && cols > 0) *bytes = al::ortho_plan(rows, cols, cfg->parts, 1, false).bytes;
+    if (rows > 0 && cols > 0) *bytes = ortho_bytes(rows, cols, cfg->parts);
     return AL_OK;
 }
 
@@ -150,9 +154,8 @@ al_status al_orthogonalize(int32_t dtype, const void* x, int64_t ldx, int64_t ro
     AL_TRY(check_mat(x, &ldx, rows, cols, dtype, true, who, "x"));
     AL_TRY(check_mat(out, &ldout, rows, cols, out_dtype, true, who, "out"));
     if (x == out && (dtype != out_dtype || ldx != ldout)) return fail(AL_EINVAL, "%s: out may be x with the same type and row pitch only", who);
-    const al::OrthoPlan p = al::ortho_plan(rows, cols, cfg->parts, 1, false);
-    AL_TRY(check_ws(ws, ws_bytes, p.bytes, who));
-    return launched(al::launch_orthogonalize(p, coefs(*cfg), dtype, x, ldx, out_dtype, out, ldout, ws, as_stream(stream)), who);
+    AL_TRY(check_ws(ws, ws_bytes, ortho_bytes(rows, cols, cfg->parts), who));
+    return launched(al::launch_orthogonalize(rows, cols, coefs(*cfg), dtype, x, ldx, out_dtype, out, ldout, ws, as_stream(stream)), who);
 }
 
 al_status al_muon_workspace_bytes(const al_tensor* tensors, int32_t nt, const al_muon_cfg* cfg, size_t* bytes) {
@@ -161,11 +164,7 @@ al_status al_muon_workspace_bytes(const al_tensor* tensors, int32_t nt, const al
     if (!bytes) return fail(AL_EINVAL, "%s: bytes is NULL", who);
     *bytes = 0;
     AL_TRY(check_muon(tensors, nt, cfg, who));
-    try {
-        *bytes = muon_bytes(tensors, by_shape(tensors, nt), cfg->ortho.parts);
-    } catch (const std::bad_alloc&) {
-        return fail(AL_EINVAL, "%s: no host memory for a list of %d tensors", who, nt);
-    }
+    *bytes = muon_bytes(tensors, nt, cfg->ortho.parts);
     return AL_OK;
 }
 
@@ -174,34 +173,30 @@ al_status al_muon_step(const al_tensor* tensors, int32_t nt, const al_muon_cfg* 
     al::api_clear();
     AL_TRY(check_muon(tensors, nt, cfg, who));
     if (step < 1) return fail(AL_EINVAL, "%s: step must be >= 1", who);
+    AL_TRY(check_ws(ws, ws_bytes, muon_bytes(tensors, nt, cfg->ortho.parts), who));
     std::vector<int> order;
-    size_t need = 0;
     try {
-        order = by_shape(tensors, nt);
-        need = muon_bytes(tensors, order, cfg->ortho.parts);
+        order = by_size(tensors, nt);
     } catch (const std::bad_alloc&) {
         return fail(AL_EINVAL, "%s: no host memory for a list of %d tensors", who, nt);
     }
-    AL_TRY(check_ws(ws, ws_bytes, need, who));
+    al::MuonArgs a = {};
+    a.beta = cfg->beta;
+    a.omb = 1.0 - cfg->beta;
+    a.decay = 1.0 - cfg->lr * cfg->weight_decay;
+    a.nesterov = cfg->nesterov;
+    a.grad_bf16 = cfg->grad_dtype == AL_DTYPE_BF16;
+    a.uf8 = cfg->m.codec == AL_CODEC_UF8;
     for (size_t i = 0; i < order.size();) {
-        const al_tensor& t = tensors[order[i]];
-        const size_t end = std::min(shape_end(tensors, order, i), i + (size_t)batch_of(t.rows, t.cols));
-        const al::OrthoPlan p = al::ortho_plan(t.rows, t.cols, cfg->ortho.parts, (int32_t)(end - i), true);
-        al::MuonList l = {};
+        const size_t end = group_end(tensors, order, i, cfg->ortho.parts);
+        al::MuonItem items[al::kOrthoGroup];
         for (size_t j = i; j < end; ++j) {
-            const al_tensor& s = tensors[order[j]];
-            l.t[j - i] = {s.param, s.grad, s.m, s.m_meta};
+            const al_tensor& t = tensors[order[j]];
+            const double r = (double)t.rows, c = (double)t.cols;
+            const double s = cfg->scale == AL_MUON_SCALE_NONE ? 1.0 : cfg->scale == AL_MUON_SCALE_SPECTRAL ? std::sqrt(std::max(1.0, r / c)) : 0.2 * std::sqrt(std::max(r, c));
+            items[j - i] = {t.param, t.grad, t.m, t.m_meta, t.rows, t.cols, cfg->lr * s};
         }
-        al::MuonArgs a = {};
-        a.beta = cfg->beta;
-        a.omb = 1.0 - cfg->beta;
-        a.decay = 1.0 - cfg->lr * cfg->weight_decay;
-        const double r = (double)t.rows, c = (double)t.cols;
-        a.step = cfg->lr * (cfg->scale == AL_MUON_SCALE_NONE ? 1.0 : cfg->scale == AL_MUON_SCALE_SPECTRAL ? std::sqrt(std::max(1.0, r / c)) : 0.2 * std::sqrt(std::max(r, c)));
-        a.nesterov = cfg->nesterov;
-        a.grad_bf16 = cfg->grad_dtype == AL_DTYPE_BF16;
-        a.uf8 = cfg->m.codec == AL_CODEC_UF8;
-        AL_TRY(launched(al::launch_muon(p, coefs(cfg->ortho), a, l, ws, as_stream(stream)), who));
+        AL_TRY(launched(al::launch_muon(items, (int)(end - i), coefs(cfg->ortho), a, ws, as_stream(stream)), who));
         i = end;
     }
     return AL_OK;

@@ -7,7 +7,7 @@
 
 #include "../../include/al.h"
 #include "act_internal.hpp"
-#include "ortho_internal.hpp"
+#include "mm_cut.hpp"
 
 namespace al {
 

@@ -133,7 +133,7 @@ struct EndGrad {
     Ids target;
     int64_t v0;
     int32_t tokens, columns;
-    __device__ __forceinline__ void operator()(int, int m, int n, f32x4 v, bool) const {
+    __device__ __forceinline__ void operator()(int m, int n, f32x4 v) const {
         if (m >= tokens_padded || n >= ld) return;
         const float c = coef[m], l = lse[m];
         const int64_t y = m < tokens ? target_at(target, m) - v0 - n : -1;
@@ -199,7 +199,7 @@ struct EndSum {
     const float* sum;
     int64_t ld, sum_ld;
     int32_t rows, cols, out_bf16;
-    __device__ __forceinline__ void operator()(int, int m, int n, f32x4 v, bool) const {
+    __device__ __forceinline__ void operator()(int m, int n, f32x4 v) const {
         if (m >= rows || n >= cols) return;
         const int in = min(4, cols - n);
         const int64_t i = m * ld + n;
@@ -243,7 +243,7 @@ XentPlan xent_plan(int64_t tokens, int64_t hidden, int64_t vocab, int64_t ldw, i
     p.dw_parts = dw ? (grad_dtype == AL_DTYPE_F32 ? 2 : 1) : 0;
     p.parts = std::max(p.dh_parts, p.dw_parts);
     const int64_t turns = p.dp / kMmTurn;
-    p.logits = mm_cut(p.block, vocab, turns, 1, false);
+    p.logits = mm_cut(p.block, vocab, turns);
     p.logits.splits = 1;
     const auto up = [](size_t x) { return (x + 255) & ~size_t(255); };
     size_t off = 0;
@@ -259,15 +259,15 @@ XentPlan xent_plan(int64_t tokens, int64_t hidden, int64_t vocab, int64_t ldw, i
     if (p.parts) {
         const int64_t room = (int64_t(1) << 26) / p.tp / 256 * 256;
         p.piece = (int32_t)std::min<int64_t>((vocab + 63) / 64 * 64, std::max<int64_t>(256, room));
-        p.back = mm_cut(p.tp, p.piece, turns, 1, false);
+        p.back = mm_cut(p.tp, p.piece, turns);
         p.back.splits = 1;
-        p.dh = mm_cut(p.tp, hidden, p.piece / kMmTurn * p.dh_parts, 1, false);
-        p.dw = mm_cut(p.piece, hidden, p.tp / kMmTurn * p.dw_parts, 1, false);
+        p.dh = mm_cut(p.tp, hidden, p.piece / kMmTurn * p.dh_parts);
+        p.dw = mm_cut(p.piece, hidden, p.tp / kMmTurn * p.dw_parts);
         p.lse_off = take((size_t)p.tp * 4);
         p.coef_off = take((size_t)p.tp * 4);
         p.d_off = take((size_t)p.tp * p.piece * 2 * p.parts);
         p.dh_off = take(dh && p.piece < vocab ? (size_t)p.tp * hidden * 4 : 0);
-        p.part_off = take(std::max(dh ? mm_part_bytes(p.dh, p.tp, hidden, 1, false) : 0, dw ? mm_part_bytes(p.dw, p.piece, hidden, 1, false) : 0));
+        p.part_off = take(std::max(dh ? mm_part_bytes(p.dh, p.tp, hidden) : 0, dw ? mm_part_bytes(p.dw, p.piece, hidden) : 0));
     }
     p.bytes = off;
     return p;
@@ -277,19 +277,19 @@ hipError_t launch_xent(const XentPlan& p, const Xent& a, void* ws, hipStream_t s
     char* const base = static_cast<char*>(ws);
     uint16_t* const h = reinterpret_cast<uint16_t*>(base + p.h_off);
     pad(a.h, p.tokens, (int32_t)p.hidden, p.tp, p.dp, a.target, p.vocab, h, st);
-    MmOperand w = {static_cast<const uint16_t*>(a.w.p), 0, 0, (int32_t)a.w.ld, (int32_t)p.vocab, (int32_t)p.hidden};
+    MmOperand w = {static_cast<const uint16_t*>(a.w.p), 0, (int32_t)a.w.ld, (int32_t)p.vocab, (int32_t)p.hidden};
     if (p.pack) {
         uint16_t* const to = reinterpret_cast<uint16_t*>(base + p.w_off);
         pad(a.w, p.vocab, (int32_t)p.hidden, p.vocab, p.dp, Ids{nullptr, 0}, p.vocab, to, st);
         w.p = to;
         w.ld = w.cols = p.dp;
     }
-    const MmOperand oh = {h, 0, 0, p.dp, p.tp, p.dp};
+    const MmOperand oh = {h, 0, p.dp, p.tp, p.dp};
     Stat* const stats = reinterpret_cast<Stat*>(base + p.stat_off);
     float* const lse = p.parts ? reinterpret_cast<float*>(base + p.lse_off) : nullptr;
     float* const coef = p.parts ? reinterpret_cast<float*>(base + p.coef_off) : nullptr;
     Mm q = {};
-    q.segs = q.batches = 1;
+    q.segs = 1;
     q.part = reinterpret_cast<float*>(base + p.part_off);
     hipError_t e;
     const int32_t groups = (int32_t)((p.vocab + wave_columns(p.logits.tile) - 1) / wave_columns(p.logits.tile));
@@ -326,7 +326,7 @@ hipError_t launch_xent(const XentPlan& p, const Xent& a, void* ws, hipStream_t s
         g.turns = p.dp / kMmTurn;
         const EndGrad end = {d, size, np, p.parts, p.tp, lse, coef, a.target, v0, (int32_t)p.tokens, n};
         if ((e = product<true, true, true>(p.back, g, end, st)) != hipSuccess) return e;
-        const MmOperand od = {d, 0, size, np, p.tp, np};
+        const MmOperand od = {d, size, np, p.tp, np};
         if (p.dh_parts) {
             Mm g2 = q;
             g2.a = od;
