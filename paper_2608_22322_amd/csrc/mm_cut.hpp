@@ -6,15 +6,22 @@
 
 namespace al {
 
+// Segments that a tile's turns are taken in; parts: of both operands together (2 to 4).
+int mm_segments(int tile, int parts);
+// us, measured, of `tiles` tiles of `turns` turns (a segment) each, every tile a workgroup's.
+double mm_time(int tile, int64_t tiles, int64_t turns, int parts);
+// What a turn takes of a slot's time with `slots` workgroups at work, and what a tile takes besides its turns.
+double mm_turn(int tile, int64_t slots, int parts);
+double mm_ends(int tile, int64_t slots, int parts);
+// Workgroups that a compute unit holds.
+int mm_fit(int tile, int parts);
+
 struct MmCut {
     int32_t tile, splits;
 };
-// One product: tile and splits of k by a measured model.
-MmCut mm_cut(int64_t m, int64_t n, int64_t turns);
+// One product: tile and splits of k.
+MmCut mm_cut(int64_t m, int64_t n, int64_t turns, int parts);
 // Bytes of the partial sums of a product cut so.
 size_t mm_part_bytes(const MmCut& c, int64_t m, int64_t n);
-
-// us of `tiles` outputs of `turns` turns each, every tile a workgroup's.
-double mm_time(int tile, int64_t tiles, int64_t turns);
 
 }  // namespace al

@@ -4,7 +4,8 @@
 //   out[m][n] = sum over k of A(m, k) B(n, k)
 //
 // Either operand lies in memory with k along its rows (a row for each m or n) or with k down its rows (a row for each
-// k). Sums are fp32. k is taken in turns of 64, and where an operand ends inside a turn the other one holds zeros.
+// k), and is one matrix of 16-bit numbers or the sum of a high and a low part (products of two low parts are dropped). Sums
+// are fp32. k is taken in turns of 64, and where an operand ends inside a turn the other one holds zeros.
 #pragma once
 
 #include <type_traits>
@@ -17,6 +18,7 @@ typedef short s16x4 __attribute__((ext_vector_type(4)));
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef f32x4 MmAcc;
 
 constexpr int kMmTurn = 64;
 
@@ -25,33 +27,53 @@ constexpr int kMmTurn = 64;
 // 8, ld too, and p is 16-byte aligned), for outputs that are not written or against zeros of the other operand.
 struct MmOperand {
     const uint16_t* p;
-    int64_t lo;  // elements from a matrix to its low part
+    int64_t lo;  // elements from the high part to the low
     int32_t ld, rows, cols;
 };
 
-// A product. An operand may be the sum of a high and a low part: `segs` segments of `turns` turns each, segment
-// i with the low part of A (B) where bit i of amask (bmask) is set.
 struct Mm {
     MmOperand a, b;
-    int32_t m, n, turns, segs;
+    int32_t m, n, turns;
+    // Operands in parts are taken together by 64-wide tiles (PA, PB: their parts; what is loaded serves two or three products). Larger tiles have no room for it in LDS and take
+    // `segs` segments of `turns` turns each instead, segment i with the low part of A (B) where bit i of amask (bmask) is set.
+    int32_t segs;
     uint32_t amask, bmask;
-    int32_t splits;  // over the turns
+    int32_t splits;  // over the turns of all segments
     int32_t sym;     // A A^T: the tiles on and below the diagonal alone
     float* part;     // splits > 1: partial sums, [split][tile][lanes' order]
 };
 
+// A workgroup's tile of B x B outputs. PA, PB: parts of the operands.
 template <int B>
 struct MmTile {
     static constexpr int kThreads = B == 256 ? 512 : 256, kWaves = kThreads / 64, WM = B / 2, WN = B == 64 ? 32 : 64, FM = WM / 16, FN = WN / 16;
-    static constexpr int kStages = B == 64 ? 4 : 2;  // turns in LDS: 64 (64-wide tiles), 64 and 128 KB
-    static constexpr int kChunks = B * kMmTurn / 8 / kThreads;  // 16-byte pieces of an operand that a thread stages in a turn
+    static constexpr int kChunks = B * kMmTurn / 8 / kThreads;  // 16-byte pieces of a part that a thread stages in a turn
     static __device__ __forceinline__ int wave_m(int w) { return w / (B / WN) * WM; }
     static __device__ __forceinline__ int wave_n(int w) { return w % (B / WN) * WN; }
     static uint32_t side(int n) { return (uint32_t)((n + B - 1) / B); }
     static uint32_t tiles(const Mm& p) { return side(p.m) * side(p.n); }
 };
+// Turns that LDS holds: 64 KB of them, two workgroups a compute unit, or two turns of 256-wide tiles (128 KB).
+template <int B, int PA, int PB>
+constexpr int mm_stages() { return B == 64 && PA + PB == 2 ? 4 : 2; }
 
-typedef f32x4 MmAcc;
+// The places of a tile's turns: arrays of their own, so that the compiler knows that a read of one does not wait for the loads into the others.
+template <int PA, int PB, int S>
+struct MmPlaces {
+    uint16_t *a[S][PA], *b[S][PB];
+};
+#define MM_ARRAY(name, used) __shared__ __attribute__((aligned(16))) uint16_t name[(used) ? kMmArray : 8]
+#define MM_PLACES(B, PA, PB, places)                                                                                               \
+    constexpr int kMmArray = (B) * kMmTurn, kMmStages = mm_stages<B, PA, PB>();                                                    \
+    MM_ARRAY(mm_a00, true); MM_ARRAY(mm_a10, true); MM_ARRAY(mm_b00, true); MM_ARRAY(mm_b10, true);                                \
+    MM_ARRAY(mm_a01, PA > 1); MM_ARRAY(mm_a11, PA > 1); MM_ARRAY(mm_b01, PB > 1); MM_ARRAY(mm_b11, PB > 1);                        \
+    MM_ARRAY(mm_a20, kMmStages > 2); MM_ARRAY(mm_a30, kMmStages > 2); MM_ARRAY(mm_b20, kMmStages > 2); MM_ARRAY(mm_b30, kMmStages > 2); \
+    MmPlaces<PA, PB, kMmStages> places;                                                                                            \
+    places.a[0][0] = mm_a00, places.a[1][0] = mm_a10, places.b[0][0] = mm_b00, places.b[1][0] = mm_b10;                            \
+    if constexpr (PA > 1) places.a[0][PA - 1] = mm_a01, places.a[1][PA - 1] = mm_a11;                                              \
+    if constexpr (PB > 1) places.b[0][PB - 1] = mm_b01, places.b[1][PB - 1] = mm_b11;                                              \
+    if constexpr (kMmStages > 2)                                                                                                   \
+        places.a[kMmStages - 2][0] = mm_a20, places.a[kMmStages - 1][0] = mm_a30, places.b[kMmStages - 2][0] = mm_b20, places.b[kMmStages - 1][0] = mm_b30
 
 union MmFragment {
     s16x4 h[2];
@@ -77,12 +99,15 @@ __device__ __forceinline__ int mm_swizzle(int k) {
     return ((k & 3) | ((k >> 1) & 4) | ((k << 1) & 8)) & (B / 16 - 1);
 }
 
-// Sums of 16 x 16 blocks: a lane holds row 16 i + l % 16 and columns 16 j + 4 (l / 16) + 0..3 of its wavefront's part.
-template <class T, int B, bool AK, bool BK, bool ENDS>
+// Sums of 16 x 16 blocks: a lane holds row 16 i + l % 16 and columns 16 j + 4 (l / 16) + 0..3 of its wavefront's part. AK, BK: k along the rows of the operand.
+// ENDS: B may end inside a turn.
+template <class T, int B, bool AK, bool BK, bool ENDS, int PA, int PB>
 struct MmCore {
     typedef MmTile<B> G;
     typedef __attribute__((address_space(3))) uint16_t* lds_t;
     typedef __attribute__((address_space(3))) s16x4* lds_s16x4;
+    static constexpr int S = mm_stages<B, PA, PB>();
+    typedef MmPlaces<PA, PB, S> Places;
 
     // byte offset of this thread's piece i of the turn at k0 from the turn's first element. SHORT: the operand may end inside the turn.
     template <bool K, bool SHORT>
@@ -112,9 +137,9 @@ struct MmCore {
     // A lane's places of block 0, in bytes: of either half (k along the rows), or of the two reads of a fragment (k down the rows, where
     // block i's unit differs from block 0's by an exclusive or).
     template <bool K>
-    struct Places {
+    struct Reader {
         uint32_t at[2];
-        __device__ __forceinline__ Places(int first, int lane) {
+        __device__ __forceinline__ Reader(int first, int lane) {
 #pragma unroll
             for (int s = 0; s < 2; ++s) {
                 if (K) {
@@ -143,11 +168,8 @@ struct MmCore {
         }
     };
 
-    // Turns t0 .. t1 of a tile. as, bs: kStages places for a turn of either operand (arrays of their own, so that the compiler knows that a
-    // read of one does not wait for the loads into the others).
-    static __device__ __forceinline__ void run(const Mm& p, int m0, int n0, int t0, int t1, uint16_t* const (&as)[G::kStages],
-                                               uint16_t* const (&bs)[G::kStages], MmAcc (&acc)[G::FM][G::FN]) {
-        constexpr int S = G::kStages;
+    // Turns t0 .. t1 of the tile whose first output is m0, n0.
+    static __device__ __forceinline__ void run(const Mm& p, int m0, int n0, int t0, int t1, const Places& at, MmAcc (&acc)[G::FM][G::FN]) {
         const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6);
         uint32_t oa[G::kChunks], ob[G::kChunks];
 #pragma unroll
@@ -155,21 +177,45 @@ struct MmCore {
             oa[i] = offset<AK, false>(p.a, m0, i, tid, 0);
             ob[i] = offset<BK, false>(p.b, n0, i, tid, 0);
         }
-        const uint16_t *const pa = p.a.p, *const pb = p.b.p;
         int seg = t0 / p.turns, k0 = (t0 - seg * p.turns) * kMmTurn;  // of the next turn to load
         const auto load = [&](int s) __attribute__((always_inline)) {
-            issue<AK, false>(p.a, (p.amask >> seg) & 1 ? pa + p.a.lo : pa, m0, k0, oa, as[s], (w << 6) | lane);
-            issue<BK, ENDS>(p.b, (p.bmask >> seg) & 1 ? pb + p.b.lo : pb, n0, k0, ob, bs[s], (w << 6) | lane);
+#pragma unroll
+            for (int q = 0; q < PA; ++q) issue<AK, false>(p.a, q || (p.amask >> seg) & 1 ? p.a.p + p.a.lo : p.a.p, m0, k0, oa, at.a[s][q], (w << 6) | lane);
+#pragma unroll
+            for (int q = 0; q < PB; ++q) issue<BK, ENDS>(p.b, q || (p.bmask >> seg) & 1 ? p.b.p + p.b.lo : p.b.p, n0, k0, ob, at.b[s][q], (w << 6) | lane);
             k0 += kMmTurn;
             if (k0 == p.turns * kMmTurn) k0 = 0, ++seg;
         };
-        Places<AK> am(G::wave_m(w), lane);
-        Places<BK> bn(G::wave_n(w), lane);
+        Reader<AK> am(G::wave_m(w), lane);
+        Reader<BK> bn(G::wave_n(w), lane);
+        struct Half {
+            MmFragment a[PA][G::FM], b[PB][G::FN];
+        };
+        const auto read_a = [&](Half& f, int s, int i, int h) __attribute__((always_inline)) {
+#pragma unroll
+            for (int q = 0; q < PA; ++q) f.a[q][i] = am.read(at.a[s][q], i, h);
+        };
+        const auto read_b = [&](Half& f, int s, int h) __attribute__((always_inline)) {
+#pragma unroll
+            for (int q = 0; q < PB; ++q)
+#pragma unroll
+                for (int j = 0; j < G::FN; ++j) f.b[q][j] = bn.read(at.b[s][q], j, h);
+        };
+        const auto multiply = [&](const Half& f, int i) __attribute__((always_inline)) {
+#pragma unroll
+            for (int j = 0; j < G::FN; ++j) acc[i][j] = mm_mul<T>(f.b[0][j], f.a[0][i], acc[i][j]);
+            if (PB > 1)
+#pragma unroll
+                for (int j = 0; j < G::FN; ++j) acc[i][j] = mm_mul<T>(f.b[PB - 1][j], f.a[0][i], acc[i][j]);
+            if (PA > 1)
+#pragma unroll
+                for (int j = 0; j < G::FN; ++j) acc[i][j] = mm_mul<T>(f.b[0][j], f.a[PA - 1][i], acc[i][j]);
+        };
         // This wavefront's pieces of a turn have arrived (`behind`: those of the S - 2 turns after it may be in flight: vmcnt), and what it read of an earlier one is
         // in its registers (lgkmcnt); behind the barrier that holds for all, and the loads into the earlier turn's place may begin. (__syncthreads would wait for every load.)
         const auto meet = [&](bool behind) __attribute__((always_inline)) {
             if (S > 2 && behind)
-                __builtin_amdgcn_s_waitcnt(0x0070 | (S - 2) * 2 * G::kChunks);
+                __builtin_amdgcn_s_waitcnt(0x0070 | (S - 2) * (PA + PB) * G::kChunks);
             else
                 __builtin_amdgcn_s_waitcnt(0x0070);
             asm volatile("" ::: "memory");
@@ -180,23 +226,18 @@ struct MmCore {
         if constexpr (B == 256) {
             // The barrier lies between the halves of a turn: the products of the second half, whose fragments are in registers, cover the next turn's first
             // reads and the issuing of loads (8 wavefronts, 2 a SIMD; 4096^3: 240 us with the barrier between the turns, 220 so. The smaller tiles have fewer products to
-            // cover them with, and take longer so.)
-            struct Half {
-                MmFragment a[G::FM], b[G::FN];
-            } f0, f1;
+            // cover them with, and take longer so).
+            Half f0, f1;
             const auto read = [&](Half& f, int s, int h) __attribute__((always_inline)) {
                 am.renew();
                 bn.renew();
+                read_b(f, s, h);
 #pragma unroll
-                for (int j = 0; j < G::FN; ++j) f.b[j] = bn.read(bs[s], j, h);
-#pragma unroll
-                for (int i = 0; i < G::FM; ++i) f.a[i] = am.read(as[s], i, h);
+                for (int i = 0; i < G::FM; ++i) read_a(f, s, i, h);
             };
-            const auto multiply = [&](const Half& f) __attribute__((always_inline)) {
+            const auto multiply_all = [&](const Half& f) __attribute__((always_inline)) {
 #pragma unroll
-                for (int i = 0; i < G::FM; ++i)
-#pragma unroll
-                    for (int j = 0; j < G::FN; ++j) acc[i][j] = mm_mul<T>(f.b[j], f.a[i], acc[i][j]);
+                for (int i = 0; i < G::FM; ++i) multiply(f, i);
             };
 #pragma unroll
             for (int s = 0; s < S; ++s)
@@ -209,7 +250,7 @@ struct MmCore {
                     if (t + s >= t1) break;
                     read(f1, s, 1);
                     __builtin_amdgcn_sched_barrier(0);
-                    multiply(f0);
+                    multiply_all(f0);
                     __builtin_amdgcn_sched_barrier(0);
                     if (t + s + 1 < t1) {
                         meet(t + s + S - 1 < t1);
@@ -217,7 +258,7 @@ struct MmCore {
                         if (t + s + S < t1) load(s);
                     }
                     __builtin_amdgcn_sched_barrier(0);
-                    multiply(f1);
+                    multiply_all(f1);
                     __builtin_amdgcn_sched_barrier(0);
                 }
             }
@@ -235,14 +276,12 @@ struct MmCore {
                     bn.renew();
 #pragma unroll
                     for (int h = 0; h < 2; ++h) {
-                        MmFragment fb[G::FN];
-#pragma unroll
-                        for (int j = 0; j < G::FN; ++j) fb[j] = bn.read(bs[s], j, h);
+                        Half f;
+                        read_b(f, s, h);
 #pragma unroll
                         for (int i = 0; i < G::FM; ++i) {
-                            const MmFragment fa = am.read(as[s], i, h);
-#pragma unroll
-                            for (int j = 0; j < G::FN; ++j) acc[i][j] = mm_mul<T>(fb[j], fa, acc[i][j]);
+                            read_a(f, s, i, h);
+                            multiply(f, i);
                         }
                     }
                 }
@@ -250,15 +289,6 @@ struct MmCore {
         }
     }
 };
-
-// The places of a tile's turns in LDS: arrays of their own.
-#define MM_PLACES(B, as, bs)                                                                                                                        \
-    __shared__ __attribute__((aligned(16))) uint16_t as##0_[B * kMmTurn], as##1_[B * kMmTurn], bs##0_[B * kMmTurn], bs##1_[B * kMmTurn];            \
-    __shared__ __attribute__((aligned(16))) uint16_t as##2_[MmTile<B>::kStages > 2 ? B * kMmTurn : 8], as##3_[MmTile<B>::kStages > 2 ? B * kMmTurn : 8], \
-        bs##2_[MmTile<B>::kStages > 2 ? B * kMmTurn : 8], bs##3_[MmTile<B>::kStages > 2 ? B * kMmTurn : 8];                                         \
-    uint16_t *as[MmTile<B>::kStages], *bs[MmTile<B>::kStages];                                                                                      \
-    as[0] = as##0_, as[1] = as##1_, bs[0] = bs##0_, bs[1] = bs##1_;                                                                                 \
-    if constexpr (MmTile<B>::kStages > 2) as[2] = as##2_, as[3] = as##3_, bs[2] = bs##2_, bs[3] = bs##3_
 
 // Tile number (the same in all lanes) -> its rows and columns of tiles: the triangle on and below the diagonal row by row, others in bands of 8 along m.
 struct MmAt {
@@ -297,14 +327,16 @@ template <class E, class = void>
 struct MmRows : std::false_type {};
 template <class E>
 struct MmRows<E, std::enable_if_t<E::kRows>> : std::true_type {};
-template <class T, int B, bool AK, bool BK, bool ENDS, class E>
+
+template <class T, int B, bool AK, bool BK, bool ENDS, int PA, class E>
 __global__ __launch_bounds__(MmTile<B>::kThreads, 2) void mm_kernel(Mm p, E end) {
     typedef MmTile<B> G;
-    MM_PLACES(B, as, bs);
+    MM_PLACES(B, PA, 1, places);
     const MmId id = mm_id<B>(p);
-    const int total = p.turns * p.segs, t0 = (int)((int64_t)total * id.split / p.splits), t1 = (int)((int64_t)total * (id.split + 1) / p.splits);
+    const int64_t turns = p.turns * p.segs;
+    const int t0 = (int)(turns * id.split / p.splits), t1 = (int)(turns * (id.split + 1) / p.splits);
     MmAcc acc[G::FM][G::FN] = {};
-    MmCore<T, B, AK, BK, ENDS>::run(p, id.m * B, id.n * B, t0, t1, as, bs, acc);
+    MmCore<T, B, AK, BK, ENDS, PA, 1>::run(p, id.m * B, id.n * B, t0, t1, places, acc);
     const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
     const int m = id.m * B + G::wave_m(w) + (lane & 15), n = id.n * B + G::wave_n(w) + 4 * (lane >> 4);
     if (p.splits > 1) {
@@ -320,11 +352,9 @@ __global__ __launch_bounds__(MmTile<B>::kThreads, 2) void mm_kernel(Mm p, E end)
         __builtin_amdgcn_sched_barrier(0);
         if constexpr (MmRows<E>::value) {
             end.template row<G::FN>(m + 16 * i, n, lane, acc[i]);
-            continue;
-        }
+        } else {
 #pragma unroll
-        for (int j = 0; j < G::FN; ++j) {
-            if constexpr (!MmRows<E>::value) end(m + 16 * i, n + 16 * j, acc[i][j]);
+            for (int j = 0; j < G::FN; ++j) end(m + 16 * i, n + 16 * j, acc[i][j]);
         }
     }
 }
@@ -352,11 +382,12 @@ __global__ __launch_bounds__(256) void mm_join_kernel(Mm p, E end, uint32_t tile
     end(id.m * B + G::wave_m((int)w) + (int)(lane & 15) + 16 * (int)(e / G::FN), id.n * B + G::wave_n((int)w) + 4 * (int)(lane >> 4) + 16 * (int)(e % G::FN), v);
 }
 
-template <class T, int B, bool AK, bool BK, bool ENDS, class E>
+// B in one part.
+template <class T, int B, bool AK, bool BK, bool ENDS, int PA, class E>
 hipError_t mm_launch(const Mm& p, const E& end, hipStream_t st) {
     const uint32_t tiles = MmTile<B>::tiles(p);
     if (tiles == 0) return hipSuccess;
-    mm_kernel<T, B, AK, BK, ENDS, E><<<tiles * (uint32_t)p.splits, MmTile<B>::kThreads, 0, st>>>(p, end);
+    mm_kernel<T, B, AK, BK, ENDS, PA, E><<<tiles * (uint32_t)p.splits, MmTile<B>::kThreads, 0, st>>>(p, end);
     if constexpr (!MmRows<E>::value)
         if (p.splits > 1) mm_join_kernel<B, E><<<tiles * (B * B / 1024), 256, 0, st>>>(p, end, tiles);
     return hipGetLastError();

@@ -187,10 +187,11 @@ __host__ __device__ inline int64_t item_tiles(const OrthoItem& t, int kind, int 
     const int64_t s = ((t.rp < t.cp ? t.rp : t.cp) + tile - 1) / tile;
     return s * (s + 1) / 2;
 }
-__host__ __device__ inline int32_t item_turns(const OrthoItem& t, int kind, int parts) {
-    const int32_t k = kind == kGram ? (t.rp > t.cp ? t.rp : t.cp) : t.rp < t.cp ? t.rp : t.cp;
-    return k / kMmTurn * (parts > 1 ? 3 : 1);
+// Turns of a segment, and segments.
+__host__ __device__ inline int32_t item_turns(const OrthoItem& t, int kind) {
+    return (kind == kGram ? (t.rp > t.cp ? t.rp : t.cp) : t.rp < t.cp ? t.rp : t.cp) / kMmTurn;
 }
+__host__ __device__ constexpr int32_t item_segments(int tile, int parts) { return tile > 64 && parts > 1 ? 3 : 1; }
 
 // One item's product.
 template <int KIND>
@@ -208,17 +209,18 @@ struct Task {
         g = {t.a, (int64_t)dp * dp, dp, a.parts};
         b = {t.a + a.parts * g.size, g.size, dp, a.parts};
     }
+    template <int B>
     __device__ __forceinline__ Mm product() const {
         Mm p;
-        p.segs = a.parts > 1 ? 3 : 1;
-        p.amask = a.parts > 1 ? 4u : 0u;
-        p.bmask = a.parts > 1 ? 2u : 0u;
+        p.segs = item_segments(B, a.parts);
+        p.amask = p.segs > 1 ? 4u : 0u;
+        p.bmask = p.segs > 1 ? 2u : 0u;
         p.splits = 1;
         p.part = nullptr;
         p.sym = square_kind(KIND);
         p.m = square_kind(KIND) ? dp : t.rp;
         p.n = square_kind(KIND) ? dp : t.cp;
-        p.turns = item_turns(t, KIND, 1);
+        p.turns = item_turns(t, KIND);
         const MmOperand ox = x.operand(t.rp);
         p.a = KIND == kGram ? ox : KIND == kPoly ? g.operand(dp) : tall ? ox : b.operand(dp);
         p.b = KIND == kGram ? ox : KIND == kPoly ? g.operand(dp) : tall ? b.operand(dp) : ox;
@@ -305,9 +307,9 @@ struct Image {
     typedef __attribute__((address_space(3))) f16x4* lds_f16x4;
     typedef __attribute__((address_space(3))) f16* lds_f16;
     uint32_t a0, a1, b0, b1;  // LDS addresses (a choice among pointers would be a generic one)
-    __device__ __forceinline__ Image(uint16_t* const (&as)[G::kStages], uint16_t* const (&bs)[G::kStages])
-        : a0((uint32_t)(uintptr_t)(lds_u16)as[0]), a1((uint32_t)(uintptr_t)(lds_u16)as[1]), b0((uint32_t)(uintptr_t)(lds_u16)bs[0]),
-          b1((uint32_t)(uintptr_t)(lds_u16)bs[1]) {}
+    __device__ __forceinline__ Image(uint16_t* p0, uint16_t* p1, uint16_t* p2, uint16_t* p3)
+        : a0((uint32_t)(uintptr_t)(lds_u16)p0), a1((uint32_t)(uintptr_t)(lds_u16)p1), b0((uint32_t)(uintptr_t)(lds_u16)p2),
+          b1((uint32_t)(uintptr_t)(lds_u16)p3) {}
     // rows 64 q .. 64 q + 63
     __device__ __forceinline__ uint32_t rows(int q) const { return B == 64 ? a0 : B == 128 ? (q & 1 ? a1 : a0) : q & 2 ? (q & 1 ? b1 : b0) : (q & 1 ? a1 : a0); }
     // bytes from those on
@@ -453,15 +455,16 @@ __device__ __forceinline__ int item_at(const OrthoLaunch& a, int64_t pos) {
 }
 
 // Turns t0 .. t1 of a tile, and its end or, where that is not all of it, its partial sums.
-template <int B, int KIND, bool TALL>
-__device__ __forceinline__ void segment(const Task<KIND>& task, int tile, int t0, int t1, int64_t place, uint16_t* const (&as)[MmTile<B>::kStages],
-                                        uint16_t* const (&bs)[MmTile<B>::kStages]) {
+template <int B, int KIND, int PARTS>
+using PlacesOf = MmPlaces<PARTS, PARTS, mm_stages<B, PARTS, PARTS>()>;
+template <int B, int KIND, int PARTS, bool TALL>
+__device__ __forceinline__ void segment(const Task<KIND>& task, int tile, int t0, int t1, int64_t place, const PlacesOf<B, KIND, PARTS>& at) {
     typedef MmTile<B> G;
-    const Mm p = task.product();
+    const Mm p = task.template product<B>();
     const MmAt id = mm_at<B>(p, (uint32_t)tile);
     MmAcc acc[G::FM][G::FN] = {};
     constexpr bool kRows = KIND == kPoly || (KIND == kGram ? !TALL : true), kCols = KIND == kPoly || (KIND == kGram ? !TALL : TALL);  // k along the rows
-    MmCore<f16, B, kRows, kCols, false>::run(p, id.m * B, id.n * B, t0, t1, as, bs, acc);
+    MmCore<f16, B, kRows, kCols, false, PARTS, PARTS>::run(p, id.m * B, id.n * B, t0, t1, at, acc);
     if (t1 - t0 < p.turns * p.segs) {
         const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
         f32x4* const part = reinterpret_cast<f32x4*>(task.a.part) + (place * G::kWaves + w) * (G::FM * G::FN * 64) + lane;
@@ -471,21 +474,21 @@ __device__ __forceinline__ void segment(const Task<KIND>& task, int tile, int t0
             for (int j = 0; j < G::FN; ++j) part[(r * G::FN + j) * 64] = acc[r][j];
     } else {
         __syncthreads();  // every wavefront has read its last turn
-        finish<B, KIND>(task, id.m * B, id.n * B, Image<B>(as, bs), acc);
+        finish<B, KIND>(task, id.m * B, id.n * B, Image<B>(at.a[0][0], at.a[1][0], at.b[0][0], at.b[1][0]), acc);
     }
 }
-template <int B, int KIND>
-__device__ __forceinline__ void segment(const Task<KIND>& task, int tile, int t0, int t1, int64_t place, uint16_t* const (&as)[MmTile<B>::kStages],
-                                        uint16_t* const (&bs)[MmTile<B>::kStages]) {
+template <int B, int KIND, int PARTS>
+__device__ __forceinline__ void segment(const Task<KIND>& task, int tile, int t0, int t1, int64_t place, const PlacesOf<B, KIND, PARTS>& at) {
     if (KIND != kPoly && task.tall)
-        segment<B, KIND, true>(task, tile, t0, t1, place, as, bs);
+        segment<B, KIND, PARTS, true>(task, tile, t0, t1, place, at);
     else
-        segment<B, KIND, false>(task, tile, t0, t1, place, as, bs);
+        segment<B, KIND, PARTS, false>(task, tile, t0, t1, place, at);
 }
 
-template <int B, int KIND>
+template <int B, int KIND, int PARTS>
 __global__ __launch_bounds__(MmTile<B>::kThreads, 2) void ortho_kernel(OrthoLaunch a) {
-    MM_PLACES(B, as, bs);
+    constexpr int PA = PARTS, PB = PARTS;
+    MM_PLACES(B, PA, PB, places);
     // An XCD takes a contiguous eighth of each item's tiles, the items one after the other (longest first): contiguous eighths of all the tiles would leave the long ones
     // to some of the XCDs. Items with few tiles begin at different XCDs.
     uint32_t k = blockIdx.x >> 3, tile = 0;
@@ -497,22 +500,23 @@ __global__ __launch_bounds__(MmTile<B>::kThreads, 2) void ortho_kernel(OrthoLaun
         k -= mine;
     }
     if (i == a.count) return;
-    segment<B, KIND>(Task<KIND>(a, i), (int32_t)tile, 0, item_turns(a.it[i], KIND, a.parts), 0, as, bs);
+    segment<B, KIND, PARTS>(Task<KIND>(a, i), (int32_t)tile, 0, item_turns(a.it[i], KIND) * item_segments(B, a.parts), 0, places);
 }
 
 // The turns dealt out to slots. (Kernels of their own: the loop over a slot's tiles takes registers that 256-wide tiles do not have.)
-template <int B, int KIND>
+template <int B, int KIND, int PARTS>
 __global__ __launch_bounds__(MmTile<B>::kThreads, 2) void ortho_slots_kernel(OrthoLaunch a) {
-    MM_PLACES(B, as, bs);
+    constexpr int PA = PARTS, PB = PARTS;
+    MM_PLACES(B, PA, PB, places);
     const int64_t g = xcd_block(blockIdx.x, gridDim.x), stop = slot_begin(a, g + 1);
     int64_t at = slot_begin(a, g), place = 2 * g;
     while (at < stop) {
         const int i = item_at(a, at);
         const Task<KIND> task(a, i);
-        const int32_t turns = item_turns(a.it[i], KIND, a.parts);
+        const int32_t turns = item_turns(a.it[i], KIND) * item_segments(B, a.parts);
         const int64_t local = at - a.begin[i];
         const int32_t tile = __builtin_amdgcn_readfirstlane((int32_t)(local / turns)), t0 = __builtin_amdgcn_readfirstlane((int32_t)(local - (int64_t)tile * turns)), t1 = (int32_t)min((int64_t)turns, t0 + (stop - at));
-        segment<B, KIND>(task, tile, t0, t1, place, as, bs);
+        segment<B, KIND, PARTS>(task, tile, t0, t1, place, places);
         at += t1 - t0;
         place = 2 * g + 1;
         __syncthreads();  // every wavefront has read its last turn, or the tile's last image
@@ -527,7 +531,7 @@ __global__ __launch_bounds__(256) void ortho_join_kernel(OrthoLaunch a) {
     const int64_t g = blockIdx.x / kBlocks + 1, pos = slot_begin(a, g);
     const int i = item_at(a, pos);
     const Task<KIND> task(a, i);
-    const Mm p = task.product();
+    const Mm p = task.template product<B>();
     const int32_t turns = p.turns * p.segs, tile = (int32_t)((pos - a.begin[i]) / turns);
     const int64_t s = a.begin[i] + (int64_t)tile * turns, e = s + turns, before = slot_begin(a, g - 1);
     if (pos == s || before > s) return;
@@ -551,23 +555,23 @@ __global__ __launch_bounds__(256) void ortho_join_kernel(OrthoLaunch a) {
              p.sym && id.m != id.n);
 }
 
-template <int B, int KIND>
+template <int B, int KIND, int PARTS>
 hipError_t launch(const OrthoLaunch& a, hipStream_t st) {
     if constexpr (B < 256) {
         if (a.slots) {
-            ortho_slots_kernel<B, KIND><<<(uint32_t)a.slots, MmTile<B>::kThreads, 0, st>>>(a);
+            ortho_slots_kernel<B, KIND, PARTS><<<(uint32_t)a.slots, MmTile<B>::kThreads, 0, st>>>(a);
             ortho_join_kernel<B, KIND><<<(uint32_t)((a.slots - 1) * (B * B / 1024)), 256, 0, st>>>(a);
             return hipGetLastError();
         }
     }
     uint32_t most = 0;  // of an XCD
     for (int i = 0; i < a.count; ++i) most += (uint32_t)((a.begin[i + 1] - a.begin[i] + 7) / 8);
-    ortho_kernel<B, KIND><<<8 * most, MmTile<B>::kThreads, 0, st>>>(a);
+    ortho_kernel<B, KIND, PARTS><<<8 * most, MmTile<B>::kThreads, 0, st>>>(a);
     return hipGetLastError();
 }
 
 // How a group's product is cut: the tile and, where that is faster by the measured times, the slots that its turns are dealt out to. Slots that work at different places of k
-// share little of what they load: whole tiles run in step and find their neighbours' loads in the L2 (FIGURES). What dealing out is for is few tiles and a long sum.
+// share little of what they load: whole tiles run in step and find their neighbours' loads in the L2. What dealing out is for is few tiles and a long sum.
 struct Cut {
     int32_t tile;
     int64_t slots;
@@ -580,28 +584,28 @@ Cut group_cut(const OrthoLaunch& a, int kind) {
         bytes += 2.0 * a.parts * (kind == kGram ? x : kind == kPoly ? d * d : x + d * d);
     }
     const double rate = bytes < 8e6 ? 17e6 : bytes < 100e6 ? 7e6 : 4.4e6;  // bytes a us, from the L2s, the last-level cache and memory
+    const int parts = 2 * a.parts;
     for (const int tile : {64, 128, 256}) {
+        const int segs = mm_segments(tile, parts);
         int64_t tiles = 0, turns = 0;
         int32_t most = 0, same = 1;
         for (int i = 0; i < a.count; ++i) {
             const int64_t n = item_tiles(a.it[i], kind, tile);
-            const int32_t t = item_turns(a.it[i], kind, a.parts);
+            const int32_t t = item_turns(a.it[i], kind);
             if (i > 0 && t != most) same = 0;
             tiles += n;
-            turns += n * t;
+            turns += n * t * segs;
             most = std::max(most, t);
         }
-        const double mean = (double)turns / (double)tiles;
-        // tiles of different lengths: the longest begin first, and one that begins alone ends last
-        const double lone = 2 + (tile == 256 ? 10.5 + 1.29 * most : tile == 128 ? 4 + 0.6 * most : 1 + 0.36 * most);
-        const double whole = same ? mm_time(tile, tiles, most) : std::max(lone, mm_time(tile, tiles, (int64_t)std::ceil(mean)));
+        const double mean = (double)turns / (double)tiles;  // turns of all segments
+        // tiles of different lengths: the longest begin first
+        const double whole = same ? mm_time(tile, tiles, most, parts) : std::max(mm_time(tile, 1, most, parts), mm_time(tile, tiles, (int64_t)std::ceil(mean / segs), parts));
         if (least < 0 || whole < least) least = whole, best = {tile, 0};
         for (const int64_t slots : {16, 32, 64, 128, 256, 512}) {
-            if (tile == 256 || turns < 4 * slots) break;
-            const bool two = slots > 256;
-            const double turn = std::max(tile == 128 ? (two ? 1.05 : 0.6) : (two ? 0.42 : 0.36), (double)(slots * tile * 256) / rate),
-                         end = tile == 128 ? (two ? 6 : 4) : (two ? 2 : 1), w = (double)turns / (double)slots,
-                         pieces = std::min((double)(2 * slots), (double)(slots + tiles)), t = 2 + w * turn + (w / mean + 1) * end + 5 + pieces * tile * tile * 4 / 4e6;
+            if (tile == 256 || slots > 256 * mm_fit(tile, parts) || turns < 4 * slots) break;
+            const double turn = std::max(mm_turn(tile, slots, parts), (double)(slots * tile * 128 * (segs > 1 ? 2 : parts)) / rate), w = (double)turns / (double)slots,
+                         pieces = std::min((double)(2 * slots), (double)(slots + tiles)),
+                         t = 2 + w * turn + (w / mean + 1) * (mm_ends(tile, slots, parts) + 1) + 5 + pieces * tile * tile * 4 / 4e6;
             if (t < least) least = t, best = {tile, slots};
         }
     }
@@ -614,8 +618,9 @@ hipError_t product(OrthoLaunch& a, hipStream_t st) {
     a.slots = c.slots;
     a.begin[0] = 0;
     for (int i = 0; i < a.count; ++i)
-        a.begin[i + 1] = a.begin[i] + item_tiles(a.it[i], KIND, c.tile) * (c.slots ? item_turns(a.it[i], KIND, a.parts) : 1);
-    return c.tile == 256 ? launch<256, KIND>(a, st) : c.tile == 128 ? launch<128, KIND>(a, st) : launch<64, KIND>(a, st);
+        a.begin[i + 1] = a.begin[i] + item_tiles(a.it[i], KIND, c.tile) * (c.slots ? item_turns(a.it[i], KIND) * item_segments(c.tile, a.parts) : 1);
+    if (c.tile == 64) return a.parts > 1 ? launch<64, KIND, 2>(a, st) : launch<64, KIND, 1>(a, st);
+    return c.tile == 256 ? launch<256, KIND, 1>(a, st) : launch<128, KIND, 1>(a, st);
 }
 
 // The steps of a group whose X0 lies in place 1; the last one's outputs go where LAST says.

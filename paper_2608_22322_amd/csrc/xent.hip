@@ -214,12 +214,15 @@ struct EndSum {
     }
 };
 
-template <bool AK, bool BK, bool ENDS, class E>
+// PA: parts of A.
+template <bool AK, bool BK, bool ENDS, int PA, class E>
 hipError_t product(const MmCut& cut, Mm p, const E& end, hipStream_t st) {
     p.splits = cut.splits;
-    if (cut.tile == 256) return mm_launch<bf16, 256, AK, BK, ENDS>(p, end, st);
-    if (cut.tile == 128) return mm_launch<bf16, 128, AK, BK, ENDS>(p, end, st);
-    return mm_launch<bf16, 64, AK, BK, ENDS>(p, end, st);
+    p.segs = mm_segments(cut.tile, 1 + PA);
+    p.amask = p.segs > 1 ? 2u : 0u;
+    if (cut.tile == 256) return mm_launch<bf16, 256, AK, BK, ENDS, 1>(p, end, st);
+    if (cut.tile == 128) return mm_launch<bf16, 128, AK, BK, ENDS, 1>(p, end, st);
+    return mm_launch<bf16, 64, AK, BK, ENDS, PA>(p, end, st);
 }
 
 void pad(Mat x, int64_t rows, int32_t cols, int64_t rp, int32_t cp, Ids target, int64_t vocab, uint16_t* out, hipStream_t st) {
@@ -243,7 +246,7 @@ XentPlan xent_plan(int64_t tokens, int64_t hidden, int64_t vocab, int64_t ldw, i
     p.dw_parts = dw ? (grad_dtype == AL_DTYPE_F32 ? 2 : 1) : 0;
     p.parts = std::max(p.dh_parts, p.dw_parts);
     const int64_t turns = p.dp / kMmTurn;
-    p.logits = mm_cut(p.block, vocab, turns);
+    p.logits = mm_cut(p.block, vocab, turns, 2);
     p.logits.splits = 1;
     const auto up = [](size_t x) { return (x + 255) & ~size_t(255); };
     size_t off = 0;
@@ -259,10 +262,10 @@ XentPlan xent_plan(int64_t tokens, int64_t hidden, int64_t vocab, int64_t ldw, i
     if (p.parts) {
         const int64_t room = (int64_t(1) << 26) / p.tp / 256 * 256;
         p.piece = (int32_t)std::min<int64_t>((vocab + 63) / 64 * 64, std::max<int64_t>(256, room));
-        p.back = mm_cut(p.tp, p.piece, turns);
+        p.back = mm_cut(p.tp, p.piece, turns, 2);
         p.back.splits = 1;
-        p.dh = mm_cut(p.tp, hidden, p.piece / kMmTurn * p.dh_parts);
-        p.dw = mm_cut(p.piece, hidden, p.tp / kMmTurn * p.dw_parts);
+        p.dh = mm_cut(p.tp, hidden, p.piece / kMmTurn, 1 + std::max(1, p.dh_parts));
+        p.dw = mm_cut(p.piece, hidden, p.tp / kMmTurn, 1 + std::max(1, p.dw_parts));
         p.lse_off = take((size_t)p.tp * 4);
         p.coef_off = take((size_t)p.tp * 4);
         p.d_off = take((size_t)p.tp * p.piece * 2 * p.parts);
@@ -289,7 +292,6 @@ hipError_t launch_xent(const XentPlan& p, const Xent& a, void* ws, hipStream_t s
     float* const lse = p.parts ? reinterpret_cast<float*>(base + p.lse_off) : nullptr;
     float* const coef = p.parts ? reinterpret_cast<float*>(base + p.coef_off) : nullptr;
     Mm q = {};
-    q.segs = 1;
     q.part = reinterpret_cast<float*>(base + p.part_off);
     hipError_t e;
     const int32_t groups = (int32_t)((p.vocab + wave_columns(p.logits.tile) - 1) / wave_columns(p.logits.tile));
@@ -305,7 +307,7 @@ hipError_t launch_xent(const XentPlan& p, const Xent& a, void* ws, hipStream_t s
         g.n = (int32_t)p.vocab;
         g.turns = p.dp / kMmTurn;
         const EndStats end = {stats, at, a.target, t0, n, (int32_t)p.vocab, groups};
-        if ((e = product<true, true, true>(p.logits, g, end, st)) != hipSuccess) return e;
+        if ((e = product<true, true, true, 1>(p.logits, g, end, st)) != hipSuccess) return e;
         loss_kernel<<<(uint32_t)((padded + 3) / 4), 256, 0, st>>>(stats, at, groups, t0, n, padded, p.vocab, a.target, a.weight, a.scale, a.loss, a.lse, lse, coef);
     }
     if (!p.parts) return hipGetLastError();
@@ -325,7 +327,7 @@ hipError_t launch_xent(const XentPlan& p, const Xent& a, void* ws, hipStream_t s
         g.n = np;
         g.turns = p.dp / kMmTurn;
         const EndGrad end = {d, size, np, p.parts, p.tp, lse, coef, a.target, v0, (int32_t)p.tokens, n};
-        if ((e = product<true, true, true>(p.back, g, end, st)) != hipSuccess) return e;
+        if ((e = product<true, true, true, 1>(p.back, g, end, st)) != hipSuccess) return e;
         const MmOperand od = {d, size, np, p.tp, np};
         if (p.dh_parts) {
             Mm g2 = q;
@@ -334,8 +336,6 @@ hipError_t launch_xent(const XentPlan& p, const Xent& a, void* ws, hipStream_t s
             g2.m = p.tp;
             g2.n = (int32_t)p.hidden;
             g2.turns = np / kMmTurn;
-            g2.segs = p.dh_parts;
-            g2.amask = 2u;
             EndSum s = {};
             s.sum = first ? nullptr : sum;
             s.sum_ld = p.hidden;
@@ -350,7 +350,8 @@ hipError_t launch_xent(const XentPlan& p, const Xent& a, void* ws, hipStream_t s
                 s.ld = p.hidden;
                 s.rows = p.tp;
             }
-            if ((e = product<true, false, true>(p.dh, g2, s, st)) != hipSuccess) return e;
+            e = p.dh_parts > 1 ? product<true, false, true, 2>(p.dh, g2, s, st) : product<true, false, true, 1>(p.dh, g2, s, st);
+            if (e != hipSuccess) return e;
         }
         if (p.dw_parts) {
             Mm g3 = q;
@@ -359,8 +360,6 @@ hipError_t launch_xent(const XentPlan& p, const Xent& a, void* ws, hipStream_t s
             g3.m = n;
             g3.n = (int32_t)p.hidden;
             g3.turns = p.tp / kMmTurn;
-            g3.segs = p.dw_parts;
-            g3.amask = 2u;
             EndSum s = {};
             const int64_t skip = v0 * p.hidden * (a.dw_bf16 ? 2 : 4);
             s.out = static_cast<char*>(a.dw) + skip;
@@ -369,7 +368,8 @@ hipError_t launch_xent(const XentPlan& p, const Xent& a, void* ws, hipStream_t s
             s.rows = n;
             s.cols = (int32_t)p.hidden;
             s.out_bf16 = a.dw_bf16;
-            if ((e = product<false, false, false>(p.dw, g3, s, st)) != hipSuccess) return e;
+            e = p.dw_parts > 1 ? product<false, false, false, 2>(p.dw, g3, s, st) : product<false, false, false, 1>(p.dw, g3, s, st);
+            if (e != hipSuccess) return e;
         }
     }
     return hipGetLastError();
