@@ -35,9 +35,9 @@ def _on_its_gpu(method):
 
 class SwigluMLP:
     """The block's parameters (fp32, with bf16 copies for the products), their gradients and states, and its buffers
-    for batches of `tokens` rows, all on `device`."""
+    for batches of `tokens` rows, all on `device`. lr None: no AdamW states, another optimizer steps the parameters (param, grad)."""
 
-    def __init__(self, hidden: int, ffn: int, tokens: int, block: int = 64, eps: float = 1e-5, lr: float = 1e-3, seed: int = 0,
+    def __init__(self, hidden: int, ffn: int, tokens: int, block: int = 64, eps: float = 1e-5, lr: float | None = 1e-3, seed: int = 0,
                  device="cuda"):
         g = torch.Generator(device=device).manual_seed(seed)
         self.hidden, self.ffn, self.tokens, self.eps = hidden, ffn, tokens, eps
@@ -52,10 +52,14 @@ class SwigluMLP:
             self.param[name], self.grad[name] = p, torch.zeros(rows, cols, **bf16)
             if name != "norm":
                 self.weight[name] = p.bfloat16()
+            if lr is None:
+                self.states.append(ParamState(p, self.grad[name], rows, cols))
+                continue
             (mc, mm), (vc, vm) = alloc_state(p.numel(), m, device), alloc_state(p.numel(), v, device)
             self.states.append(ParamState(p, self.grad[name], rows, cols, m=mc, m_meta=mm, v=vc, v_meta=vm))
-        self.cfg, self.arr = adamw_cfg(lr=lr, m=m, v=v), tensor_array(self.states)
-        self.step_ws = workspace(adamw_workspace_bytes(self.states, self.cfg, arr=self.arr), device)
+        if lr is not None:
+            self.cfg, self.arr = adamw_cfg(lr=lr, m=m, v=v), tensor_array(self.states)
+            self.step_ws = workspace(adamw_workspace_bytes(self.states, self.cfg, arr=self.arr), device)
         # what a batch leaves for its backward pass
         self.xhat = act.alloc_code(tokens, hidden, block, device)
         self.gate_code, self.up_code = act.alloc_code(tokens, ffn, block, device), act.alloc_code(tokens, ffn, block, device)
@@ -108,6 +112,10 @@ class SwigluMLP:
     def step(self, t: int) -> None:
         """One AdamW step (8-bit states) and the weights' bf16 copies from the new parameters."""
         adamw_step(self.states, self.cfg, t, self.step_ws, arr=self.arr)
+        self.refresh()
+
+    def refresh(self) -> None:
+        """The weights' bf16 copies from the parameters."""
         for name, w in self.weight.items():
             w.copy_(self.param[name])
 

@@ -1,0 +1,152 @@
+"""Orthogonalised matrices against the 64-bit definition: sides from one up, both operand orders, types, pitches, streams, graphs, bad values."""
+import numpy as np
+import pytest
+import torch
+
+from tests.act_util import DT, f64, gpu, out_like, untouched
+from tests.ortho_util import newton_schulz, tolerance
+
+pytestmark = pytest.mark.gpu
+
+OUT = {"f32": 2.0**-24, "bf16": 2.0**-8}
+
+
+def run(x, out, **kw):
+    import paper_2608_22322_amd as al
+    from paper_2608_22322_amd import muon
+
+    ws = al.workspace(muon.orthogonalize_workspace_bytes(x, out, kw.get("parts")))
+    ws.fill_(0xff)  # what an earlier call left: NaN to whoever reads it
+    muon.orthogonalize(x, out, ws, **kw)
+    return out
+
+
+def matrix(rows, cols, dtype, seed, spread=0.0):
+    rng = np.random.default_rng(seed)
+    x = rng.normal(size=(rows, cols)) * np.exp(spread * rng.normal(size=cols)) * 1e-3
+    return torch.from_numpy(x.astype(np.float32)).to(DT[dtype])
+
+
+SHAPES = [(1, 1), (1, 300), (300, 1), (2, 3), (63, 65), (65, 63), (60, 50), (50, 60), (64, 64), (64, 128), (129, 64), (500, 64), (64, 1750), (257, 256),
+          (300, 700), (700, 301), (1001, 130), (100, 4100), (4100, 100)]
+
+
+@pytest.mark.parametrize("rows,cols", SHAPES)
+@pytest.mark.parametrize("dtype,out,parts", [("bf16", "bf16", None), ("f32", "f32", None), ("f32", "bf16", 2), ("bf16", "f32", 1)])
+def test_against_the_definition(rows, cols, dtype, out, parts):
+    x = matrix(rows, cols, dtype, rows * 7 + cols, 0.3)
+    held = gpu(x, pad=5, shift=3)
+    view, buf = out_like(rows, cols, DT[out], pad=3, shift=1)
+    run(held, view, parts=parts)
+    want, seen = newton_schulz(f64(x))
+    p = parts or (2 if out == "f32" else 1)
+    tol = tolerance(seen, p, OUT[out], dtype == "bf16")
+    off = np.sqrt(((f64(view) - want) ** 2).sum())
+    print(f"{rows} x {cols} {dtype} -> {out}, {p} parts: off {off:.3e} of {tol:.3e}", flush=True)
+    assert off <= tol
+    assert untouched(view, buf)
+    assert np.array_equal(f64(held), f64(x))
+
+
+@pytest.mark.parametrize("rows,cols", [(2048, 2048), (1536, 4200), (4200, 1536), (2500, 640)])
+@pytest.mark.parametrize("parts", [1, 2])
+def test_large_tiles(rows, cols, parts):
+    """Sides at which the wider tiles are taken, the last of them partly outside."""
+    x = matrix(rows, cols, "bf16", 5).cuda()
+    got = run(x, torch.empty(rows, cols, device="cuda"), parts=parts).double()
+    y = x.double()
+    a, b, c = 3.4445, -4.7750, 2.0315
+    y = y / (y.square().sum().sqrt() + 1e-7)
+    y = y if rows <= cols else y.t().contiguous()
+    seen = [y]
+    for _ in range(5):
+        s = y @ y.t().contiguous()
+        y = a * y + (b * s + c * (s @ s)) @ y
+        seen.append(y)
+    off, tol = float((got - (y if rows <= cols else y.t())).norm()), tolerance(seen, parts, 2.0**-24, True, bound=True)
+    print(f"{rows} x {cols}, {parts} parts: off {off:.3e} of {tol:.3e}", flush=True)
+    assert off <= tol
+
+
+def test_other_coefficients_and_steps():
+    x = matrix(90, 200, "f32", 1)
+    for coefs, steps in (((1.5, -0.5, 0.0), 7), ((2.0, -1.5, 0.5), 4), ((3.4445, -4.7750, 2.0315), 1), ((15 / 8, -10 / 8, 3 / 8), 12)):
+        want, seen = newton_schulz(f64(x), steps, coefs)
+        got = run(x.cuda(), torch.empty(90, 200, device="cuda"), steps=steps, coefs=coefs, parts=2)
+        assert np.sqrt(((f64(got) - want) ** 2).sum()) <= tolerance(seen, 2, 2.0**-24, False, coefs)
+
+
+@pytest.mark.parametrize("scale", [1e-30, 1e-12, 1e12, 1e30])
+def test_any_scale_of_the_input(scale):
+    """The norm is a binary64 sum and the input is scaled by a power of two: squares that fp32 would lose or overflow do no harm (eps = 0)."""
+    x = torch.from_numpy((np.random.default_rng(2).normal(size=(70, 90)) * scale).astype(np.float32))
+    want, seen = newton_schulz(f64(x), eps=0.0)
+    got = run(x.cuda(), torch.empty(70, 90, device="cuda"), eps=0.0)
+    assert np.sqrt(((f64(got) - want) ** 2).sum()) <= tolerance(seen, 2, 2.0**-24, False)
+
+
+def test_zero_and_bad_values():
+    z = torch.zeros(70, 130, device="cuda")
+    for eps in (0.0, 1e-7):
+        assert not run(z, torch.full_like(z, 3.0), eps=eps).any()
+    for bad in (float("nan"), float("inf"), float("-inf")):
+        x = matrix(70, 130, "f32", 3).cuda()
+        x[5, 7] = bad
+        assert run(x, torch.zeros_like(x)).isnan().all()
+    x = matrix(70, 130, "f32", 3).cuda()
+    x[1, 1] = 2e38  # its square is beyond fp32, not beyond binary64
+    assert run(x, torch.zeros_like(x)).isfinite().all()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_in_place(dtype):
+    x = gpu(matrix(130, 200, dtype, 4), pad=7)
+    want = run(x, torch.empty(130, 200, dtype=DT[dtype], device="cuda"))
+    run(x, x)
+    assert torch.equal(x, want)
+
+
+def test_repeats_bit_for_bit_on_any_stream():
+    x = matrix(500, 700, "f32", 6).cuda()
+    want = run(x, torch.empty_like(x))
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        got = run(x, torch.empty_like(x))
+        other = run(x, torch.empty_like(x), stream=side)
+    side.synchronize()
+    assert torch.equal(want, got) and torch.equal(want, other)
+
+
+def test_replayed_graphs_that_share_a_workspace():
+    import paper_2608_22322_amd as al
+    from paper_2608_22322_amd import muon
+
+    a, b = matrix(300, 200, "bf16", 7).cuda(), matrix(100, 900, "f32", 8).cuda()
+    oa, ob = torch.empty_like(a), torch.empty_like(b)
+    ws = al.workspace(max(muon.orthogonalize_workspace_bytes(a, oa), muon.orthogonalize_workspace_bytes(b, ob)))
+    muon.orthogonalize(a, oa, ws)
+    muon.orthogonalize(b, ob, ws)
+    torch.cuda.synchronize()
+    graphs = []
+    for x, o in ((a, oa), (b, ob)):
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            muon.orthogonalize(x, o, ws)
+        graphs.append(g)
+    for seed in range(3):
+        a.copy_(matrix(300, 200, "bf16", 20 + seed))
+        b.copy_(matrix(100, 900, "f32", 30 + seed))
+        for g in graphs:
+            g.replay()
+        torch.cuda.synchronize()
+        ra, rb = oa.clone(), ob.clone()
+        assert torch.equal(run(a, torch.empty_like(a)), ra) and torch.equal(run(b, torch.empty_like(b)), rb)
+
+
+def test_nothing_to_do():
+    from paper_2608_22322_amd import muon
+
+    for shape in ((0, 5), (5, 0)):
+        x = torch.empty(shape, device="cuda")
+        muon.orthogonalize(x, torch.empty_like(x), None)
