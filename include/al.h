@@ -327,11 +327,11 @@ al_status al_apollo_step(const al_apollo_tensor* tensors, int32_t nt, const al_a
  * A zero matrix gives zeros (also with eps = 0), one that holds an infinity or a NaN gives NaN.
  * parts: what X, A and b A + c A A are held in between the products, whose
  * sums are fp32: 1 = one fp16 number each (11 bits: the result is about 1.4e-3 off for normal matrices, 3e-3 where singular values
- * fall as 1 / k), 2 = the sum of two (22 bits, 3e-7 and 5e-7; three products for one). |G| is a binary64 sum in a fixed order:
+ * fall as 1 / k), 2 = the sum of two (22 bits; 2e-6 to 3e-6, of the fp32 sums; three products for one). |G| is a binary64 sum in a fixed order:
  * every result repeats bit for bit.
  * a, b, c: for singular values of at most 1 to begin with, those of X must stay within 4 and those of b A + c A A within
  * 128 (AL_EINVAL; a = 3.4445, b = -4.7750, c = 2.0315 are usual). steps: 1 to 64.
- * rows, cols up to 2^21, the smaller of them up to 2^16 (AL_EUNSUPPORTED). */
+ * rows, cols up to 2^21, the smaller of them up to 2^16, 2^33 elements (AL_EUNSUPPORTED). */
 typedef struct al_ortho_cfg {
     double a, b, c, eps;
     int32_t steps, parts;
@@ -362,13 +362,14 @@ typedef struct al_muon_cfg {
 } al_muon_cfg;
 
 /* Workspace size (bytes) that al_muon_step needs for this tensor list and config. A part of a list never needs more than the list.
- * Tensors of one shape are stepped together, up to 64 of them and 2^26 elements at a time (one at least): an fp32 update of each, X twice and A and
- * b A + c A A, 2 or 4 bytes an element, sides padded to multiples of 64. */
+ * Up to 32 matrices of any shapes share launches, longest sides first, while they take no more than 2^30 bytes (one matrix at least): for each an fp32
+ * update or X twice, and A and b A + c A A, 2 or 4 bytes an element, sides padded to multiples of 64. */
 al_status al_muon_workspace_bytes(const al_tensor* tensors, int32_t nt, const al_muon_cfg* cfg, size_t* bytes);
 
 /* One step over nt matrices (rows, cols >= 1; a list's 1-D tensors, embedding and head take al_adamw_step). Uses per tensor: param, grad, m, m_meta;
- * the other slots must be NULL, and no two tensors may share memory. step: the 1-based step count, which the update does not depend on. Per shape: the momentum pass (which also sums the squares of u),
- * the norm, u into 16-bit parts, and three products a step of O, the last of which ends in the parameters. ws: device workspace
+ * the other slots must be NULL, and no two tensors may share memory. step: the 1-based step count, which the update does not depend on. m's codes are al_quantize's, but for values half way between
+ * two codes (the position is x fl(127 fl(1 / absmax)) in binary64 here). Per group: the momentum pass (which also sums the squares of u), u into 16-bit parts with its norm, and three
+ * products a step of O, the last of which ends in the parameters. ws: device workspace
  * of at least the queried size, 256-byte aligned. */
 al_status al_muon_step(const al_tensor* tensors, int32_t nt, const al_muon_cfg* cfg, int64_t step, void* ws, size_t ws_bytes, void* stream);
 
@@ -491,15 +492,16 @@ al_status al_linear_wgrad(int32_t dtype, const void* dy, int64_t lddy, const voi
 /* ------------------------------------------------------------------------
  * The two ends of a token model: the lookup of embeddings and its gradient,
  * and softmax cross entropy of a linear head with its gradients. Matrices as
- * for the activations above, except that a matrix of the products (w) has 16-byte
- * aligned rows of bf16; weight gradients are packed, in the types the optimizer steps read.
+ * for the activations above, except that the head's weight begins at a 16-byte
+ * aligned address; weight gradients are packed, in the types the optimizer steps read. scale: finite in fp32.
  *
  * Token ids and targets: tokens values of index_dtype, one behind the other. An
  * id or a target below 0 or from vocab on stands for no token: its embedding is zero, and it takes part in no loss and no
  * gradient, whatever its row holds.
  *
  * Sums are fp32 and independent of scheduling: every result repeats bit for
- * bit. tokens up to 2^31 - 1, vocab up to 2^31 - 1. */
+ * bit. tokens and vocab up to 2^31 - 1; with a gradient of the table vocab up to 2^26
+ * and ceil(tokens / 32) ceil(cols / 1024) up to 2^23 (AL_EUNSUPPORTED). */
 typedef enum al_index { AL_INDEX_I32 = 0, AL_INDEX_I64 = 1 } al_index;
 
 /* out[t] = scale table[ids[t]], in fp32, rounded once to out_dtype. table:
@@ -532,7 +534,8 @@ al_status al_linear_xent_workspace_bytes(int64_t tokens, int64_t hidden, int64_t
  * Products of bf16 numbers with fp32 sums; d is rounded to bf16 for a bf16 gradient and to the sum of two bf16 numbers (16 bits) for an fp32
  * one. Logits are taken once for the losses and, where a gradient is wanted, again, a piece of the vocabulary at a time: the workspace holds 2^26
  * elements of d (256 columns at least) and, with several pieces, dh in fp32. w: 16-byte aligned; ldw or hidden that is no multiple of 8 costs a copy of w in the
- * workspace. tokens * vocab up to 2^38, tokens * hidden and vocab * hidden up to 2^34, each of them up to 2^24 (AL_EUNSUPPORTED). */
+ * workspace. tokens * vocab up to 2^38, tokens * hidden and vocab * hidden up to 2^34, tokens and vocab
+ * up to 2^24, hidden up to 2^22 (AL_EUNSUPPORTED). */
 al_status al_linear_xent(const void* h, int64_t ldh, const void* w, int64_t ldw, int64_t tokens, int64_t hidden, int64_t vocab,
                          int32_t index_dtype, const void* target, const float* weight, double scale, float* loss, float* lse, int32_t dh_dtype, void* dh,
                          int64_t lddh, int32_t grad_dtype, const void* base, void* dw, void* ws, size_t ws_bytes, void* stream);

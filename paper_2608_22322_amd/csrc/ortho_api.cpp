@@ -51,7 +51,7 @@ al_status check_ortho(const al_ortho_cfg& k, const char* who) {
 
 al_status check_sides(int64_t rows, int64_t cols, const char* who) {
     if (rows < 0 || cols < 0) return fail(AL_EINVAL, "%s: negative shape", who);
-    if (std::max(rows, cols) > al::kOrthoLong || std::min(rows, cols) > al::kOrthoShort)
+    if (std::max(rows, cols) > al::kOrthoLong || std::min(rows, cols) > al::kOrthoShort || rows * cols > al::kOrthoMost)
         return fail(AL_EUNSUPPORTED, "%s: %lld x %lld is too large", who, (long long)rows, (long long)cols);
     return AL_OK;
 }

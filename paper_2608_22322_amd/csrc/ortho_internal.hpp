@@ -9,8 +9,8 @@
 
 namespace al {
 
-// Most rows and columns, and most on the shorter side (a product's tiles and offsets).
-constexpr int64_t kOrthoLong = int64_t(1) << 21, kOrthoShort = int64_t(1) << 16;
+// Most rows and columns, most on the shorter side and most elements (a product's tiles and offsets, the grids of the passes over a matrix).
+constexpr int64_t kOrthoLong = int64_t(1) << 21, kOrthoShort = int64_t(1) << 16, kOrthoMost = int64_t(1) << 33;
 
 // Matrices whose products share launches: at most kOrthoGroup, and at most kOrthoBytes of workspace where there are several.
 constexpr int kOrthoGroup = 32;

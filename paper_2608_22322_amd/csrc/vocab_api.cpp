@@ -10,7 +10,9 @@
 
 namespace {
 
-constexpr int64_t kMostIds = (int64_t(1) << 31) - 1, kMostSide = int64_t(1) << 24;
+// Most entries of a table that is looked up, of one with a gradient (a grid of rows), most tokens or entries and most features of a head (offsets inside a
+// tile's operands are 32 bits).
+constexpr int64_t kMostIds = (int64_t(1) << 31) - 1, kMostRowsOfGrad = int64_t(1) << 26, kMostSide = int64_t(1) << 24, kMostHidden = int64_t(1) << 22;
 
 al_status check_index(int32_t d, const char* who) {
     if (d != AL_INDEX_I32 && d != AL_INDEX_I64) return fail(AL_EINVAL, "%s: index_dtype %d", who, d);
@@ -37,17 +39,23 @@ al_status check_packed(const void* dw, const void* base, int64_t rows, int64_t c
     return AL_OK;
 }
 
-// What the rows of the table's gradient take: a grid of rows by 1024 columns.
-al_status check_rows(int64_t vocab, int64_t cols, const char* who) {
-    if ((cols + 1023) / 1024 > 65535) return fail(AL_EUNSUPPORTED, "%s: %lld columns are too many", who, (long long)cols);
-    (void)vocab;
+// The grids of the table's gradient: rows by 1024 columns, and a workgroup for every 32 tokens of 1024 columns, fewer than 2^23 of these.
+al_status check_grad(int64_t tokens, int64_t vocab, int64_t cols, const char* who) {
+    const int64_t slabs = (cols + 1023) / 1024;
+    if (vocab > kMostRowsOfGrad || slabs > 65535 || (slabs > 0 && tokens / 32 >= (int64_t(1) << 23) / slabs))
+        return fail(AL_EUNSUPPORTED, "%s: %lld tokens, a table of %lld x %lld are too large", who, (long long)tokens, (long long)vocab, (long long)cols);
+    return AL_OK;
+}
+
+al_status check_scale(double scale, const char* who) {
+    if (!std::isfinite((float)scale)) return fail(AL_EINVAL, "%s: scale must be finite in fp32", who);
     return AL_OK;
 }
 
 al_status check_xent(int64_t tokens, int64_t hidden, int64_t vocab, const char* who) {
     if (tokens < 0 || hidden < 0 || vocab < 0) return fail(AL_EINVAL, "%s: negative shape", who);
     constexpr int64_t most = int64_t(1) << 34;
-    if (tokens > kMostSide || hidden > kMostSide || vocab > kMostSide || tokens * vocab > (int64_t(1) << 38) || tokens * hidden > most || vocab * hidden > most)
+    if (tokens > kMostSide || hidden > kMostHidden || vocab > kMostSide || tokens * vocab > (int64_t(1) << 38) || tokens * hidden > most || vocab * hidden > most)
         return fail(AL_EUNSUPPORTED, "%s: %lld tokens, %lld features, a vocabulary of %lld are too large", who, (long long)tokens, (long long)hidden, (long long)vocab);
     if (hidden == 0 || vocab == 0) return fail(AL_EINVAL, "%s: no logits without features and a vocabulary", who);
     return AL_OK;
@@ -67,7 +75,7 @@ al_status al_embed_forward(int32_t table_dtype, const void* table, int64_t ldtab
     AL_TRY(check_dtype(out_dtype, who, "out_dtype"));
     AL_TRY(check_index(index_dtype, who));
     AL_TRY(check_sizes(tokens, vocab, cols, who));
-    if (!std::isfinite(scale)) return fail(AL_EINVAL, "%s: scale must be finite", who);
+    AL_TRY(check_scale(scale, who));
     if (tokens == 0 || cols == 0) return AL_OK;
     AL_TRY(check_ids(ids, index_dtype, who, "ids"));
     AL_TRY(check_mat(table, &ldtable, vocab, cols, table_dtype, vocab > 0, who, "table"));
@@ -82,7 +90,7 @@ al_status al_embed_backward_workspace_bytes(int64_t tokens, int64_t vocab, int64
     if (!bytes) return fail(AL_EINVAL, "%s: bytes is NULL", who);
     *bytes = 0;
     AL_TRY(check_sizes(tokens, vocab, cols, who));
-    AL_TRY(check_rows(vocab, cols, who));
+    AL_TRY(check_grad(tokens, vocab, cols, who));
     *bytes = al::embed_plan(tokens, vocab, cols).bytes;
     return AL_OK;
 }
@@ -95,8 +103,8 @@ al_status al_embed_backward(int32_t dtype, const void* dy, int64_t lddy, int32_t
     AL_TRY(check_dtype(grad_dtype, who, "grad_dtype"));
     AL_TRY(check_index(index_dtype, who));
     AL_TRY(check_sizes(tokens, vocab, cols, who));
-    AL_TRY(check_rows(vocab, cols, who));
-    if (!std::isfinite(scale)) return fail(AL_EINVAL, "%s: scale must be finite", who);
+    AL_TRY(check_grad(tokens, vocab, cols, who));
+    AL_TRY(check_scale(scale, who));
     if (vocab == 0 || cols == 0) return AL_OK;
     AL_TRY(check_packed(dw, base, vocab, cols, who));
     if (tokens > 0) {
@@ -147,7 +155,7 @@ al_status al_linear_xent(const void* h, int64_t ldh, const void* w, int64_t ldw,
     AL_TRY(check_dtype(dh_dtype, who, "dh_dtype"));
     AL_TRY(check_dtype(grad_dtype, who, "grad_dtype"));
     AL_TRY(check_index(index_dtype, who));
-    if (!std::isfinite(scale)) return fail(AL_EINVAL, "%s: scale must be finite", who);
+    AL_TRY(check_scale(scale, who));
     if (dw)
         AL_TRY(check_packed(dw, base, vocab, hidden, who));
     else if (base)
@@ -160,7 +168,6 @@ al_status al_linear_xent(const void* h, int64_t ldh, const void* w, int64_t ldw,
         a.cols = (int32_t)hidden;
         a.base = base;
         a.dw = dw;
-        AL_TRY(check_rows(vocab, hidden, who));
         return launched(al::launch_embed_backward(AL_DTYPE_BF16, grad_dtype, a, as_stream(stream)), who);
     }
     AL_TRY(check_mat(h, &ldh, tokens, hidden, AL_DTYPE_BF16, true, who, "h"));

@@ -44,7 +44,7 @@ hipError_t launch_embed_backward(int dtype, int grad_dtype, const EmbedBackward&
 struct XentPlan {
     int64_t tokens, hidden, vocab;
     int32_t tp, dp;        // tokens and hidden padded to multiples of 64
-    int32_t block;         // tokens a pass of the statistics
+    int32_t block, groups; // tokens a pass of the statistics, and the groups of columns that it leaves a row's statistics of
     int32_t piece;         // columns of the vocabulary a pass of the gradients
     int32_t parts, dh_parts, dw_parts;  // of the logits' gradients
     bool pack;             // w is copied into padded rows

@@ -257,8 +257,8 @@ XentPlan xent_plan(int64_t tokens, int64_t hidden, int64_t vocab, int64_t ldw, i
     };
     p.h_off = take((size_t)p.tp * p.dp * 2);
     p.w_off = take(p.pack ? (size_t)vocab * p.dp * 2 : 0);
-    const int64_t groups = (vocab + 31) / 32;  // (64 columns each but for the smallest tiles)
-    p.stat_off = take((size_t)p.block * groups * sizeof(Stat) + (size_t)p.block * 4);
+    p.groups = (int32_t)((vocab + wave_columns(p.logits.tile) - 1) / wave_columns(p.logits.tile));
+    p.stat_off = take((size_t)p.block * p.groups * sizeof(Stat) + (size_t)p.block * 4);
     if (p.parts) {
         const int64_t room = (int64_t(1) << 26) / p.tp / 256 * 256;
         p.piece = (int32_t)std::min<int64_t>((vocab + 63) / 64 * 64, std::max<int64_t>(256, room));
@@ -294,8 +294,7 @@ hipError_t launch_xent(const XentPlan& p, const Xent& a, void* ws, hipStream_t s
     Mm q = {};
     q.part = reinterpret_cast<float*>(base + p.part_off);
     hipError_t e;
-    const int32_t groups = (int32_t)((p.vocab + wave_columns(p.logits.tile) - 1) / wave_columns(p.logits.tile));
-    float* const at = reinterpret_cast<float*>(stats + (size_t)p.block * groups);
+    float* const at = reinterpret_cast<float*>(stats + (size_t)p.block * p.groups);
     for (int64_t t0 = 0; t0 < p.tokens; t0 += p.block) {
         const int32_t padded = (int32_t)std::min<int64_t>(p.block, p.tp - t0), n = (int32_t)std::min<int64_t>(p.block, p.tokens - t0);
         Mm g = q;
@@ -306,9 +305,9 @@ hipError_t launch_xent(const XentPlan& p, const Xent& a, void* ws, hipStream_t s
         g.m = n;
         g.n = (int32_t)p.vocab;
         g.turns = p.dp / kMmTurn;
-        const EndStats end = {stats, at, a.target, t0, n, (int32_t)p.vocab, groups};
+        const EndStats end = {stats, at, a.target, t0, n, (int32_t)p.vocab, p.groups};
         if ((e = product<true, true, true, 1>(p.logits, g, end, st)) != hipSuccess) return e;
-        loss_kernel<<<(uint32_t)((padded + 3) / 4), 256, 0, st>>>(stats, at, groups, t0, n, padded, p.vocab, a.target, a.weight, a.scale, a.loss, a.lse, lse, coef);
+        loss_kernel<<<(uint32_t)((padded + 3) / 4), 256, 0, st>>>(stats, at, p.groups, t0, n, padded, p.vocab, a.target, a.weight, a.scale, a.loss, a.lse, lse, coef);
     }
     if (!p.parts) return hipGetLastError();
     uint16_t* const d = reinterpret_cast<uint16_t*>(base + p.d_off);
