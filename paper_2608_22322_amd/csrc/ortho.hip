@@ -165,15 +165,32 @@ struct Held {
 };
 
 // The products of a step: A = X X^T, B = b A + c A A, and a X + B X as the next X, the result, or a step of the parameters.
+//
+// Two steps at once: what multiplies X is a polynomial of A, and so is the next step's A. With M = a I + B, which commutes with A,
+//   A' = M A M,  B' = b A' + c A' A',  X'' = (a I + B') M X = a a X + D X,  D = a B + a B' + B' B:
+// the next step's A by Y = M A = a A + B A and A' = Y M = a Y + Y B, and no X in between. Three more products of symmetric matrices (half of each is
+// computed) for one of X with its transpose and one with X, which is less work where X is long. Each pair starts anew from its X: in fp16 parts the singular
+// values that A holds badly, those far below the largest, grow by 3.4 a step, and over two steps that costs little (two parts, 1024 x 2816: 3.3e-6 for 3.1e-6 off in
+// the Frobenius norm; three steps 5.6e-6, five on values falling as 1 / k 1e-4).
 enum Kind : int { kGram, kPoly, kNext, kOut, kStep };
+
+// A product of two symmetric matrices of an item: out = sum factor + one c1 + two c2 (c2 = 0: without). The numbers are the matrices' places.
+struct Square {
+    int32_t a, b, one, two, out;
+    float factor, c1, c2;
+};
 __host__ __device__ constexpr bool square_kind(int kind) { return kind == kGram || kind == kPoly; }
 
 struct OrthoLaunch {
     OrthoItem it[kOrthoGroup];
     int64_t begin[kOrthoGroup + 1];  // first tile of each item, or, with slots, first turn
-    int64_t slots;                   // workgroups that the turns are dealt out to; 0: a tile a workgroup
+    int64_t slots;                   // workgroups that the turns are dealt out to; 0: a tile a workgroup, or a piece of one:
+    uint32_t whole;                  // tiles that are taken whole
+    uint32_t rest, split;            // the tiles behind them, each in so many pieces
     int32_t count, parts, from, first;  // from: which place X is in; first: the first step
-    float ca, cb, cc;
+    int32_t by;                          // which square matrix X is multiplied with, and
+    float ca;                            // the multiple of X that is added
+    Square square;
     const Norm* norms;
     float* part;  // [2 slots][a tile in the lanes' order]
     double decay;
@@ -201,13 +218,16 @@ struct Task {
     int item;
     bool tall;
     int32_t dp;
-    Held x, g, b;
+    Held x;
+    // the item's square matrices
+    __device__ __forceinline__ Held square(int i) const {
+        const int64_t n = (int64_t)dp * dp;
+        return {t.a + i * a.parts * n, n, dp, a.parts};
+    }
     __device__ __forceinline__ Task(const OrthoLaunch& l, int i) : a(l), t(l.it[i]), item(i) {
         tall = t.rp > t.cp || (t.rp == t.cp && t.rows > t.cols);
         dp = min(t.rp, t.cp);
         x = {a.from ? t.x[1] : t.x[0], (int64_t)t.rp * t.cp, t.cp, a.parts};
-        g = {t.a, (int64_t)dp * dp, dp, a.parts};
-        b = {t.a + a.parts * g.size, g.size, dp, a.parts};
     }
     template <int B>
     __device__ __forceinline__ Mm product() const {
@@ -222,22 +242,23 @@ struct Task {
         p.n = square_kind(KIND) ? dp : t.cp;
         p.turns = item_turns(t, KIND);
         const MmOperand ox = x.operand(t.rp);
-        p.a = KIND == kGram ? ox : KIND == kPoly ? g.operand(dp) : tall ? ox : b.operand(dp);
-        p.b = KIND == kGram ? ox : KIND == kPoly ? g.operand(dp) : tall ? b.operand(dp) : ox;
+        p.a = KIND == kGram ? ox : KIND == kPoly ? square(a.square.a).operand(dp) : tall ? ox : square(a.by).operand(dp);
+        p.b = KIND == kGram ? ox : KIND == kPoly ? square(a.square.b).operand(dp) : tall ? square(a.by).operand(dp) : ox;
         return p;
     }
-    // What the product is combined with: sum * factor() + from() * other(), and that times after().
-    __device__ __forceinline__ const Held& from() const { return KIND == kPoly ? g : x; }
+    // What the product is combined with: sum * factor() + one() * other() + two() * second(), and that times after().
+    __device__ __forceinline__ Held one() const { return KIND == kPoly ? square(a.square.one) : x; }
+    __device__ __forceinline__ Held two() const { return square(a.square.two); }
     __device__ __forceinline__ float factor() const {
-        return KIND == kGram ? kAScale / (kXScale * kXScale) * (a.first ? a.norms[item].inv2 : 1.0f)
-                             : KIND == kPoly ? a.cc * (kBScale / (kAScale * kAScale)) : 1.0f / kBScale;
+        return KIND == kGram ? kAScale / (kXScale * kXScale) * (a.first ? a.norms[item].inv2 : 1.0f) : KIND == kPoly ? a.square.factor : 1.0f / kBScale;
     }
-    __device__ __forceinline__ float other() const { return KIND == kPoly ? a.cb * (kBScale / kAScale) : a.ca; }
+    __device__ __forceinline__ float other() const { return KIND == kPoly ? a.square.c1 : a.ca; }
+    __device__ __forceinline__ float second() const { return KIND == kPoly ? a.square.c2 : 0.0f; }
     __device__ __forceinline__ float after() const { return !square_kind(KIND) && a.first ? a.norms[item].inv : 1.0f; }
     // where it goes, for what stays in the workspace
     __device__ __forceinline__ Held to() const {
-        if (KIND == kGram) return g;
-        if (KIND == kPoly) return b;
+        if (KIND == kGram) return square(0);
+        if (KIND == kPoly) return square(a.square.out);
         return {a.from ? t.x[0] : t.x[1], x.size, x.ld, a.parts};
     }
     __device__ __forceinline__ int32_t rows() const { return square_kind(KIND) ? dp : t.rp; }
@@ -286,7 +307,8 @@ struct Task {
     __device__ __forceinline__ void end(int m, int n, f32x4 v, bool mirror) const {
         if (m >= rows() || n >= cols()) return;
         v *= factor();
-        if constexpr (KIND != kGram) v += from().get(m, n) * other();
+        if constexpr (KIND != kGram) v += one().get(m, n) * other();
+        if (KIND == kPoly && second() != 0.0f) v += two().get(m, n) * second();
         v *= after();
         if constexpr (KIND == kOut || KIND == kStep)
             write(m, n, v);
@@ -405,12 +427,15 @@ __device__ __forceinline__ void finish(const Task<KIND>& task, int m0, int n0, c
     const int parts = task.a.parts, m = task.rows(), n = task.cols();
     each([&](f32x4& v) { v *= factor; });
     if constexpr (KIND != kGram) {
-        const Held& f = task.from();
+        const int32_t added = parts * (task.second() != 0.0f ? 2 : 1);
 #pragma unroll 1
-        for (int p = 0; p < parts; ++p) {
-            image.load(tid, f.p + p * f.size, f.ld, m0, n0, m, n);
+        for (int p = 0; p < added; ++p) {
+            const bool first = p < parts;
+            const Held f = first ? task.one() : task.two();
+            const float by = first ? other : task.second();
+            image.load(tid, f.p + (first ? p : p - parts) * f.size, f.ld, m0, n0, m, n);
             __syncthreads();
-            image.quads(r, c, acc, [&](f32x4& v, auto q) { v += __builtin_convertvector((f16x4)*q, f32x4) * other; });
+            image.quads(r, c, acc, [&](f32x4& v, auto q) { v += __builtin_convertvector((f16x4)*q, f32x4) * by; });
             __syncthreads();
         }
         each([&](f32x4& v) { v *= after; });
@@ -457,7 +482,7 @@ __device__ __forceinline__ int item_at(const OrthoLaunch& a, int64_t pos) {
 // Turns t0 .. t1 of a tile, and its end or, where that is not all of it, its partial sums.
 template <int B, int KIND, int PARTS>
 using PlacesOf = MmPlaces<PARTS, PARTS, mm_stages<B, PARTS, PARTS>()>;
-template <int B, int KIND, int PARTS, bool TALL>
+template <int B, int KIND, int PARTS, bool PIECE, bool TALL>
 __device__ __forceinline__ void segment(const Task<KIND>& task, int tile, int t0, int t1, int64_t place, const PlacesOf<B, KIND, PARTS>& at) {
     typedef MmTile<B> G;
     const Mm p = task.template product<B>();
@@ -465,7 +490,7 @@ __device__ __forceinline__ void segment(const Task<KIND>& task, int tile, int t0
     MmAcc acc[G::FM][G::FN] = {};
     constexpr bool kRows = KIND == kPoly || (KIND == kGram ? !TALL : true), kCols = KIND == kPoly || (KIND == kGram ? !TALL : TALL);  // k along the rows
     MmCore<f16, B, kRows, kCols, false, PARTS, PARTS>::run(p, id.m * B, id.n * B, t0, t1, at, acc);
-    if (t1 - t0 < p.turns * p.segs) {
+    if (PIECE || t1 - t0 < p.turns * p.segs) {
         const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
         f32x4* const part = reinterpret_cast<f32x4*>(task.a.part) + (place * G::kWaves + w) * (G::FM * G::FN * 64) + lane;
 #pragma unroll
@@ -477,12 +502,12 @@ __device__ __forceinline__ void segment(const Task<KIND>& task, int tile, int t0
         finish<B, KIND>(task, id.m * B, id.n * B, Image<B>(at.a[0][0], at.a[1][0], at.b[0][0], at.b[1][0]), acc);
     }
 }
-template <int B, int KIND, int PARTS>
+template <int B, int KIND, int PARTS, bool PIECE = false>
 __device__ __forceinline__ void segment(const Task<KIND>& task, int tile, int t0, int t1, int64_t place, const PlacesOf<B, KIND, PARTS>& at) {
     if (KIND != kPoly && task.tall)
-        segment<B, KIND, PARTS, true>(task, tile, t0, t1, place, at);
+        segment<B, KIND, PARTS, PIECE, true>(task, tile, t0, t1, place, at);
     else
-        segment<B, KIND, PARTS, false>(task, tile, t0, t1, place, at);
+        segment<B, KIND, PARTS, PIECE, false>(task, tile, t0, t1, place, at);
 }
 
 template <int B, int KIND, int PARTS>
@@ -494,13 +519,26 @@ __global__ __launch_bounds__(MmTile<B>::kThreads, 2) void ortho_kernel(OrthoLaun
     uint32_t k = blockIdx.x >> 3, tile = 0;
     int i = 0;
     for (; i < a.count; ++i) {
-        const uint32_t n = (uint32_t)(a.begin[i + 1] - a.begin[i]), x = (blockIdx.x + (uint32_t)i) & 7u, per = n >> 3, rest = n & 7u, mine = per + (x < rest ? 1u : 0u);
+        const uint32_t n = (uint32_t)(min(a.begin[i + 1], (int64_t)a.whole) - min(a.begin[i], (int64_t)a.whole)), x = (blockIdx.x + (uint32_t)i) & 7u, per = n >> 3,
+                       rest = n & 7u, mine = per + (x < rest ? 1u : 0u);
         tile = x * per + min(x, rest) + k;
         if (k < mine) break;
         k -= mine;
     }
     if (i == a.count) return;
     segment<B, KIND, PARTS>(Task<KIND>(a, i), (int32_t)tile, 0, item_turns(a.it[i], KIND) * item_segments(B, a.parts), 0, places);
+}
+
+// The pieces of the tiles behind the whole ones, those at one place of k neighbours.
+template <int B, int KIND, int PARTS>
+__global__ __launch_bounds__(MmTile<B>::kThreads, 2) void ortho_pieces_kernel(OrthoLaunch a) {
+    constexpr int PA = PARTS, PB = PARTS;
+    MM_PLACES(B, PA, PB, places);
+    const uint32_t piece = blockIdx.x / a.rest, tile = a.whole + blockIdx.x - piece * a.rest;
+    const int i = item_at(a, tile);
+    const uint64_t turns = (uint64_t)(item_turns(a.it[i], KIND) * item_segments(B, a.parts));
+    segment<B, KIND, PARTS, true>(Task<KIND>(a, i), (int32_t)(tile - a.begin[i]), __builtin_amdgcn_readfirstlane((int32_t)(piece * turns / a.split)),
+                                  __builtin_amdgcn_readfirstlane((int32_t)((piece + 1) * turns / a.split)), blockIdx.x, places);
 }
 
 // The turns dealt out to slots. (Kernels of their own: the loop over a slot's tiles takes registers that 256-wide tiles do not have.)
@@ -555,8 +593,36 @@ __global__ __launch_bounds__(256) void ortho_join_kernel(OrthoLaunch a) {
              p.sym && id.m != id.n);
 }
 
+// The tiles that were taken in pieces.
+template <int B, int KIND>
+__global__ __launch_bounds__(256) void ortho_sum_kernel(OrthoLaunch a) {
+    typedef MmTile<B> G;
+    constexpr uint32_t kBlocks = B * B / 1024;
+    const uint32_t r = blockIdx.x / kBlocks;
+    const int i = item_at(a, a.whole + r);
+    const Task<KIND> task(a, i);
+    const uint32_t at = blockIdx.x % kBlocks * 256 + threadIdx.x, lane = at & 63, slot = at >> 6;
+    const f32x4* const part = reinterpret_cast<const f32x4*>(a.part) + at;
+    constexpr int64_t kTile = B * B / 4;
+    f32x4 v = {};
+    for (uint32_t h = 0; h < a.split; h += 8) {
+        f32x4 q[8];
+#pragma unroll
+        for (uint32_t j = 0; j < 8; ++j)
+            if (h + j < a.split) q[j] = part[((int64_t)(h + j) * a.rest + r) * kTile];
+#pragma unroll
+        for (uint32_t j = 0; j < 8; ++j)
+            if (h + j < a.split) v += q[j];
+    }
+    const Mm p = task.template product<B>();
+    const MmAt id = mm_at<B>(p, (uint32_t)(a.whole + r - a.begin[i]));
+    const uint32_t w = slot / (G::FM * G::FN), q = slot % (G::FM * G::FN);
+    task.end(id.m * B + G::wave_m((int)w) + (int)(lane & 15) + 16 * (int)(q / G::FN), id.n * B + G::wave_n((int)w) + 4 * (int)(lane >> 4) + 16 * (int)(q % G::FN), v,
+             p.sym && id.m != id.n);
+}
+
 template <int B, int KIND, int PARTS>
-hipError_t launch(const OrthoLaunch& a, hipStream_t st) {
+hipError_t launch(OrthoLaunch& a, hipStream_t st) {
     if constexpr (B < 256) {
         if (a.slots) {
             ortho_slots_kernel<B, KIND, PARTS><<<(uint32_t)a.slots, MmTile<B>::kThreads, 0, st>>>(a);
@@ -564,20 +630,32 @@ hipError_t launch(const OrthoLaunch& a, hipStream_t st) {
             return hipGetLastError();
         }
     }
+    a.whole = (uint32_t)a.begin[a.count] - a.rest;
     uint32_t most = 0;  // of an XCD
-    for (int i = 0; i < a.count; ++i) most += (uint32_t)((a.begin[i + 1] - a.begin[i] + 7) / 8);
-    ortho_kernel<B, KIND, PARTS><<<8 * most, MmTile<B>::kThreads, 0, st>>>(a);
+    for (int i = 0; i < a.count; ++i) most += (uint32_t)((std::min<int64_t>(a.begin[i + 1], a.whole) - std::min<int64_t>(a.begin[i], a.whole) + 7) / 8);
+    if (most) ortho_kernel<B, KIND, PARTS><<<8 * most, MmTile<B>::kThreads, 0, st>>>(a);
+    if (a.rest) {
+        ortho_pieces_kernel<B, KIND, PARTS><<<a.rest * a.split, MmTile<B>::kThreads, 0, st>>>(a);
+        ortho_sum_kernel<B, KIND><<<a.rest * (B * B / 1024), 256, 0, st>>>(a);
+    }
     return hipGetLastError();
 }
 
 // How a group's product is cut: the tile and, where that is faster by the measured times, the slots that its turns are dealt out to. Slots that work at different places of k
 // share little of what they load: whole tiles run in step and find their neighbours' loads in the L2. What dealing out is for is few tiles and a long sum.
+// Tiles of one length that are some rounds of the device and a few more: the rounds are taken whole, the rest in pieces, up to three rounds of them (4096 x 11008, A: 136
+// tiles of 256, half of a round, 269 us, 528 of 128, of which 16 in 32 pieces each, 221; B 115 and 98).
 struct Cut {
     int32_t tile;
     int64_t slots;
+    uint32_t rest, split;
+    double us;
 };
+// What partial sums may take, in elements: slots leave at most two tiles each, pieces one.
+constexpr int64_t kPartials = 512 * 2 * 128 * 128;
+
 Cut group_cut(const OrthoLaunch& a, int kind) {
-    Cut best = {64, 0};
+    Cut best = {64, 0, 0, 0, 0};
     double least = -1, bytes = 0;  // bytes: of the operands
     for (int i = 0; i < a.count; ++i) {
         const double x = (double)a.it[i].rp * a.it[i].cp, d = (double)std::min(a.it[i].rp, a.it[i].cp);
@@ -600,13 +678,23 @@ Cut group_cut(const OrthoLaunch& a, int kind) {
         const double mean = (double)turns / (double)tiles;  // turns of all segments
         // tiles of different lengths: the longest begin first
         const double whole = same ? mm_time(tile, tiles, most, parts) : std::max(mm_time(tile, 1, most, parts), mm_time(tile, tiles, (int64_t)std::ceil(mean / segs), parts));
-        if (least < 0 || whole < least) least = whole, best = {tile, 0};
+        if (least < 0 || whole < least) least = whole, best = {tile, 0, 0, 0, whole};
+        const int64_t round = 256 * mm_fit(tile, parts), rest = tiles % round;
+        const double n = (double)most * segs;
+        if (same && rest > 0)
+            for (const int64_t rounds : {1, 2, 3}) {
+                const int64_t split = std::min<int64_t>(rounds * round / rest, segs * most / (tile > 128 ? 8 : 4)), pieces = rest * split;
+                if (split < 2 || pieces * tile * tile > kPartials) break;
+                const double t = mm_time(tile, tiles - rest, most, parts) + (double)rounds * (mm_ends(tile, std::min(pieces, round), parts) + std::ceil(n / (double)split) * mm_turn(tile, std::min(pieces, round), parts)) +
+                                 9 + (double)(pieces * tile * tile) * 4 / 4e6;
+                if (t < least) least = t, best = {tile, 0, (uint32_t)rest, (uint32_t)split, t};
+            }
         for (const int64_t slots : {16, 32, 64, 128, 256, 512}) {
             if (tile == 256 || slots > 256 * mm_fit(tile, parts) || turns < 4 * slots) break;
             const double turn = std::max(mm_turn(tile, slots, parts), (double)(slots * tile * 128 * (segs > 1 ? 2 : parts)) / rate), w = (double)turns / (double)slots,
                          pieces = std::min((double)(2 * slots), (double)(slots + tiles)),
                          t = 2 + w * turn + (w / mean + 1) * (mm_ends(tile, slots, parts) + 1) + 5 + pieces * tile * tile * 4 / 4e6;
-            if (t < least) least = t, best = {tile, slots};
+            if (t < least) least = t, best = {tile, slots, 0, 0, t};
         }
     }
     return best;
@@ -616,6 +704,8 @@ template <int KIND>
 hipError_t product(OrthoLaunch& a, hipStream_t st) {
     const Cut c = group_cut(a, KIND);
     a.slots = c.slots;
+    a.rest = c.rest;
+    a.split = c.split;
     a.begin[0] = 0;
     for (int i = 0; i < a.count; ++i)
         a.begin[i + 1] = a.begin[i] + item_tiles(a.it[i], KIND, c.tile) * (c.slots ? item_turns(a.it[i], KIND) * item_segments(c.tile, a.parts) : 1);
@@ -623,20 +713,43 @@ hipError_t product(OrthoLaunch& a, hipStream_t st) {
     return c.tile == 256 ? launch<256, KIND, 1>(a, st) : launch<128, KIND, 1>(a, st);
 }
 
+// Whether a group's steps are taken two at a time: three products of square matrices against X X^T and one with X, where the measured times say that this saves 25 us
+// a pair (4096 x 11008 in one part: 3 x 98 us against 602; in two parts three matrices of 2048 x 5632, two of 2048 x 2048 and two small ones: 3 x 187
+// against 931. 1001 x 1750 in two parts: 3 x 17 against 42; the ends of small products take longer than the times say).
+bool in_pairs(const OrthoLaunch& a, const OrthoCoefs& k) {
+    return k.pairs && k.steps > 1 && group_cut(a, kGram).us + group_cut(a, kNext).us > 3 * group_cut(a, kPoly).us + 25;
+}
+
 // The steps of a group whose X0 lies in place 1; the last one's outputs go where LAST says.
 template <int LAST>
 hipError_t iterate(OrthoLaunch& a, const OrthoCoefs& k, hipStream_t st) {
     a.parts = k.parts;
-    a.ca = k.a;
-    a.cb = k.b;
-    a.cc = k.c;
-    for (int i = 0; i < k.steps; ++i) {
-        a.from = (i & 1) ^ 1;
-        a.first = i == 0;
+    constexpr float kA = kAScale, kB = kBScale;
+    const Square poly = {0, 0, 0, 0, 1, k.c * (kB / (kA * kA)), k.b * (kB / kA), 0};
+    const Square pair[5] = {
+        poly,                                                               // B, at 1
+        {1, 0, 0, 0, 2, 1 / kB, k.a, 0},                                    // Y = a A + B A, at 2
+        {2, 1, 2, 0, 0, 1 / kB, k.a, 0},                                    // A' = a Y + Y B, at 0
+        {0, 0, 0, 0, 2, k.c * (kB / (kA * kA)), k.b * (kB / kA), 0},        // B', at 2
+        {2, 1, 1, 2, 0, 1 / kB, k.a, k.a},                                  // D = a B + a B' + B' B, at 0
+    };
+    const bool pairs = in_pairs(a, k);
+    a.from = 1;
+    a.first = 1;
+    for (int i = 0; i < k.steps;) {
+        const bool two = pairs && i + 1 < k.steps;
         hipError_t e = product<kGram>(a, st);
-        if (e == hipSuccess) e = product<kPoly>(a, st);
-        if (e == hipSuccess) e = i + 1 < k.steps ? product<kNext>(a, st) : product<LAST>(a, st);
+        for (int j = 0; j < (two ? 5 : 1) && e == hipSuccess; ++j) {
+            a.square = two ? pair[j] : poly;
+            e = product<kPoly>(a, st);
+        }
+        a.by = two ? 0 : 1;
+        a.ca = two ? k.a * k.a : k.a;
+        i += two ? 2 : 1;
+        if (e == hipSuccess) e = i < k.steps ? product<kNext>(a, st) : product<LAST>(a, st);
         if (e != hipSuccess) return e;
+        a.from ^= 1;
+        a.first = 0;
     }
     return hipSuccess;
 }
@@ -658,7 +771,7 @@ char* place(OrthoItem& t, int64_t rows, int64_t cols, int32_t parts, bool update
     at += up((size_t)t.rp * t.cp * 2 * parts);
     t.a = reinterpret_cast<uint16_t*>(at);
     const size_t d = (size_t)std::min(t.rp, t.cp);
-    return at + up(d * d * 2 * parts * 2);
+    return at + up(d * d * 2 * parts * 3);
 }
 
 }  // namespace
@@ -675,8 +788,8 @@ int64_t ortho_turns(int64_t rows, int64_t cols, int32_t parts) {
     return std::max(d * (d + 1) / 2 * std::max(r, c), r * c * d) * (parts > 1 ? 3 : 1);
 }
 
-// A slot has at least 4 turns and leaves at most two tiles of sums; 512 slots of 128 x 128 outputs leave the most.
-size_t ortho_part_bytes(int64_t turns) { return (size_t)std::min<int64_t>(512, turns / 4) * 2 * 128 * 128 * 4; }
+// A slot has at least 4 turns and leaves at most two tiles of sums of 128 x 128 outputs at most, a piece has 4 of those and leaves one, or 8 of 256 x 256 outputs.
+size_t ortho_part_bytes(int64_t turns) { return (size_t)std::min<int64_t>(kPartials, turns / 4 * 2 * 128 * 128) * 4; }
 
 size_t ortho_part_bytes(int64_t rows, int64_t cols, int32_t parts) {
     OrthoLaunch a;
@@ -687,7 +800,7 @@ size_t ortho_part_bytes(int64_t rows, int64_t cols, int32_t parts) {
     size_t most = 0;
     for (const int kind : {kGram, kPoly, kNext}) {
         const Cut c = group_cut(a, kind);
-        most = std::max(most, (size_t)c.slots * 2 * c.tile * c.tile * 4);
+        most = std::max(most, ((size_t)c.slots * 2 + (size_t)c.rest * c.split) * c.tile * c.tile * 4);
     }
     return most;
 }

@@ -16,7 +16,7 @@ constexpr int kMostSteps = 64;
 constexpr double kMostSigma = 4.0, kMostPoly = 128.0;  // what fp16 holds of X, A and b A + c A A at their scales
 
 // The coefficients, followed over the steps: the largest singular value of X (t = its square) and of b A + c A A.
-al_status check_ortho(const al_ortho_cfg& k, const char* who) {
+al_status check_ortho(const al_ortho_cfg& k, const char* who, double* largest = nullptr) {
     if (!std::isfinite(k.a) || !std::isfinite(k.b) || !std::isfinite(k.c) || !std::isfinite(k.eps) || k.eps < 0)
         return fail(AL_EINVAL, "%s: coefficients or eps out of range", who);
     if (k.steps < 1 || k.steps > kMostSteps) return fail(AL_EINVAL, "%s: steps %d must be 1 to %d", who, k.steps, kMostSteps);
@@ -44,6 +44,7 @@ al_status check_ortho(const al_ortho_cfg& k, const char* who) {
         if (!(next <= kMostSigma) || !(poly <= kMostPoly))
             return fail(AL_EINVAL, "%s: step %d of these coefficients takes singular values to %g, those of b A + c A A to %g (at most %g and %g)", who, i + 1, next, poly,
                         kMostSigma, kMostPoly);
+        if (largest) *largest = std::max(*largest, poly);
         top = std::max(next, 1e-6);
     }
     return AL_OK;
@@ -56,7 +57,13 @@ al_status check_sides(int64_t rows, int64_t cols, const char* who) {
     return AL_OK;
 }
 
-al::OrthoCoefs coefs(const al_ortho_cfg& k) { return {(float)k.a, (float)k.b, (float)k.c, k.eps, k.steps, k.parts}; }
+// Two steps at once hold (a I + B') (a I + B) - a a I as they hold B.
+al::OrthoCoefs coefs(const al_ortho_cfg& k) {
+    double poly = 0;
+    (void)check_ortho(k, "", &poly);
+    const double m = std::fabs(k.a) + poly;
+    return {(float)k.a, (float)k.b, (float)k.c, k.eps, k.steps, k.parts, m * m + k.a * k.a <= 200.0};
+}
 
 bool aligned16(const void* p) { return (at(p) & 15u) == 0; }
 

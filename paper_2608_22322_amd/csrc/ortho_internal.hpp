@@ -17,7 +17,7 @@ constexpr int kOrthoGroup = 32;
 constexpr size_t kOrthoBytes = size_t(1) << 30;
 
 // One matrix, held padded with zeros to rp x cp (multiples of 64) as one 16-bit part or the sum of two: X in two places in turn, A = X X^T (or
-// X^T X) and B = b A + c A A behind it.
+// X^T X) and B = b A + c A A behind it, and a third place for two steps at once.
 struct OrthoItem {
     uint16_t *x[2], *a;
     float* p;     // al_muon_step: the parameters, and lr times the shape's scale
@@ -42,6 +42,7 @@ struct OrthoCoefs {
     float a, b, c;
     double eps;
     int32_t steps, parts;
+    int32_t pairs;  // two steps at once stay within what fp16 holds
 };
 
 // One matrix x (dtype) -> out (out_dtype). ws: ortho_head_bytes, ortho_part_bytes and ortho_item_bytes.

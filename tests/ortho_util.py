@@ -25,8 +25,8 @@ def newton_schulz(x, steps=5, coefs=COEFS, eps=1e-7):
 def tolerance(seen, parts, out_unit, exact_start, coefs=COEFS, bound=False):
     """Frobenius norm of the error allowed to the last X, from the X of every step.
 
-    u: half a step of what is held between the products, relative to it: 2^-11 for one fp16 part; 2^-22 for the sum of two (the second holds the first's error to 2^-11 of
-    itself, and the dropped product of two second parts is another 2^-22). s: sums of K products in fp32, at most (K / 32 + 5) 2^-24 of the sum of magnitudes, taken as the
+    u: half a step of what is held between the products, relative to it: 2^-11 for one fp16 part; 2^-21 for the sum of two (the second holds the first's error to 2^-11 of
+    itself, 2^-22, and the dropped product of two second parts is another 2^-22). s: sums of K products in fp32, at most (K / 32 + 5) 2^-24 of the sum of magnitudes, taken as the
     product of Frobenius norms (K / 32 matrix instructions one after the other, 5 levels inside one).
     A step maps an error e of X to at most L e, L the largest |f'| for f(t) = a t + b t^3 + c t^5 over the singular values, and adds (F: Frobenius, S: spectral norm)
       of X, rounded:        L u F(X)   (not for the first X where it is held exactly)
@@ -52,3 +52,39 @@ def tolerance(seen, parts, out_unit, exact_start, coefs=COEFS, bound=False):
         e += (u + s) * f(x) ** 2 * (abs(b) + 2 * abs(c) * s_x**2) * s_x
         e += (u * f(poly) + abs(c) * s * f(gram) ** 2) * s_x + s * f(poly) * f(x) + 2 * 2.0**-24 * f(seen[i + 1])
     return 1.1 * e + out_unit * f(seen[-1])
+
+
+def _held(x, scale, parts):
+    y = x * scale
+    hi = y.half().float()
+    if parts > 1:
+        hi = hi + (y - hi).half().float()
+    return hi / scale
+
+
+def rounded(x, parts, pairs=False, steps=5, coefs=COEFS):
+    """The same steps in fp32 with every matrix between the products rounded to the parts that hold it (X, A times 2^10, B times 2^8), one at a time or in pairs that
+    leave X out: M = a I + B, A' = M A M, X'' = (a I + B') M X. A torch matrix, rows <= cols."""
+    import torch
+
+    a, b, c = coefs
+    half = lambda m: torch.tril(m) + torch.tril(m, -1).t()  # noqa: E731
+    mm = lambda p, q: p @ q.contiguous()  # noqa: E731
+    x = _held((x.double() / x.double().norm()).float(), 1024.0, parts)
+    i = 0
+    while i < steps:
+        gram = _held(half(mm(x, x.t())), 1024.0, parts)
+        poly = _held(half(b * gram + c * mm(gram, gram)), 256.0, parts)
+        if pairs and i + 1 < steps:
+            y = _held(half(a * gram + mm(poly, gram)), 1024.0, parts)
+            gram = _held(half(a * y + mm(y, poly)), 1024.0, parts)
+            nxt = _held(half(b * gram + c * mm(gram, gram)), 256.0, parts)
+            both = _held(half(a * poly + a * nxt + mm(nxt, poly)), 256.0, parts)
+            x = a * a * x + mm(both, x)
+            i += 2
+        else:
+            x = a * x + mm(poly, x)
+            i += 1
+        if i < steps:
+            x = _held(x, 1024.0, parts)
+    return x

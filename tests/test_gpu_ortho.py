@@ -4,7 +4,7 @@ import pytest
 import torch
 
 from tests.act_util import DT, f64, gpu, out_like, untouched
-from tests.ortho_util import newton_schulz, tolerance
+from tests.ortho_util import newton_schulz, rounded, tolerance
 
 pytestmark = pytest.mark.gpu
 
@@ -66,6 +66,29 @@ def test_large_tiles(rows, cols, parts):
     off, tol = float((got - (y if rows <= cols else y.t())).norm()), tolerance(seen, parts, 2.0**-24, True, bound=True)
     print(f"{rows} x {cols}, {parts} parts: off {off:.3e} of {tol:.3e}", flush=True)
     assert off <= tol
+
+
+@pytest.mark.parametrize("rows,cols", [(64, 300), (300, 64), (257, 300), (600, 200), (1536, 1536), (1500, 4200), (4200, 1536), (4200, 4100), (8200, 2100)])
+@pytest.mark.parametrize("parts", [1, 2])
+@pytest.mark.parametrize("spectrum", ["random", "falling"])
+def test_as_close_as_its_roundings(rows, cols, parts, spectrum):
+    """The worst case that `tolerance` bounds, every error along the values that grow, is far from what happens. This compares with what the same roundings give in
+    another order of sums: Frobenius norms of errors from thousands of independent roundings, which agree to a few per cent; half as much again is allowed for one part, and for two, where
+    the fp32 sums of the products matter as much and are formed otherwise (up to twice the error in a sum), three times."""
+    x = matrix(rows, cols, "f32", 9).cuda()
+    if spectrum == "falling":
+        x *= 1.0 / torch.arange(1, rows + 1, device="cuda")[:, None] if rows <= cols else 1.0 / torch.arange(1, cols + 1, device="cuda")
+    got = run(x, torch.empty(rows, cols, device="cuda"), parts=parts).double()
+    wide = x if rows <= cols else x.t().contiguous()
+    y = wide.double() / (wide.double().norm() + 1e-7)
+    a, b, c = 3.4445, -4.7750, 2.0315
+    for _ in range(5):
+        s = y @ y.t().contiguous()
+        y = a * y + (b * s + c * (s @ s)) @ y
+    off = float(((got if rows <= cols else got.t()) - y).norm() / y.norm())
+    like = [float((rounded(wide, parts, pairs).double() - y).norm() / y.norm()) for pairs in (False, True)]
+    print(f"{rows} x {cols}, {parts} parts, {spectrum}: off {off:.2e}, its roundings {like[0]:.2e}, in pairs of steps {like[1]:.2e}", flush=True)
+    assert off <= max(like) * (1.5 if parts == 1 else 3.0)
 
 
 def test_other_coefficients_and_steps():
