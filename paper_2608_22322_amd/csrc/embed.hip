@@ -36,64 +36,40 @@ __global__ __launch_bounds__(256) void lookup_kernel(Mat table, Ids ids, int64_t
 
 constexpr uint64_t kNoToken = ~uint64_t(0);
 
-// Runs of kSortRun keys (id, token), each sorted by a workgroup with a bitonic network. Ids outside the table come last. A lane holds 4 neighbouring keys, a
-// wavefront 256: of the 55 steps 52 exchange within a wavefront, without a barrier. Up to 2^22 - 1 ids a key is 32 bits (the id, the place in the run).
-// The steps are a loop: unrolled, one workgroup's time is the fetching of its instructions (8192 tokens 13.8 us, exchanged by DPP moves 24.9).
-__device__ __forceinline__ uint32_t either(uint32_t x, uint32_t y, bool least) { return least ? std::min(x, y) : std::max(x, y); }
-__device__ __forceinline__ uint64_t either(uint64_t x, uint64_t y, bool least) { return (x < y) == least ? x : y; }
-__device__ __forceinline__ uint32_t from_lane(uint32_t x, int mask) { return (uint32_t)__shfl_xor((int)x, mask); }
-__device__ __forceinline__ uint64_t from_lane(uint64_t x, int mask) { return (uint64_t)__shfl_xor((unsigned long long)x, mask); }
-
+// Runs of kSortRun keys (id, token) in order, each key put where as many of its run are less as it is from the run's begin. Ids outside the table come last. A workgroup
+// places 64 keys of a run, a quarter of the run's keys compared by each wavefront: 1024^2 comparisons a run, but all of them at once (300 tokens 3.8 us, a bitonic
+// network in registers 6.7; 8192 tokens 6.9 and 13.8). Up to 2^22 - 1 ids a key is 32 bits (the id, the place in the run).
 template <typename K>
 __global__ __launch_bounds__(256) void sort_kernel(Ids ids, int64_t tokens, int64_t vocab, uint64_t* keys) {
     constexpr bool kNarrow = sizeof(K) == 4;
-    __shared__ K s[kSortRun];
-    const int64_t first = (int64_t)blockIdx.x * kSortRun;
-    const int p0 = threadIdx.x * 4;
-    K k[4];
+    typedef K k16 __attribute__((ext_vector_type(16 / sizeof(K))));
+    __shared__ __attribute__((aligned(16))) K s[kSortRun];
+    __shared__ uint32_t below[4][64];
+    const int64_t first = (int64_t)(blockIdx.x / (kSortRun / 64)) * kSortRun;
+    const int w = threadIdx.x >> 6, lane = threadIdx.x & 63, mine = (int)(blockIdx.x % (kSortRun / 64)) * 64 + lane;
+    const int n = (int)std::min<int64_t>(kSortRun, tokens - first), quarter = (n + 31) / 32 * 8;
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-        const int64_t t = first + p0 + j, id = t < tokens ? id_at(ids, t) : -1;
-        const uint64_t at = kNarrow ? (uint64_t)id * kSortRun + (uint64_t)(p0 + j) : (uint64_t)id << 32 | (uint64_t)t;
-        k[j] = id >= 0 && id < vocab ? (K)at : ~K(0);
+    for (int j = 0; j < kSortRun / 256; ++j) {
+        const int p = j * 256 + threadIdx.x;
+        const int64_t t = first + p, id = t < tokens ? id_at(ids, t) : -1;
+        const uint64_t at = (uint64_t)(id >= 0 && id < vocab ? id : vocab);  // (keys stay different without a token)
+        s[p] = t < tokens ? (K)(kNarrow ? at * kSortRun + (uint64_t)p : at << 32 | (uint64_t)t) : ~K(0);
     }
-    const int64_t left = std::min<int64_t>(kSortRun, tokens - first);  // few tokens: the rest of the run is in order
-#pragma unroll 1
-    for (int size = 2; size / 2 < left; size *= 2) {
-#pragma unroll 1
-        for (int gap = size / 2; gap >= 4; gap /= 2) {
-            K y[4];
-            if (gap >= 256) {
-                __syncthreads();
+    __syncthreads();
+    const K k = s[mine];
+    uint32_t count = 0;
+    for (int i = w * quarter; i < (w + 1) * quarter; i += 8) {
+        k16 x[sizeof(K) / 2];
 #pragma unroll
-                for (int j = 0; j < 4; ++j) s[p0 + j] = k[j];
-                __syncthreads();
+        for (int j = 0; j < (int)sizeof(K) / 2; ++j) x[j] = reinterpret_cast<const k16*>(s + i)[j];
 #pragma unroll
-                for (int j = 0; j < 4; ++j) y[j] = s[(p0 ^ gap) + j];
-            } else {
-#pragma unroll
-                for (int j = 0; j < 4; ++j) y[j] = from_lane(k[j], gap / 4);
-            }
-            const bool least = ((p0 & gap) == 0) == ((p0 & size) == 0);
-#pragma unroll
-            for (int j = 0; j < 4; ++j) k[j] = either(k[j], y[j], least);
-        }
-        const auto step = [&](int i, int j) __attribute__((always_inline)) {
-            const bool up = ((p0 + i) & size) == 0;
-            const K x = k[i], y = k[j];
-            k[i] = either(x, y, up);
-            k[j] = either(x, y, !up);
-        };
-        if (size > 2) step(0, 2), step(1, 3);
-        step(0, 1), step(2, 3);
+        for (int j = 0; j < 8; ++j) count += x[j * (int)sizeof(K) / 16][j % (16 / (int)sizeof(K))] < k ? 1u : 0u;
     }
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-        if (p0 + j >= left) continue;
-        uint64_t out = k[j];
-        if (kNarrow) out = k[j] == ~K(0) ? kNoToken : (uint64_t)(k[j] / kSortRun) << 32 | (uint64_t)(first + k[j] % kSortRun);
-        keys[first + p0 + j] = out;
-    }
+    below[w][lane] = count;
+    __syncthreads();
+    if (w || mine >= n) return;
+    const uint64_t id = kNarrow ? (uint64_t)k / kSortRun : (uint64_t)k >> 32;
+    keys[first + below[0][lane] + below[1][lane] + below[2][lane] + below[3][lane]] = id < (uint64_t)vocab ? id << 32 | (uint64_t)(first + mine) : kNoToken;
 }
 
 // Up to kMergeRuns sorted runs of `run` keys into one: a key's place is its own plus the numbers of the other runs' keys before it (keys without a
@@ -302,11 +278,11 @@ template <typename T, typename O>
 hipError_t run_backward(EmbedBackward a, hipStream_t st) {
     const uint32_t slabs = (uint32_t)((a.cols + kSlab - 1) / kSlab);
     if (a.tokens > 0) {
-        const uint32_t runs = (uint32_t)((a.tokens + kSortRun - 1) / kSortRun);
+        const uint32_t groups = (uint32_t)((a.tokens + 63) / 64);
         if (a.vocab < (1 << 22))
-            sort_kernel<uint32_t><<<runs, 256, 0, st>>>(a.ids, a.tokens, a.vocab, a.key0);
+            sort_kernel<uint32_t><<<groups, 256, 0, st>>>(a.ids, a.tokens, a.vocab, a.key0);
         else
-            sort_kernel<uint64_t><<<runs, 256, 0, st>>>(a.ids, a.tokens, a.vocab, a.key0);
+            sort_kernel<uint64_t><<<groups, 256, 0, st>>>(a.ids, a.tokens, a.vocab, a.key0);
         for (int64_t run = kSortRun; run < a.tokens; run *= kMergeRuns) {
             int steps = 1;  // a search among n keys takes floor(log2 n) + 1 steps
             while ((run >> steps) > 0) ++steps;

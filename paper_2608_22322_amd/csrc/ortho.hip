@@ -217,14 +217,14 @@ struct Task {
     const OrthoItem t;
     int item;
     bool tall;
-    int32_t dp;
+    int32_t dp, own;  // own: places from a launch's square matrices to this tile's
     Held x;
     // the item's square matrices
     __device__ __forceinline__ Held square(int i) const {
         const int64_t n = (int64_t)dp * dp;
         return {t.a + i * a.parts * n, n, dp, a.parts};
     }
-    __device__ __forceinline__ Task(const OrthoLaunch& l, int i) : a(l), t(l.it[i]), item(i) {
+    __device__ __forceinline__ Task(const OrthoLaunch& l, int i, int to = 0) : a(l), t(l.it[i]), item(i), own(to) {
         tall = t.rp > t.cp || (t.rp == t.cp && t.rows > t.cols);
         dp = min(t.rp, t.cp);
         x = {a.from ? t.x[1] : t.x[0], (int64_t)t.rp * t.cp, t.cp, a.parts};
@@ -242,8 +242,8 @@ struct Task {
         p.n = square_kind(KIND) ? dp : t.cp;
         p.turns = item_turns(t, KIND);
         const MmOperand ox = x.operand(t.rp);
-        p.a = KIND == kGram ? ox : KIND == kPoly ? square(a.square.a).operand(dp) : tall ? ox : square(a.by).operand(dp);
-        p.b = KIND == kGram ? ox : KIND == kPoly ? square(a.square.b).operand(dp) : tall ? square(a.by).operand(dp) : ox;
+        p.a = KIND == kGram ? ox : KIND == kPoly ? square(a.square.a).operand(dp) : tall ? ox : square(a.by + own).operand(dp);
+        p.b = KIND == kGram ? ox : KIND == kPoly ? square(a.square.b).operand(dp) : tall ? square(a.by + own).operand(dp) : ox;
         return p;
     }
     // What the product is combined with: sum * factor() + one() * other() + two() * second(), and that times after().
@@ -258,7 +258,7 @@ struct Task {
     // where it goes, for what stays in the workspace
     __device__ __forceinline__ Held to() const {
         if (KIND == kGram) return square(0);
-        if (KIND == kPoly) return square(a.square.out);
+        if (KIND == kPoly) return square(a.square.out + own);
         return {a.from ? t.x[0] : t.x[1], x.size, x.ld, a.parts};
     }
     __device__ __forceinline__ int32_t rows() const { return square_kind(KIND) ? dp : t.rp; }
@@ -510,23 +510,44 @@ __device__ __forceinline__ void segment(const Task<KIND>& task, int tile, int t0
         segment<B, KIND, PARTS, PIECE, false>(task, tile, t0, t1, place, at);
 }
 
+// An XCD takes a contiguous eighth of each item's tiles, the items one after the other (longest first): contiguous eighths of all the tiles would leave the long ones
+// to some of the XCDs. Items with few tiles begin at different XCDs. False: no tile for this workgroup.
+__device__ __forceinline__ bool whole_tile(const OrthoLaunch& a, int& i, uint32_t& tile) {
+    uint32_t k = blockIdx.x >> 3;
+    tile = 0;
+    for (i = 0; i < a.count; ++i) {
+        const uint32_t n = (uint32_t)(min(a.begin[i + 1], (int64_t)a.whole) - min(a.begin[i], (int64_t)a.whole)), x = (blockIdx.x + (uint32_t)i) & 7u, per = n >> 3,
+                       rest = n & 7u, mine = per + (x < rest ? 1u : 0u);
+        tile = x * per + min(x, rest) + k;
+        if (k < mine) return true;
+        k -= mine;
+    }
+    return false;
+}
+
 template <int B, int KIND, int PARTS>
 __global__ __launch_bounds__(MmTile<B>::kThreads, 2) void ortho_kernel(OrthoLaunch a) {
     constexpr int PA = PARTS, PB = PARTS;
     MM_PLACES(B, PA, PB, places);
-    // An XCD takes a contiguous eighth of each item's tiles, the items one after the other (longest first): contiguous eighths of all the tiles would leave the long ones
-    // to some of the XCDs. Items with few tiles begin at different XCDs.
-    uint32_t k = blockIdx.x >> 3, tile = 0;
-    int i = 0;
-    for (; i < a.count; ++i) {
-        const uint32_t n = (uint32_t)(min(a.begin[i + 1], (int64_t)a.whole) - min(a.begin[i], (int64_t)a.whole)), x = (blockIdx.x + (uint32_t)i) & 7u, per = n >> 3,
-                       rest = n & 7u, mine = per + (x < rest ? 1u : 0u);
-        tile = x * per + min(x, rest) + k;
-        if (k < mine) break;
-        k -= mine;
-    }
-    if (i == a.count) return;
+    int i;
+    uint32_t tile;
+    if (!whole_tile(a, i, tile)) return;
     segment<B, KIND, PARTS>(Task<KIND>(a, i), (int32_t)tile, 0, item_turns(a.it[i], KIND) * item_segments(B, a.parts), 0, places);
+}
+
+// Matrices with a shorter side of up to 64, whose b A + c A A is one tile: each workgroup of X's product takes it for itself, into a place of its own (500 x 64: 5
+// launches less, 64 us of kernels in place of 75).
+template <int KIND, int PARTS>
+__global__ __launch_bounds__(MmTile<64>::kThreads, 2) void ortho_narrow_kernel(OrthoLaunch a) {
+    constexpr int PA = PARTS, PB = PARTS;
+    MM_PLACES(64, PA, PB, places);
+    int i;
+    uint32_t tile;
+    if (!whole_tile(a, i, tile)) return;
+    segment<64, kPoly, PARTS>(Task<kPoly>(a, i, (int)tile), 0, 0, 1, 0, places);
+    __threadfence_block();  // the workgroup's stores of its own place before its loads
+    __syncthreads();
+    segment<64, KIND, PARTS>(Task<KIND>(a, i, (int)tile), (int32_t)tile, 0, 1, 0, places);
 }
 
 // The pieces of the tiles behind the whole ones, those at one place of k neighbours.
@@ -720,6 +741,33 @@ bool in_pairs(const OrthoLaunch& a, const OrthoCoefs& k) {
     return k.pairs && k.steps > 1 && group_cut(a, kGram).us + group_cut(a, kNext).us > 3 * group_cut(a, kPoly).us + 25;
 }
 
+// Whether each tile of X takes b A + c A A for itself: one tile of it, and no more than a round of X's.
+bool is_narrow(const OrthoItem& t) { return std::min(t.rp, t.cp) == 64 && std::max(t.rp, t.cp) <= 64 * 256; }
+bool is_narrow(const OrthoLaunch& a) {
+    for (int i = 0; i < a.count; ++i)
+        if (!is_narrow(a.it[i])) return false;
+    return true;
+}
+constexpr int32_t kSquares = 3;  // places for square matrices, and behind them the tiles' own
+
+template <int KIND>
+hipError_t narrow_product(OrthoLaunch& a, hipStream_t st) {
+    a.slots = 0;
+    a.rest = 0;
+    uint32_t most = 0;
+    for (int i = 0; i < a.count; ++i) {
+        const int64_t n = item_tiles(a.it[i], KIND, 64);
+        a.begin[i + 1] = a.begin[i] + n;
+        most += (uint32_t)((n + 7) / 8);
+    }
+    a.whole = (uint32_t)a.begin[a.count];
+    if (a.parts > 1)
+        ortho_narrow_kernel<KIND, 2><<<8 * most, MmTile<64>::kThreads, 0, st>>>(a);
+    else
+        ortho_narrow_kernel<KIND, 1><<<8 * most, MmTile<64>::kThreads, 0, st>>>(a);
+    return hipGetLastError();
+}
+
 // The steps of a group whose X0 lies in place 1; the last one's outputs go where LAST says.
 template <int LAST>
 hipError_t iterate(OrthoLaunch& a, const OrthoCoefs& k, hipStream_t st) {
@@ -733,12 +781,23 @@ hipError_t iterate(OrthoLaunch& a, const OrthoCoefs& k, hipStream_t st) {
         {0, 0, 0, 0, 2, k.c * (kB / (kA * kA)), k.b * (kB / kA), 0},        // B', at 2
         {2, 1, 1, 2, 0, 1 / kB, k.a, k.a},                                  // D = a B + a B' + B' B, at 0
     };
-    const bool pairs = in_pairs(a, k);
+    const bool narrow = is_narrow(a), pairs = !narrow && in_pairs(a, k);
     a.from = 1;
     a.first = 1;
     for (int i = 0; i < k.steps;) {
         const bool two = pairs && i + 1 < k.steps;
         hipError_t e = product<kGram>(a, st);
+        if (narrow) {
+            a.square = poly;
+            a.square.out = a.by = kSquares;
+            a.ca = k.a;
+            ++i;
+            if (e == hipSuccess) e = i < k.steps ? narrow_product<kNext>(a, st) : narrow_product<LAST>(a, st);
+            if (e != hipSuccess) return e;
+            a.from ^= 1;
+            a.first = 0;
+            continue;
+        }
         for (int j = 0; j < (two ? 5 : 1) && e == hipSuccess; ++j) {
             a.square = two ? pair[j] : poly;
             e = product<kPoly>(a, st);
@@ -771,7 +830,7 @@ char* place(OrthoItem& t, int64_t rows, int64_t cols, int32_t parts, bool update
     at += up((size_t)t.rp * t.cp * 2 * parts);
     t.a = reinterpret_cast<uint16_t*>(at);
     const size_t d = (size_t)std::min(t.rp, t.cp);
-    return at + up(d * d * 2 * parts * 3);
+    return at + up(d * d * 2 * parts * (kSquares + (is_narrow(t) ? (size_t)std::max(t.rp, t.cp) / 64 : 0)));
 }
 
 }  // namespace
