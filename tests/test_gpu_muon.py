@@ -189,3 +189,50 @@ def test_step_of_a_named_list():
         al.adamw_step(rest, ac, t, al.workspace(al.adamw_workspace_bytes(rest, ac)))
     for x, y in zip(a, b):
         assert torch.equal(x.param, y.param)
+
+
+def test_lists_of_one_kind():
+    """MuonStep over matrices alone and over nothing for it to orthogonalise."""
+    import paper_2608_22322_amd as al
+    from paper_2608_22322_amd.muon import MuonStep
+
+    for names, shapes in ((["layer0.q", "layer1.q"], [(70, 64), (64, 130)]), (["embed", "norm"], [(30, 64), (1, 64)])):
+        sts = [al.ParamState(torch.ones(r, c, device="cuda"), torch.randn(r, c, device="cuda").bfloat16(), r, c) for r, c in shapes]
+        MuonStep(sts, names).step(1)
+        assert all(s.param.isfinite().all() and not (s.param == 1).all() for s in sts)
+
+
+def test_a_bad_gradient_stays_with_its_matrix():
+    import paper_2608_22322_amd as al
+
+    for bad in (float("nan"), float("inf")):
+        a, b = (states([(100, 60), (64, 300), (300, 64)], True, False, 17) for _ in range(2))
+        a[1].grad[3, 7] = bad
+        cfg = al.muon_cfg(lr=1e-2, grad_bf16=False)
+        for s in (a, b):
+            al.muon_step(s, cfg, 1, al.workspace(al.muon_workspace_bytes(s, cfg)))
+        assert a[1].param.isnan().all()
+        for i in (0, 2):
+            assert torch.equal(a[i].param, b[i].param) and torch.equal(a[i].m, b[i].m)
+
+
+def test_resumed_from_a_checkpoint(tmp_path):
+    import paper_2608_22322_amd as al
+    from paper_2608_22322_amd import checkpoint
+
+    shapes = [(120, 300), (64, 70)]
+    a, b = states(shapes, True, True, 19), states(shapes, True, True, 23)
+    cfg = al.muon_cfg(lr=1e-2)
+    ws = al.workspace(al.muon_workspace_bytes(a, cfg))
+    specs = [{"m": al.Spec(al.UF8, 256)}] * 2
+    al.muon_step(a, cfg, 1, ws)
+    path = str(tmp_path / "muon.safetensors")
+    checkpoint.save(path, a, specs, ["layer0.q", "layer0.k"], "muon", 1)
+    for x, y in zip(a, b):
+        y.param.copy_(x.param)
+        y.grad.copy_(x.grad)
+    assert checkpoint.load(path, b, specs, "muon") == ("muon", 1)
+    for s in (a, b):
+        al.muon_step(s, cfg, 2, ws)
+    for x, y in zip(a, b):
+        assert torch.equal(x.param, y.param) and torch.equal(x.m, y.m) and torch.equal(x.m_meta, y.m_meta)

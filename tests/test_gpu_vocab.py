@@ -187,3 +187,31 @@ def test_replayed_graphs_that_share_a_workspace():
         torch.cuda.synchronize()
         for d, i, w in zip(dy, ids, dw):
             assert torch.equal(w, backward(d, i, 60, torch.float32))
+
+
+def test_streams():
+    """On a side stream, given or current, as on the default one."""
+    from paper_2608_22322_amd import vocab as voc
+
+    ids = ids_of("ignored", 700, 90, 8).cuda()
+    table, dy = torch.randn(90, 100, device="cuda"), torch.randn(700, 100, device="cuda")
+    out = [torch.empty(700, 100, device="cuda") for _ in range(3)]
+    want = backward(dy, ids, 90, torch.float32)
+    voc.embed_forward(table, ids, out[0])
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    voc.embed_forward(table, ids, out[1], stream=side)
+    with torch.cuda.stream(side):
+        voc.embed_forward(table, ids, out[2])
+        got = backward(dy, ids, 90, torch.float32)
+    side.synchronize()
+    torch.cuda.synchronize()
+    assert torch.equal(out[0], out[1]) and torch.equal(out[0], out[2]) and torch.equal(got, want)
+
+
+@pytest.mark.parametrize("vocab", [(1 << 22) - 1, 1 << 22])
+def test_both_sides_of_the_narrow_keys(vocab):
+    """The last id and one past it, at the largest vocabulary whose keys are 32 bits and the next."""
+    ids = torch.tensor([vocab - 1, vocab, 0, vocab - 1, -1, vocab - 2] * 200, device="cuda")
+    got = backward(torch.ones(1200, 2, device="cuda"), ids, vocab, torch.float32)
+    assert (got[-1] == 400).all() and (got[0] == 200).all() and (got[-2] == 200).all() and float(got.sum()) == 1600

@@ -250,3 +250,40 @@ def test_replayed_graphs_that_share_a_workspace():
             got = loss.clone(), dh.clone(), dw.clone()
             voc.linear_xent(h, w, t, loss, ws, dh=dh, dw=dw)
             assert all(torch.equal(x, y) for x, y in zip(got, (loss, dh, dw)))
+
+
+@pytest.mark.parametrize("pad,tokens", [(0, 1), (0, 70), (8, 130), (4, 65), (0, 16450)])
+def test_hidden_states_read_where_they_are(pad, tokens):
+    """Without dw and with whole, aligned rows h is not copied: what an ignored token holds still reaches nothing, and other pitches give the same."""
+    c = Case(tokens, 128, 90 if tokens > 1000 else 300)
+    c.h[~c.keep] = float("nan")
+    out = call(c, "f32", None, lse=True, pad=(pad, 0))
+    only = call(c, None, None, pad=(pad, 0))
+    assert torch.equal(only["loss"], out["loss"])
+    packed = call(c, "f32", "f32", lse=True, pad=(pad, 0))  # dw: h is copied
+    for name in ("loss", "lse", "dh"):
+        assert out[name].isfinite().all() and not out[name][torch.from_numpy(~c.keep)].any()
+        assert torch.equal(out[name], packed[name])
+    c.h[~c.keep] = 0.0
+    check(c, out, "f32")
+
+
+def test_streams_and_two_calls_at_once():
+    """Two calls on streams of their own with workspaces of their own, at the same time."""
+    import paper_2608_22322_amd as al
+    from paper_2608_22322_amd import vocab as voc
+
+    cases = [Case(300, 128, 2000), Case(500, 200, 1500)]
+    want = [call(c, "f32", "f32") for c in cases]
+    made = []
+    for c in cases:
+        h, w, t = c.h.cuda(), c.w.cuda(), c.target.cuda()
+        dh, dw = torch.empty(c.h.shape, device="cuda"), torch.empty(c.w.shape, device="cuda")
+        made.append((h, w, t, c.weight.cuda(), torch.empty(len(t), device="cuda"), dh, dw, al.workspace(voc.linear_xent_workspace_bytes(h, w, dh, dw)), torch.cuda.Stream()))
+    torch.cuda.synchronize()
+    for _ in range(3):
+        for c, (h, w, t, weight, loss, dh, dw, ws, st) in zip(cases, made):
+            voc.linear_xent(h, w, t, loss, ws, weight=weight, scale=c.scale, dh=dh, dw=dw, stream=st)
+    torch.cuda.synchronize()
+    for (_, _, _, _, loss, dh, dw, _, _), x in zip(made, want):
+        assert torch.equal(loss, x["loss"]) and torch.equal(dh, x["dh"]) and torch.equal(dw, x["dw"])
