@@ -173,3 +173,24 @@ def test_nothing_to_do():
     for shape in ((0, 5), (5, 0)):
         x = torch.empty(shape, device="cuda")
         muon.orthogonalize(x, torch.empty_like(x), None)
+
+
+@pytest.mark.parametrize("rows,cols", [(1, 1 << 21), (1 << 21, 1), (16384, 64), (16448, 64), (60, 16450), (70000, 3)])
+@pytest.mark.parametrize("parts", [1, 2])
+def test_long_and_narrow(rows, cols, parts):
+    """One side at its longest; a side of 64 with as many tiles as a round of the device, and one more."""
+    g = torch.Generator(device="cuda").manual_seed(rows)
+    x = torch.empty(rows, cols, device="cuda").normal_(generator=g)
+    got = run(x, torch.empty_like(x), parts=parts).double()
+    wide = x if rows <= cols else x.t().contiguous()
+    y = wide.double() / (wide.double().norm() + 1e-7)
+    a, b, c = 3.4445, -4.7750, 2.0315
+    for _ in range(5):
+        s = y @ y.t().contiguous()
+        y = a * y + (b * s + c * (s @ s)) @ y
+    off = float(((got if rows <= cols else got.t()) - y).norm() / y.norm())
+    like = float((rounded(wide, parts).double() - y).norm() / y.norm())
+    print(f"{rows} x {cols}, {parts} parts: off {off:.2e}, its roundings {like:.2e}", flush=True)
+    # (fp32 sums over up to 2^21 products, a random walk of roundings each way: sqrt(K) 2^-24 of the sum, as in a step's error for what it does to the singular value:
+    # at most 3.4 a step at the start, so 3.4^5; for several rows the comparison covers it)
+    assert off <= like * 3.0 + (3.4**5 * max(rows, cols) ** 0.5 * 2.0**-24 if min(rows, cols) < 64 else 0.0)

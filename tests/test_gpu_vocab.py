@@ -215,3 +215,16 @@ def test_both_sides_of_the_narrow_keys(vocab):
     ids = torch.tensor([vocab - 1, vocab, 0, vocab - 1, -1, vocab - 2] * 200, device="cuda")
     got = backward(torch.ones(1200, 2, device="cuda"), ids, vocab, torch.float32)
     assert (got[-1] == 400).all() and (got[0] == 200).all() and (got[-2] == 200).all() and float(got.sum()) == 1600
+
+
+@pytest.mark.parametrize("tokens,vocab,cols", [(3, 4, (1 << 20) + 3), (70, 1, 100001), (40, 1 << 20, 1)])
+def test_long_sides(tokens, vocab, cols):
+    from paper_2608_22322_amd import vocab as voc
+
+    ids = ids_of("random", tokens, vocab, 3).cuda()
+    dy = torch.randint(-8, 9, (tokens, cols), device="cuda").float()
+    got = backward(dy.bfloat16(), ids, vocab, torch.float32)
+    assert torch.equal(got.double(), torch.zeros(vocab, cols, dtype=torch.float64, device="cuda").index_add_(0, ids, dy.double()))
+    out = torch.empty(tokens, cols, device="cuda")
+    voc.embed_forward(got, ids, out)
+    assert torch.equal(out, got[ids])

@@ -287,3 +287,11 @@ def test_streams_and_two_calls_at_once():
     torch.cuda.synchronize()
     for (_, _, _, _, loss, dh, dw, _, _), x in zip(made, want):
         assert torch.equal(loss, x["loss"]) and torch.equal(dh, x["dh"]) and torch.equal(dw, x["dw"])
+
+
+@pytest.mark.parametrize("tokens,hidden,vocab", [(3, 1 << 18, 5), (2, 100001, 70), (70, 8, 1 << 20), (1, 3, 300007), (5, 16, (1 << 21) + 3)])
+def test_long_sides(tokens, hidden, vocab):
+    """Features or a vocabulary far longer than the other sides."""
+    c = Case(tokens, hidden, vocab, ignored=False)
+    check(c, call(c, "f32", "bf16", lse=True), "f32", "bf16")
+    check(c, call(c), None, None)
