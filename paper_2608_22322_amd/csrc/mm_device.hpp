@@ -321,8 +321,8 @@ __device__ __forceinline__ MmId mm_id(const Mm& p) {
     return t;
 }
 
-// E: end(row, first column, 4 sums) takes 4 neighbouring outputs. One with E::kRows takes a wavefront's
-// row instead, end.row<FN>(row, first column of its part, lane, sums), and no splits.
+// E: end(row, first column, 4 sums) takes 4 neighbouring outputs. One with E::kRows takes all of a lane's rows instead (every 16th from `row` on),
+// end.rows<FM, FN>(row, first column of its part, lane, sums), and no splits.
 template <class E, class = void>
 struct MmRows : std::false_type {};
 template <class E>
@@ -347,12 +347,12 @@ __global__ __launch_bounds__(MmTile<B>::kThreads, 2) void mm_kernel(Mm p, E end)
             for (int j = 0; j < G::FN; ++j) part[(i * G::FN + j) * 64] = acc[i][j];
         return;
     }
+    if constexpr (MmRows<E>::value) {
+        end.template rows<G::FM, G::FN>(m, n, lane, acc);
+    } else {
 #pragma unroll
-    for (int i = 0; i < G::FM; ++i) {
-        __builtin_amdgcn_sched_barrier(0);
-        if constexpr (MmRows<E>::value) {
-            end.template row<G::FN>(m + 16 * i, n, lane, acc[i]);
-        } else {
+        for (int i = 0; i < G::FM; ++i) {
+            __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
             for (int j = 0; j < G::FN; ++j) end(m + 16 * i, n + 16 * j, acc[i][j]);
         }
