@@ -1,7 +1,7 @@
 // Token embeddings: the lookup with its scale, and the table's gradient summed in the order of the tokens sorted by id.
 //
 // Both are bound by memory: the lookup of 8192 x 2048 bf16 takes 10.3 us (67 MB), the gradient of 8192 tokens in 32000 x 4096 fp32 135 us (591 MB, the rows' kernel 107 at
-// 5.5 TB/s). Small calls are bound by their launches: one token 6.2 us, 300 tokens in 5003 x 1001 25 us, three launches.
+// 5.5 TB/s). Small calls are bound by their launches: one token 6.2 us, 300 tokens in 5003 x 1001 21 us, three launches.
 #include <algorithm>
 
 #include "act_device.hpp"
@@ -226,9 +226,9 @@ __global__ __launch_bounds__(256) void piece_kernel(EmbedBackward a, uint32_t pi
     store4(a.part + (int64_t)piece * a.cols, c, a.cols, s);
 }
 
-// kRows rows of the table's gradient, kSlab columns: sums of their tokens, scaled, added to the base and rounded once.
-constexpr int kRows = 8;
-template <typename T, typename O>
+// kRows rows of the table's gradient, kSlab columns: sums of their tokens, scaled, added to the base and rounded once. 8 rows one after the other share the loads of
+// where their tokens begin; 2 where there are too few rows for that to fill the device (300 tokens in 5003 x 1001: 10.9 and 8.8 us).
+template <typename T, typename O, int kRows>
 __global__ __launch_bounds__(256) void rows_kernel(EmbedBackward a) {
     const int64_t v0 = (int64_t)blockIdx.x * kRows;
     const int c = (int)blockIdx.y * kSlab + threadIdx.x * 4;
@@ -295,7 +295,10 @@ hipError_t run_backward(EmbedBackward a, hipStream_t st) {
         const uint32_t pieces = (uint32_t)(a.tokens / kPiece);
         piece_kernel<T><<<pieces * slabs + (uint32_t)(a.vocab / 256 + 1), 256, 0, st>>>(a, pieces, slabs);
     }
-    rows_kernel<T, O><<<dim3((uint32_t)((a.vocab + kRows - 1) / kRows), slabs), 256, 0, st>>>(a);
+    if (a.vocab * slabs >= 8 * 2048)
+        rows_kernel<T, O, 8><<<dim3((uint32_t)((a.vocab + 7) / 8), slabs), 256, 0, st>>>(a);
+    else
+        rows_kernel<T, O, 2><<<dim3((uint32_t)((a.vocab + 1) / 2), slabs), 256, 0, st>>>(a);
     return hipGetLastError();
 }
 

@@ -12,7 +12,7 @@
 // tiles for 256 of them, or matrices of different sizes), the group's turns are dealt out evenly instead: a workgroup takes a stretch of them, across tiles, and tiles
 // that two or more worked on are joined in a second launch, in order; or the tiles behind the last full round are taken in pieces.
 //
-// Bound by the matrix cores where matrices are large: 4096 x 11008 in one part 2.77 ms, 1.0 to 1.2 PFLOP/s in its products (a library product of 4096^3 1.38); by
+// Bound by the matrix cores where matrices are large: 4096 x 11008 in one part 2.77 to 2.86 ms, 1.0 to 1.2 PFLOP/s in its products (a library product of 4096^3 1.38); by
 // launches and by what one or two workgroups a compute unit reach where they are not: 1001 x 1750 in two parts 285 us, 1.0e11 operations.
 #include <algorithm>
 #include <cmath>

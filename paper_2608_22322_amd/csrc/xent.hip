@@ -8,7 +8,7 @@
 // part, or two where a gradient is wanted in fp32); two more products use it while it is in the caches. A fourth product for three, but no
 // tokens x vocabulary matrix: what is kept is tokens x piece.
 //
-// Bound by the matrix cores (8192 tokens, 32000 x 2048, bf16 gradients: 3.73 ms, the four products at 1.0 to 1.2 PFLOP/s), for one token by reading w (32000 x 4096: 54 us, the
+// Bound by the matrix cores (8192 tokens, 32000 x 2048, bf16 gradients: 3.68 ms, the four products at 1.0 to 1.2 PFLOP/s), for one token by reading w (32000 x 4096: 54 us, the
 // product 6.5 TB/s), for fp32 gradients by the ends that read a base and write dw between rounds of tiles (1501 tokens, 32003 x 1750: 1.16 ms).
 #include <algorithm>
 #include <cmath>
