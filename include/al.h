@@ -326,8 +326,8 @@ al_status al_apollo_step(const al_apollo_tensor* tensors, int32_t nt, const al_a
  *   X <- a X + X (b A + c A A), A = X^T X        (rows > cols).
  * A zero matrix gives zeros (also with eps = 0), one that holds an infinity or a NaN gives NaN.
  * parts: what X, A and b A + c A A are held in between the products, whose
- * sums are fp32: 1 = one fp16 number each (11 bits: the result is 1e-3 to 2e-3 off for normal matrices, 2e-3 to 4e-3 where singular values
- * fall as 1 / k), 2 = the sum of two (22 bits; 2e-6 to 4e-6, of the fp32 sums; three products for one). Where that is less work, two steps are taken at
+ * sums are fp32: 1 = one fp16 number each (11 bits: the result is 1e-3 to 3.5e-3 off for normal matrices, up to 4e-3 where singular values
+ * fall as 1 / k), 2 = the sum of two (22 bits; 1e-6 to 6e-6, of the fp32 sums too; three products for one). Where that is less work, two steps are taken at
  * once, as X <- a a X + D X with a second A = M A M, M = a I + b A + c A A (the same polynomial of A, other roundings). |G| is a binary64 sum in a fixed order:
  * every result repeats bit for bit.
  * a, b, c: for singular values of at most 1 to begin with, those of X must stay within 4 and those of b A + c A A within

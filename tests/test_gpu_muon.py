@@ -236,3 +236,30 @@ def test_resumed_from_a_checkpoint(tmp_path):
         al.muon_step(s, cfg, 2, ws)
     for x, y in zip(a, b):
         assert torch.equal(x.param, y.param) and torch.equal(x.m, y.m) and torch.equal(x.m_meta, y.m_meta)
+
+
+@pytest.mark.parametrize("parts", [1, 2])
+def test_a_layer(parts):
+    """Matrices at whose sizes the wide tiles are taken and steps go two at a time, among small ones: parameters from zero, against the 64-bit form and the same
+    roundings in another order (as for the products alone)."""
+    import paper_2608_22322_amd as al
+    from tests.ortho_util import rounded
+
+    shapes = [(2048, 2048), (256, 2048), (5632, 2048), (2048, 5632), (64, 64), (4224, 4200)]
+    sts = states(shapes, False, False, 29, momentum=False)
+    for s in sts:
+        s.param.zero_()
+    cfg = al.muon_cfg(lr=1.0, beta=0.0, nesterov=False, scale=al.SCALE_NONE, parts=parts, grad_bf16=False, m=al.Spec(al.FP32, 256))
+    al.muon_step(sts, cfg, 1, al.workspace(al.muon_workspace_bytes(sts, cfg)))
+    a, b, c = al.ORTHO_COEFS
+    for s in sts:
+        wide = s.grad if s.rows <= s.cols else s.grad.t().contiguous()
+        got = -(s.param if s.rows <= s.cols else s.param.t()).double()
+        y = wide.double() / (wide.double().norm() + 1e-7)
+        for _ in range(5):
+            q = y @ y.t().contiguous()
+            y = a * y + (b * q + c * (q @ q)) @ y
+        off = float((got - y).norm() / y.norm())
+        like = max(float((rounded(wide, parts, pairs).double() - y).norm() / y.norm()) for pairs in (False, True))
+        print(f"{s.rows} x {s.cols}, {parts} parts: off {off:.2e}, its roundings {like:.2e}", flush=True)
+        assert off <= like * (1.5 if parts == 1 else 3.0)
