@@ -62,6 +62,8 @@ MmCut mm_cut(int64_t m, int64_t n, int64_t turns, int parts) {
     return best;
 }
 
+int64_t mm_threads(const MmCut& c, int64_t m, int64_t n) { return tiles_of(c.tile, m, n) * c.splits * (c.tile == 256 ? 512 : 256); }
+
 size_t mm_part_bytes(const MmCut& c, int64_t m, int64_t n) {
     return c.splits == 1 ? 0 : (size_t)(tiles_of(c.tile, m, n) * c.splits) * c.tile * c.tile * 4;
 }

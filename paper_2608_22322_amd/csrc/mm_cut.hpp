@@ -21,6 +21,8 @@ struct MmCut {
 };
 // One product: tile and splits of k.
 MmCut mm_cut(int64_t m, int64_t n, int64_t turns, int parts);
+// Threads of the launch of a product cut so. A grid of 2^32 threads and more loses its upper part without an error.
+int64_t mm_threads(const MmCut& c, int64_t m, int64_t n);
 // Bytes of the partial sums of a product cut so.
 size_t mm_part_bytes(const MmCut& c, int64_t m, int64_t n);
 

@@ -286,8 +286,12 @@ XentPlan xent_plan(int64_t tokens, int64_t hidden, int64_t vocab, int64_t ldw, i
     p.dw_parts = dw ? (grad_dtype == AL_DTYPE_F32 ? 2 : 1) : 0;
     p.parts = std::max(p.dh_parts, p.dw_parts);
     const int64_t turns = p.dp / kMmTurn;
-    p.logits = mm_cut(p.block, vocab, turns, 2);
-    p.logits.splits = 1;
+    // (16384 tokens of up to 64 features by 2^24 columns are 2^32 threads of 128-wide tiles: two passes)
+    for (;; p.block = (p.block / 2 + 63) / 64 * 64) {
+        p.logits = mm_cut(p.block, vocab, turns, 2);
+        p.logits.splits = 1;
+        if (mm_threads(p.logits, p.block, vocab) < (int64_t(1) << 32)) break;
+    }
     const auto up = [](size_t x) { return (x + 255) & ~size_t(255); };
     size_t off = 0;
     const auto take = [&](size_t bytes) {
