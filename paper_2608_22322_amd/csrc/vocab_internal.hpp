@@ -49,7 +49,7 @@ struct XentPlan {
     int32_t parts, dh_parts, dw_parts;  // of the logits' gradients
     bool pack;             // w is copied into padded rows
     MmCut logits, back, dh, dw;
-    size_t h_off, w_off, stat_off, lse_off, coef_off, d_off, dh_off, part_off, bytes;
+    size_t h_off, w_off, stat_off, norm_off, coef_off, d_off, dh_off, part_off, bytes;
 };
 XentPlan xent_plan(int64_t tokens, int64_t hidden, int64_t vocab, int64_t ldw, int dh_dtype, int grad_dtype, bool dh, bool dw);
 struct Xent {

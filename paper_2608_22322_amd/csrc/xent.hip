@@ -4,7 +4,8 @@
 //   d[t][v] = coef[t] (exp(logit[t][v] - lse[t]) - [v = target]),  dh = d w,  dw = d^T h + base
 //
 // The statistics come from the end of the product itself: a wavefront reduces its 64 (32) columns of each row to a maximum and a sum, and a pass over
-// those gives lse. For the gradients the product is taken once more, a piece of the vocabulary at a time, whose end forms d in bf16 (one
+// those gives the row's. lse is kept as these two numbers, lse = top + log(sum): rounded to one, it would be off by 2^-24 of the logits' size, which for a confident token is more than its loss
+// and is the same factor in all of a row's probabilities. For the gradients the product is taken once more, a piece of the vocabulary at a time, whose end forms d in bf16 (one
 // part, or two where a gradient is wanted in fp32); two more products use it while it is in the caches. A fourth product for three, but no
 // tokens x vocabulary matrix: what is kept is tokens x piece.
 //
@@ -42,10 +43,14 @@ __global__ __launch_bounds__(256) void pad_kernel(Mat x, int64_t rows, int32_t c
     *reinterpret_cast<u32x4*>(out + r * cp + c) = k.q;
 }
 
-__device__ __forceinline__ float exp_of(float x) { return __builtin_amdgcn_exp2f(x * 1.44269504088896341f); }
+constexpr float kLog2e = 1.44269504088896341f;
+__device__ __forceinline__ float exp_of(float x) { return __builtin_amdgcn_exp2f(x * kLog2e); }
 
 struct Stat {
     float top, sum;  // largest logit of some columns, and the sum of exp(logit - top)
+};
+struct Norm {
+    float top, log2;  // of a row: the largest logit, and the logarithm of the sum of exp(logit - top) to base 2
 };
 
 // End of the statistics' product: a wavefront's columns of a row as one Stat, and the target's logit where it is among them.
@@ -100,13 +105,16 @@ struct EndStats {
     }
 };
 
-// lse, loss and the gradients' coefficient of each token; tokens behind the last have coefficient 0.
+// What a row is normed by, its loss and the gradients' coefficient of each token; tokens behind the last have coefficient 0.
 __global__ __launch_bounds__(256) void loss_kernel(const Stat* stats, const float* at, int32_t groups, int64_t t0, int32_t tokens, int32_t tokens_padded, int64_t vocab,
-                                                   Ids target, const float* weight, float scale, float* loss, float* lse_out, float* lse, float* coef) {
+                                                   Ids target, const float* weight, float scale, float* loss, float* lse, Norm* norms, float* coef) {
     const int lane = threadIdx.x & 63, m = blockIdx.x * 4 + (threadIdx.x >> 6);
     if (m >= tokens_padded) return;
     if (m >= tokens) {
-        if (lane == 0 && coef) lse[t0 + m] = coef[t0 + m] = 0.0f;
+        if (lane == 0 && coef) {
+            norms[t0 + m] = {0.0f, 0.0f};
+            coef[t0 + m] = 0.0f;
+        }
         return;
     }
     float top = -__builtin_inff(), sum = 0;
@@ -135,13 +143,13 @@ __global__ __launch_bounds__(256) void loss_kernel(const Stat* stats, const floa
     }
     bad = __any(bad);
     if (lane) return;
-    const float l = bad ? __builtin_nanf("") : top + __logf(sum);
+    const float l = bad ? __builtin_nanf("") : logf(sum);
     const int64_t y = target_at(target, t0 + m);
     const bool has = y >= 0 && y < vocab;
-    if (loss) loss[t0 + m] = has ? l - at[m] : 0.0f;
-    if (lse_out) lse_out[t0 + m] = has ? l : 0.0f;
+    if (loss) loss[t0 + m] = has ? (top - at[m]) + l : 0.0f;
+    if (lse) lse[t0 + m] = has ? top + l : 0.0f;
     if (coef) {
-        lse[t0 + m] = l;
+        norms[t0 + m] = {top, l * kLog2e};
         coef[t0 + m] = has ? scale * (weight ? weight[t0 + m] : 1.0f) : 0.0f;
     }
 }
@@ -152,20 +160,22 @@ struct EndGrad {
     uint16_t* d;
     int64_t size;  // from the high part to the low
     int32_t ld, parts, tokens_padded;
-    const float *lse, *coef;
+    const Norm* norms;
+    const float* coef;
     Ids target;
     int64_t v0;
     int32_t tokens, columns;
     // (what belongs to the rows is loaded at once, before any of them is written: one after the other 8192 x 8192 logits of K = 2048 take 285 us, so 266)
     template <int FM, int FN>
     __device__ __forceinline__ void rows(int m, int n, int lane, const f32x4 (&v)[FM][FN]) const {
-        float c[FM], l[FM];
+        float c[FM];
+        Norm l[FM];
         int64_t y[FM];
 #pragma unroll
         for (int i = 0; i < FM; ++i) {
             const int r = min(m + 16 * i, tokens_padded - 1);
             c[i] = coef[r];
-            l[i] = lse[r];
+            l[i] = norms[r];
             y[i] = r < tokens ? target_at(target, r) - v0 - n : -1;
         }
 #pragma unroll
@@ -175,12 +185,12 @@ struct EndGrad {
             for (int j = 0; j < FN; ++j) quad(m + 16 * i, n + 16 * j, v[i][j], c[i], l[i], y[i] - 16 * j);
         }
     }
-    __device__ __forceinline__ void quad(int m, int n, f32x4 v, float c, float l, int64_t y) const {
+    __device__ __forceinline__ void quad(int m, int n, f32x4 v, float c, Norm l, int64_t y) const {
         if (m >= tokens_padded || n >= ld) return;
         f32x4 g;
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
-            const float p = exp_of(v[r] - l) - (y == r ? 1.0f : 0.0f);
+            const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(v[r] - l.top, kLog2e, -l.log2)) - (y == r ? 1.0f : 0.0f);
             g[r] = c != 0.0f && n + r < columns ? c * p : 0.0f;
         }
         uint16_t* const q = d + (int64_t)m * ld + n;
@@ -310,7 +320,7 @@ XentPlan xent_plan(int64_t tokens, int64_t hidden, int64_t vocab, int64_t ldw, i
         p.back.splits = 1;
         p.dh = mm_cut(p.tp, hidden, p.piece / kMmTurn, 1 + std::max(1, p.dh_parts));
         p.dw = mm_cut(p.piece, hidden, p.tp / kMmTurn, 1 + std::max(1, p.dw_parts));
-        p.lse_off = take((size_t)p.tp * 4);
+        p.norm_off = take((size_t)p.tp * sizeof(Norm));
         p.coef_off = take((size_t)p.tp * 4);
         p.d_off = take((size_t)p.tp * p.piece * 2 * p.parts);
         p.dh_off = take(dh && p.piece < vocab ? (size_t)p.tp * hidden * 4 : 0);
@@ -336,7 +346,7 @@ hipError_t launch_xent(const XentPlan& p, const Xent& a, void* ws, hipStream_t s
     MmOperand oh = {h, 0, p.dp, p.tp, p.dp};
     if (as_is) oh = {static_cast<const uint16_t*>(a.h.p), 0, (int32_t)a.h.ld, (int32_t)p.tokens, p.dp};
     Stat* const stats = reinterpret_cast<Stat*>(base + p.stat_off);
-    float* const lse = p.parts ? reinterpret_cast<float*>(base + p.lse_off) : nullptr;
+    Norm* const norms = p.parts ? reinterpret_cast<Norm*>(base + p.norm_off) : nullptr;
     float* const coef = p.parts ? reinterpret_cast<float*>(base + p.coef_off) : nullptr;
     Mm q = {};
     q.part = reinterpret_cast<float*>(base + p.part_off);
@@ -354,7 +364,7 @@ hipError_t launch_xent(const XentPlan& p, const Xent& a, void* ws, hipStream_t s
         g.turns = p.dp / kMmTurn;
         const EndStats end = {stats, at, a.target, t0, n, (int32_t)p.vocab, p.groups};
         if ((e = product<true, true, true, 1>(p.logits, g, end, st)) != hipSuccess) return e;
-        loss_kernel<<<(uint32_t)((padded + 3) / 4), 256, 0, st>>>(stats, at, p.groups, t0, n, padded, p.vocab, a.target, a.weight, a.scale, a.loss, a.lse, lse, coef);
+        loss_kernel<<<(uint32_t)((padded + 3) / 4), 256, 0, st>>>(stats, at, p.groups, t0, n, padded, p.vocab, a.target, a.weight, a.scale, a.loss, a.lse, norms, coef);
     }
     if (!p.parts) return hipGetLastError();
     uint16_t* const d = reinterpret_cast<uint16_t*>(base + p.d_off);
@@ -372,7 +382,7 @@ hipError_t launch_xent(const XentPlan& p, const Xent& a, void* ws, hipStream_t s
         g.m = p.tp;
         g.n = np;
         g.turns = p.dp / kMmTurn;
-        const EndGrad end = {d, size, np, p.parts, p.tp, lse, coef, a.target, v0, (int32_t)p.tokens, n};
+        const EndGrad end = {d, size, np, p.parts, p.tp, norms, coef, a.target, v0, (int32_t)p.tokens, n};
         if ((e = product<true, true, true, 1>(p.back, g, end, st)) != hipSuccess) return e;
         const MmOperand od = {d, size, np, p.tp, np};
         if (p.dh_parts) {
