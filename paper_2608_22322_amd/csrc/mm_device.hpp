@@ -5,7 +5,7 @@
 //
 // Either operand lies in memory with k along its rows (a row for each m or n) or with k down its rows (a row for each
 // k), and is one matrix of 16-bit numbers or the sum of a high and a low part (products of two low parts are dropped). Sums
-// are fp32. k is taken in turns of 64, and where an operand ends inside a turn the other one holds zeros.
+// are fp32. k is taken in turns of 64, and where B ends inside a turn A holds zeros.
 #pragma once
 
 #include <type_traits>
@@ -24,12 +24,16 @@ constexpr int kMmTurn = 64;
 
 // An operand of 16-bit values. k along the rows: `rows` rows of `cols` values each; k down the rows: `rows` values of k, each a row
 // of `cols`. What a tile reaches past either is read from the last row or the last 8 columns instead (cols is a multiple of
-// 8, ld too, and p is 16-byte aligned), for outputs that are not written or against zeros of the other operand.
+// 8, ld too, and p is 16-byte aligned), for outputs that are not written or, by MmEnds, against zeros of the other operand.
 struct MmOperand {
     const uint16_t* p;
     int64_t lo;  // elements from the high part to the low
     int32_t ld, rows, cols;
 };
+
+// Where B's k may end inside a turn: nowhere; what is past the end is the last there is, finite, against A's zeros; or (k along the rows, B of any values: an infinity against a zero would be a
+// NaN) it is A's last 8 columns of its first row, which are zeros then.
+enum MmEnds : int { kMmWhole, kMmLast, kMmZeros };
 
 struct Mm {
     MmOperand a, b;
@@ -100,8 +104,7 @@ __device__ __forceinline__ int mm_swizzle(int k) {
 }
 
 // Sums of 16 x 16 blocks: a lane holds row 16 i + l % 16 and columns 16 j + 4 (l / 16) + 0..3 of its wavefront's part. AK, BK: k along the rows of the operand.
-// ENDS: B may end inside a turn.
-template <class T, int B, bool AK, bool BK, bool ENDS, int PA, int PB>
+template <class T, int B, bool AK, bool BK, int ENDS, int PA, int PB>
 struct MmCore {
     typedef MmTile<B> G;
     typedef __attribute__((address_space(3))) uint16_t* lds_t;
@@ -109,27 +112,31 @@ struct MmCore {
     static constexpr int S = mm_stages<B, PA, PB>();
     typedef MmPlaces<PA, PB, S> Places;
 
+    // k of a piece within its turn, k along the rows
+    static __device__ __forceinline__ int column(int q) { return ((q & 7) ^ ((q >> 3) & 7)) * 8; }
     // byte offset of this thread's piece i of the turn at k0 from the turn's first element. SHORT: the operand may end inside the turn.
     template <bool K, bool SHORT>
     static __device__ __forceinline__ uint32_t offset(const MmOperand& o, int first, int i, int tid, int k0) {
         const int q = i * G::kThreads + tid;
         if (K) {
-            const int r = q >> 3, c = ((q & 7) ^ (r & 7)) * 8;
+            const int r = q >> 3, c = column(q);
             return (uint32_t)(min(first + r, o.rows - 1) - first) * (uint32_t)o.ld * 2u + (uint32_t)(SHORT ? min(k0 + c, o.cols - 8) - k0 : c) * 2u;
         }
         const int k = q / (B / 8), s = q % (B / 8), c = (((s >> 1) ^ mm_swizzle<B>(k)) << 4) | ((s & 1) << 3);
         return (uint32_t)(SHORT ? min(k0 + k, o.rows - 1) - k0 : k) * (uint32_t)o.ld * 2u + (uint32_t)(min(first + c, o.cols - 8) - first) * 2u;
     }
 
-    template <bool K, bool SHORT>
+    template <bool K, int SHORT>
     static __device__ __forceinline__ void issue(const MmOperand& o, const uint16_t* p, int first, int k0, const uint32_t (&off)[G::kChunks], uint16_t* lds,
-                                                 int tid) {
+                                                 int tid, const uint16_t* zeros = nullptr) {
         const char* const at = reinterpret_cast<const char*>(K ? p + (int64_t)first * o.ld + k0 : p + (int64_t)k0 * o.ld + first);
         uint16_t* const to = lds + (tid & ~63) * 8;
 #pragma unroll
         for (int i = 0; i < G::kChunks; ++i) {
-            const uint32_t f = SHORT ? offset<K, SHORT>(o, first, i, tid, k0) : off[i];
-            __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)(at + f),
+            static_assert(K || SHORT != kMmZeros, "");
+            const uint32_t f = SHORT == kMmLast ? offset<K, true>(o, first, i, tid, k0) : off[i];
+            const char* const from = SHORT == kMmZeros && k0 + column(i * G::kThreads + tid) >= o.cols ? reinterpret_cast<const char*>(zeros) : at + f;
+            __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)from,
                                              (__attribute__((address_space(3))) void*)(to + i * G::kThreads * 8), 16, 0, 0);
         }
     }
@@ -180,9 +187,9 @@ struct MmCore {
         int seg = t0 / p.turns, k0 = (t0 - seg * p.turns) * kMmTurn;  // of the next turn to load
         const auto load = [&](int s) __attribute__((always_inline)) {
 #pragma unroll
-            for (int q = 0; q < PA; ++q) issue<AK, false>(p.a, q || (p.amask >> seg) & 1 ? p.a.p + p.a.lo : p.a.p, m0, k0, oa, at.a[s][q], (w << 6) | lane);
+            for (int q = 0; q < PA; ++q) issue<AK, kMmWhole>(p.a, q || (p.amask >> seg) & 1 ? p.a.p + p.a.lo : p.a.p, m0, k0, oa, at.a[s][q], (w << 6) | lane);
 #pragma unroll
-            for (int q = 0; q < PB; ++q) issue<BK, ENDS>(p.b, q || (p.bmask >> seg) & 1 ? p.b.p + p.b.lo : p.b.p, n0, k0, ob, at.b[s][q], (w << 6) | lane);
+            for (int q = 0; q < PB; ++q) issue<BK, ENDS>(p.b, q || (p.bmask >> seg) & 1 ? p.b.p + p.b.lo : p.b.p, n0, k0, ob, at.b[s][q], (w << 6) | lane, p.a.p + (p.a.cols - 8));
             k0 += kMmTurn;
             if (k0 == p.turns * kMmTurn) k0 = 0, ++seg;
         };
@@ -328,7 +335,7 @@ struct MmRows : std::false_type {};
 template <class E>
 struct MmRows<E, std::enable_if_t<E::kRows>> : std::true_type {};
 
-template <class T, int B, bool AK, bool BK, bool ENDS, int PA, class E>
+template <class T, int B, bool AK, bool BK, int ENDS, int PA, class E>
 __global__ __launch_bounds__(MmTile<B>::kThreads, 2) void mm_kernel(Mm p, E end) {
     typedef MmTile<B> G;
     MM_PLACES(B, PA, 1, places);
@@ -383,7 +390,7 @@ __global__ __launch_bounds__(256) void mm_join_kernel(Mm p, E end, uint32_t tile
 }
 
 // B in one part.
-template <class T, int B, bool AK, bool BK, bool ENDS, int PA, class E>
+template <class T, int B, bool AK, bool BK, int ENDS, int PA, class E>
 hipError_t mm_launch(const Mm& p, const E& end, hipStream_t st) {
     const uint32_t tiles = MmTile<B>::tiles(p);
     if (tiles == 0) return hipSuccess;

@@ -492,7 +492,7 @@ __device__ __forceinline__ void segment(const Task<KIND>& task, int tile, int t0
     const MmAt id = mm_at<B>(p, (uint32_t)tile);
     MmAcc acc[G::FM][G::FN] = {};
     constexpr bool kRows = KIND == kPoly || (KIND == kGram ? !TALL : true), kCols = KIND == kPoly || (KIND == kGram ? !TALL : TALL);  // k along the rows
-    MmCore<f16, B, kRows, kCols, false, PARTS, PARTS>::run(p, id.m * B, id.n * B, t0, t1, at, acc);
+    MmCore<f16, B, kRows, kCols, kMmWhole, PARTS, PARTS>::run(p, id.m * B, id.n * B, t0, t1, at, acc);
     if (PIECE || t1 - t0 < p.turns * p.segs) {
         const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
         f32x4* const part = reinterpret_cast<f32x4*>(task.a.part) + (place * G::kWaves + w) * (G::FM * G::FN * 64) + lane;

@@ -265,7 +265,7 @@ struct EndSum {
 };
 
 // PA: parts of A.
-template <bool AK, bool BK, bool ENDS, int PA, class E>
+template <bool AK, bool BK, int ENDS, int PA, class E>
 hipError_t product(const MmCut& cut, Mm p, const E& end, hipStream_t st) {
     p.splits = cut.splits;
     p.segs = mm_segments(cut.tile, 1 + PA);
@@ -348,6 +348,11 @@ hipError_t launch_xent(const XentPlan& p, const Xent& a, void* ws, hipStream_t s
     Stat* const stats = reinterpret_cast<Stat*>(base + p.stat_off);
     Norm* const norms = p.parts ? reinterpret_cast<Norm*>(base + p.norm_off) : nullptr;
     float* const coef = p.parts ? reinterpret_cast<float*>(base + p.coef_off) : nullptr;
+    // The logits' products. (Rows of w that end with a whole turn could take kMmWhole. Its addresses wait in registers, kMmLast's are formed beside the products: 8192 x 32000 x 2048 935 us
+    // so, 953 with the former; kMmZeros' choice for each piece makes both products about 1% longer.)
+    const auto logits = [&](const MmCut& cut, const Mm& g, const auto& end) {
+        return w.cols < p.dp ? product<true, true, kMmZeros, 1>(cut, g, end, st) : product<true, true, kMmLast, 1>(cut, g, end, st);
+    };
     Mm q = {};
     q.part = reinterpret_cast<float*>(base + p.part_off);
     hipError_t e;
@@ -363,7 +368,7 @@ hipError_t launch_xent(const XentPlan& p, const Xent& a, void* ws, hipStream_t s
         g.n = (int32_t)p.vocab;
         g.turns = p.dp / kMmTurn;
         const EndStats end = {stats, at, a.target, t0, n, (int32_t)p.vocab, p.groups};
-        if ((e = product<true, true, true, 1>(p.logits, g, end, st)) != hipSuccess) return e;
+        if ((e = logits(p.logits, g, end)) != hipSuccess) return e;
         loss_kernel<<<(uint32_t)((padded + 3) / 4), 256, 0, st>>>(stats, at, p.groups, t0, n, padded, p.vocab, a.target, a.weight, a.scale, a.loss, a.lse, norms, coef);
     }
     if (!p.parts) return hipGetLastError();
@@ -383,7 +388,7 @@ hipError_t launch_xent(const XentPlan& p, const Xent& a, void* ws, hipStream_t s
         g.n = np;
         g.turns = p.dp / kMmTurn;
         const EndGrad end = {d, size, np, p.parts, p.tp, norms, coef, a.target, v0, (int32_t)p.tokens, n};
-        if ((e = product<true, true, true, 1>(p.back, g, end, st)) != hipSuccess) return e;
+        if ((e = logits(p.back, g, end)) != hipSuccess) return e;
         const MmOperand od = {d, size, np, p.tp, np};
         if (p.dh_parts) {
             Mm g2 = q;
@@ -406,7 +411,7 @@ hipError_t launch_xent(const XentPlan& p, const Xent& a, void* ws, hipStream_t s
                 s.ld = p.hidden;
                 s.rows = p.tp;
             }
-            e = p.dh_parts > 1 ? product<true, false, true, 2>(p.dh, g2, s, st) : product<true, false, true, 1>(p.dh, g2, s, st);
+            e = p.dh_parts > 1 ? product<true, false, kMmLast, 2>(p.dh, g2, s, st) : product<true, false, kMmLast, 1>(p.dh, g2, s, st);
             if (e != hipSuccess) return e;
         }
         if (p.dw_parts) {
@@ -424,7 +429,7 @@ hipError_t launch_xent(const XentPlan& p, const Xent& a, void* ws, hipStream_t s
             s.rows = n;
             s.cols = (int32_t)p.hidden;
             s.out_bf16 = a.dw_bf16;
-            e = p.dw_parts > 1 ? product<false, false, false, 2>(p.dw, g3, s, st) : product<false, false, false, 1>(p.dw, g3, s, st);
+            e = p.dw_parts > 1 ? product<false, false, kMmWhole, 2>(p.dw, g3, s, st) : product<false, false, kMmWhole, 1>(p.dw, g3, s, st);
             if (e != hipSuccess) return e;
         }
     }
