@@ -369,8 +369,8 @@ al_status al_muon_workspace_bytes(const al_tensor* tensors, int32_t nt, const al
 
 /* One step over nt matrices (rows, cols >= 1; a list's 1-D tensors, embedding and head take al_adamw_step). Uses per tensor: param, grad, m, m_meta;
  * the other slots must be NULL, and no two tensors may share memory. step: the 1-based step count, which the update does not depend on. m's codes are al_quantize's, but for values half way between
- * two codes (the position is x fl(127 fl(1 / absmax)) in binary64 here). Per group: the momentum pass (which also sums the squares of u), u into 16-bit parts with its norm, and three
- * products a step of O, the last of which ends in the parameters. ws: device workspace
+ * two codes (the position is x fl(127 fl(1 / absmax)) in binary64 here). Per group: the momentum pass (which also sums the squares of u), the norms of matrices of more than 2^23
+ * elements, u into 16-bit parts with its norm, and three products a step of O, the last of which ends in the parameters. ws: device workspace
  * of at least the queried size, 256-byte aligned. */
 al_status al_muon_step(const al_tensor* tensors, int32_t nt, const al_muon_cfg* cfg, int64_t step, void* ws, size_t ws_bytes, void* stream);
 

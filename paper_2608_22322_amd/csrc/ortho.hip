@@ -93,6 +93,10 @@ __device__ __forceinline__ uint32_t pair(f16 a, f16 b) {
     return (uint32_t)__builtin_bit_cast(uint16_t, a) | (uint32_t)__builtin_bit_cast(uint16_t, b) << 16;
 }
 
+// Partial sums of a matrix that every workgroup of pack_kernel adds up for itself: there is one of these for 2048 elements, and al_muon_step leaves a sum for 8192, so that what is read grows with
+// the square of the size (2^21 x 512: 30 ms of a step's 37). More are added up in a launch before.
+constexpr uint32_t kMostSums = 1024;
+
 struct PackList {
     struct {
         const void* x;
@@ -105,15 +109,24 @@ struct PackList {
     int32_t count;
 };
 
-// x (fp32 or bf16) -> X0 2^10 as one or two fp16 parts, padded with zeros: 8 columns a lane. Each workgroup takes the norm from its partial sums by itself (a launch
+// The norms of the matrices with many partial sums, a workgroup each.
+__global__ __launch_bounds__(256) void norm_kernel(PackList l, double eps, const double* sums, Norm* norms) {
+    const uint32_t b = blockIdx.x, n = l.sums[b + 1] - l.sums[b];
+    if (n <= kMostSums) return;
+    const Norm norm = norm_of(sums + l.sums[b], n, eps);
+    if (threadIdx.x == 0) norms[b] = norm;
+}
+
+// x (fp32 or bf16) -> X0 2^10 as one or two fp16 parts, padded with zeros: 8 columns a lane. Each workgroup takes the norm from up to kMostSums partial sums by itself (a launch
 // less); the first of a matrix writes it for the first step's sums.
 template <typename T>
 __global__ __launch_bounds__(256) void pack_kernel(PackList l, int parts, double eps, const double* sums, Norm* norms) {
     int b = 0;
     while (b + 1 < l.count && blockIdx.x >= l.begin[b + 1]) ++b;
     const auto& t = l.t[b];
-    const Norm norm = norm_of(sums + l.sums[b], l.sums[b + 1] - l.sums[b], eps);
-    if (threadIdx.x == 0 && blockIdx.x == l.begin[b]) norms[b] = norm;
+    const uint32_t n = l.sums[b + 1] - l.sums[b];
+    const Norm norm = n > kMostSums ? norms[b] : norm_of(sums + l.sums[b], n, eps);
+    if (n <= kMostSums && threadIdx.x == 0 && blockIdx.x == l.begin[b]) norms[b] = norm;
     const int64_t i = (int64_t)(blockIdx.x - l.begin[b]) * 256 + threadIdx.x;
     const int chunks = t.cp / 8, r = (int)(i / chunks), c = (int)(i - (int64_t)r * chunks) * 8;
     float v[8] = {};
@@ -885,7 +898,7 @@ hipError_t launch_orthogonalize(int64_t rows, int64_t cols, const OrthoCoefs& k,
     a.out = out;
     a.ldout = ldout;
     a.out_bf16 = out_dtype == AL_DTYPE_BF16;
-    const uint32_t slabs = (uint32_t)std::min<int64_t>(units, 1024);
+    const uint32_t slabs = (uint32_t)std::min<int64_t>(units, kMostSums);
     PackList l;
     std::memset(&l, 0, sizeof(l));
     l.count = 1;
@@ -935,6 +948,11 @@ hipError_t launch_muon(const MuonItem* items, int count, const OrthoCoefs& k, co
     }
     const hipError_t e = launch_momentum(m, l, sums, st);
     if (e != hipSuccess) return e;
+    for (int i = 0; i < count; ++i)
+        if (q.sums[i + 1] - q.sums[i] > kMostSums) {
+            norm_kernel<<<(uint32_t)count, 256, 0, st>>>(q, k.eps, sums, norms);
+            break;
+        }
     pack_kernel<float><<<q.begin[count], 256, 0, st>>>(q, k.parts, k.eps, sums, norms);
     return iterate<kStep>(a, k, st);
 }
