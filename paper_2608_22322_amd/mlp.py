@@ -26,9 +26,9 @@ def _on_its_gpu(method):
     """Run a method with the block's GPU as the current device, where this package's kernels run."""
 
     @functools.wraps(method)
-    def run(self, *args):
+    def run(self, *args, **named):
         with torch.cuda.device(self.device):
-            return method(self, *args)
+            return method(self, *args, **named)
 
     return run
 
