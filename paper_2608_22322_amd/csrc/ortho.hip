@@ -681,7 +681,7 @@ hipError_t launch(OrthoLaunch& a, hipStream_t st) {
 // How a group's product is cut: the tile and, where that is faster by the measured times, the slots that its turns are dealt out to. Slots that work at different places of k
 // share little of what they load: whole tiles run in step and find their neighbours' loads in the L2. What dealing out is for is few tiles and a long sum.
 // Tiles of one length that are some rounds of the device and a few more: the rounds are taken whole, the rest in pieces, up to three rounds of them (4096 x 11008, A: 136
-// tiles of 256, half of a round, 269 us, 528 of 128, of which 16 in 32 pieces each, 221; B 115 and 98).
+// tiles of 256, half of a round, 269 us, 528 of 128, of which 16 in 32 pieces each, 221; B 115 and 98; 1600 x 6400 in two parts, whose rests are more than half a round, 998 us whole, 948 so).
 struct Cut {
     int32_t tile;
     int64_t slots;
@@ -721,7 +721,8 @@ Cut group_cut(const OrthoLaunch& a, int kind) {
         if (same && rest > 0)
             for (const int64_t rounds : {1, 2, 3}) {
                 const int64_t split = std::min<int64_t>(rounds * round / rest, segs * most / (tile > 128 ? 8 : 4)), pieces = rest * split;
-                if (split < 2 || pieces * tile * tile > kPartials) break;
+                if (split < 2) continue;  // a rest of more than half a round in one round
+                if (pieces * tile * tile > kPartials) break;
                 const double t = mm_time(tile, tiles - rest, most, parts) + (double)rounds * (mm_ends(tile, std::min(pieces, round), parts) + std::ceil(n / (double)split) * mm_turn(tile, std::min(pieces, round), parts)) +
                                  9 + (double)(pieces * tile * tile) * 4 / 4e6;
                 if (t < least) least = t, best = {tile, 0, (uint32_t)rest, (uint32_t)split, t};
