@@ -57,7 +57,8 @@
  *
  * Alignment. Every device pointer must be 16-byte aligned (AL_EALIGN), except
  * the matrices of the al_act_*, al_norm_*, al_swiglu_*, al_linear_wgrad and
- * al_orthogonalize calls (see there).
+ * al_orthogonalize calls, and the matrices, ids and vectors of al_embed_* and
+ * al_linear_xent (see there).
  */
 #ifndef AL_H
 #define AL_H
@@ -327,9 +328,10 @@ al_status al_apollo_step(const al_apollo_tensor* tensors, int32_t nt, const al_a
  * A zero matrix gives zeros (also with eps = 0), one that holds an infinity or a NaN gives NaN.
  * parts: what X, A and b A + c A A are held in between the products, whose
  * sums are fp32: 1 = one fp16 number each (11 bits: the result is 1e-3 to 3.5e-3 off for normal matrices, up to 4e-3 where singular values
- * fall as 1 / k), 2 = the sum of two (22 bits; 1e-6 to 6e-6, of the fp32 sums too; three products for one). Where that is less work, two steps are taken at
+ * fall as 1 / k), 2 = the sum of two (22 bits; 1e-6 to 6e-6, of the fp32 sums too; three products for one). Both hold an element of X to no less than 2^-35 of X's norm: in one part
+ * elements below 2^-24 of the norm have fewer bits, in two those below 2^-13. Where that is less work, two steps are taken at
  * once, as X <- a a X + D X with a second A = M A M, M = a I + b A + c A A (the same polynomial of A, other roundings). |G| is a binary64 sum in a fixed order:
- * every result repeats bit for bit.
+ * the same call gives the same bits. (How the products are cut, and whether steps go two at a time, is chosen by the sizes that go together: see al_muon_step.)
  * a, b, c: for singular values of at most 1 to begin with, those of X must stay within 4 and those of b A + c A A within
  * 128 (AL_EINVAL; a = 3.4445, b = -4.7750, c = 2.0315 are usual). steps: 1 to 64.
  * rows, cols up to 2^21, the smaller of them up to 2^16, 2^33 elements (AL_EUNSUPPORTED). */
@@ -370,7 +372,9 @@ al_status al_muon_workspace_bytes(const al_tensor* tensors, int32_t nt, const al
 /* One step over nt matrices (rows, cols >= 1; a list's 1-D tensors, embedding and head take al_adamw_step). Uses per tensor: param, grad, m, m_meta;
  * the other slots must be NULL, and no two tensors may share memory. step: the 1-based step count, which the update does not depend on. m's codes are al_quantize's, but for values half way between
  * two codes (the position is x fl(127 fl(1 / absmax)) in binary64 here). Per group: the momentum pass (which also sums the squares of u), the norms of matrices of more than 2^23
- * elements, u into 16-bit parts with its norm, and three products a step of O, the last of which ends in the parameters. ws: device workspace
+ * elements, u into 16-bit parts with its norm, and three products a step of O, the last of which ends in the parameters. A matrix's parameters may differ by
+ * O's roundings with the list that it is stepped in: the group's sizes choose the tiles and whether steps go two at a time. Its momentum does not. Processes that have to agree bit for bit step
+ * the same lists. ws: device workspace
  * of at least the queried size, 256-byte aligned. */
 al_status al_muon_step(const al_tensor* tensors, int32_t nt, const al_muon_cfg* cfg, int64_t step, void* ws, size_t ws_bytes, void* stream);
 
@@ -501,8 +505,8 @@ al_status al_linear_wgrad(int32_t dtype, const void* dy, int64_t lddy, const voi
  * gradient, whatever its row holds.
  *
  * Sums are fp32 and independent of scheduling: every result repeats bit for
- * bit. tokens and vocab up to 2^31 - 1; with a gradient of the table vocab up to 2^26
- * and ceil(tokens / 32) ceil(cols / 1024) up to 2^23 (AL_EUNSUPPORTED). */
+ * bit. tokens and vocab up to 2^31 - 1; with a gradient of the table vocab up to 2^26, cols up to
+ * 65535 * 1024 and floor(tokens / 32) below floor(2^23 / ceil(cols / 1024)) (AL_EUNSUPPORTED). */
 typedef enum al_index { AL_INDEX_I32 = 0, AL_INDEX_I64 = 1 } al_index;
 
 /* out[t] = scale table[ids[t]], in fp32, rounded once to out_dtype. table:
@@ -534,7 +538,10 @@ al_status al_linear_xent_workspace_bytes(int64_t tokens, int64_t hidden, int64_t
  * dh_dtype; base, dw: packed vocab x hidden of grad_dtype, 16-byte aligned, base NULL = 0, base may be dw itself (dw NULL: base too); NULL where not wanted.
  * Products of bf16 numbers with fp32 sums; d is rounded to bf16 for a bf16 gradient and to the sum of two bf16 numbers (16 bits) for an fp32
  * one. Logits are taken once for the losses and, where a gradient is wanted, again, a piece of the vocabulary at a time: the workspace holds 2^26
- * elements of d (256 columns at least) and, with several pieces, dh in fp32. w: 16-byte aligned; ldw or hidden that is no multiple of 8 costs a copy of w in the
+ * elements of d (256 columns at least) and, with several pieces, dh in fp32; besides a copy of h, the statistics (8 bytes for each 64 columns, 32 in small calls, of up to 16384 tokens at a
+ * time) and what products that are split over their sums leave, up to 256 MiB. Besides the logits' own fp32 sums a loss is as near for large logits as for small ones: it is taken from
+ * differences to a row's largest, and nothing is rounded at the logits' size, but lse. A weight of minus infinity takes its row out of the softmax where h is positive there (dh then has no value).
+ * w: 16-byte aligned; ldw or hidden that is no multiple of 8 costs a copy of w in the
  * workspace. tokens * vocab up to 2^38, tokens * hidden and vocab * hidden up to 2^34, tokens and vocab
  * up to 2^24, hidden up to 2^22 (AL_EUNSUPPORTED). */
 al_status al_linear_xent(const void* h, int64_t ldh, const void* w, int64_t ldw, int64_t tokens, int64_t hidden, int64_t vocab,

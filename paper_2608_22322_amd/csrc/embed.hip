@@ -197,7 +197,8 @@ __device__ __forceinline__ void add_tokens(const EmbedBackward& a, int64_t i0, i
     }
 }
 
-// Two things that the sorted tokens give, side by side: sums over pieces of kPiece tokens of one id, so that a frequent id is not one workgroup's work, and
+// Two things that the sorted tokens give, side by side: sums over pieces of kPiece tokens of one id, so that of a frequent id's tokens one workgroup (for each kSlab columns of its row) is left
+// with a sum for each kPiece, and
 // for each row of the table where its tokens begin (a search by every lane; in the rows' own kernel it would hold up their stores: 8192 tokens, 32000 x 4096 in fp32 225 us).
 template <typename T>
 __global__ __launch_bounds__(256) void piece_kernel(EmbedBackward a, uint32_t pieces, uint32_t slabs) {

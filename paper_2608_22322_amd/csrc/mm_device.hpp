@@ -38,7 +38,8 @@ enum MmEnds : int { kMmWhole, kMmLast, kMmZeros };
 struct Mm {
     MmOperand a, b;
     int32_t m, n, turns;
-    // Operands in parts are taken together by 64-wide tiles (PA, PB: their parts; what is loaded serves two or three products). Larger tiles have no room for it in LDS and take
+    // Operands in parts are taken together by 64-wide tiles (PA, PB: their parts; what is loaded serves two or three products). Larger tiles, whose turns of one part already are 32 and 64 KB (two
+    // parts of both operands would leave one 128-wide workgroup to a compute unit, and a 256-wide one no second turn), take
     // `segs` segments of `turns` turns each instead, segment i with the low part of A (B) where bit i of amask (bmask) is set.
     int32_t segs;
     uint32_t amask, bmask;

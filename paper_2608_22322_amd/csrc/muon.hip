@@ -72,7 +72,8 @@ __global__ __launch_bounds__(256) void momentum_kernel(MomentumList l, MuonArgs 
             for (int m = 1; m < 64; m <<= 1) top = umax(top, (uint32_t)__shfl_xor((int)top, m));
             const float am = u2f(top);
             // A position is x times 127 (1 / absmax), each rounded: within 2 ulps of 127 x / absmax, so that a code differs from one decided by the
-            // quotient only where |x| is half of absmax (position 63.5).
+            // quotient only where that lies half way between two codes (|x| half of absmax, or an absmax whose significand is a multiple of 127); other quotients of fp32 numbers are
+            // 2^-33 or more away from there.
             const double r = am > 0.0f ? 127.0 * (1.0 / (double)am) : 0.0;
             uint32_t q[4];
 #pragma unroll

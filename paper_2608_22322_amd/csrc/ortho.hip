@@ -5,8 +5,9 @@
 //
 // Held between the products as fp16, scaled by powers of two, either one number (11 bits) or the sum of two (22 bits; the
 // products hi hi + hi lo + lo hi). bf16 at the same speed has 8 bits: the products amplify what is lost in X by up to a^steps in
-// directions of small singular values, and the result is 1e-2 off instead of 1.4e-3 (normal matrices). X0 is scaled by a power of two alone, so a bf16 G
-// is held exactly; 1 / |G| goes into the sums of the first step.
+// directions of small singular values, and the result is 1e-2 off instead of 1.4e-3 (normal matrices). X0 is scaled by a power of two alone, so a bf16 G's elements
+// down to 2^-27 of its norm are held exactly; 1 / |G| goes into the sums of the first step. (fp16 ends at 2^-24: nothing is held closer than 2^-35 of X's norm, and two parts have all 22 bits of
+// elements from 2^-13 of it on.)
 //
 // A step is three launches for all the matrices of a group (two where they are narrow, seven for two steps at once). Where whole tiles would leave compute units idle (136
 // tiles for 256 of them, or matrices of different sizes), the group's turns are dealt out evenly instead: a workgroup takes a stretch of them, across tiles, and tiles

@@ -42,7 +42,7 @@ def orthogonalize(x, out, ws, steps: int = 5, coefs=ORTHO_COEFS, eps: float = 1e
 
 class MuonStep:
     """One step per call over a list of ParamState (param, grad, rows, cols) with names: block matrices take al_muon_step, the others al_adamw_step
-    (states allocated here, the momentum by `cfg.m`)."""
+    (states allocated here, the momentum by `cfg.m`). Matrices share launches, and the roundings of one's update go with the list: processes that have to agree bit for bit step the same list."""
 
     def __init__(self, states, names, cfg=None, adamw=None, device="cuda"):
         from . import (Spec, adamw_cfg, adamw_workspace_bytes, alloc_state, muon_cfg, muon_workspace_bytes, tensor_array, workspace)
