@@ -152,3 +152,34 @@ def test_the_head_loss_past_32_bits(tokens, vocab):
         total += d.t().contiguous() @ h[p].double()
         assert float((dh[p].double() - d @ wide).norm()) < 0.01 * float((d @ wide).norm())
     near(dw, total, "dw")
+
+
+def test_the_longest_vocabulary_with_the_most_tokens():
+    """2^38 logits of 64 features: passes of the statistics whose grid stays below 2^32 threads, every token's statistics written. Losses within 64 products summed in fp32 (at most
+    (64 / 32 + 6) 2^-24 of the sum of magnitudes, twice: lse's and the target's) and the sum of 2^24 exponentials (2^-24 for each of 16 in a lane, 8 a thousand groups and 6 at the end)."""
+    import paper_2608_22322_amd as al
+    from paper_2608_22322_amd import vocab as voc
+
+    tokens, vocab = 16384, 1 << 24
+    h = torch.empty(tokens, 64, device="cuda", dtype=torch.bfloat16).normal_()
+    w = torch.empty(vocab, 64, device="cuda", dtype=torch.bfloat16).normal_(0, 1.0 / 8)
+    target = torch.randint(vocab, (tokens,), device="cuda")
+    loss = torch.full((tokens,), float("nan"), device="cuda")
+    ws = al.workspace(voc.linear_xent_workspace_bytes(h, w))
+    ws.fill_(0xff)
+    voc.linear_xent(h, w, target, loss, ws)
+    assert bool(loss.isfinite().all())
+    picked = torch.cat([torch.arange(0, tokens, 700), torch.arange(tokens - 8, tokens), torch.arange(8188, 8196)]).cuda()
+    x = h[picked].double()
+    top, total, size = torch.full((len(picked),), -1e300, dtype=torch.float64, device="cuda"), 0.0, 0.0
+    for p in _parts_of(vocab, 1 << 20):
+        z = x @ w[p].double().t().contiguous()
+        new = torch.maximum(top, z.amax(1))
+        total = total * (top - new).exp() + (z - new[:, None]).exp().sum(1)
+        top = new
+        size = max(size, float((x.abs() @ w[p].double().abs().t().contiguous()).max()))
+    want = top + total.log() - (x * w[target[picked]].double()).sum(1)
+    tol = 2.0**-24 * (2 * 8 * size + 2 * 40 + 300) + 4 * 2.0**-24 * want.abs()
+    off = (loss[picked].double() - want).abs()
+    print(f"off {float(off.max()):.1e} of {float(tol.min()):.1e}", flush=True)
+    assert bool((off <= tol).all())
